@@ -21,7 +21,7 @@ STATUS_NAMES = {0: "DIT_OK", -1: "DIT_EINVAL", -2: "DIT_ENOMEM", -3: "DIT_EHIP",
                 -5: "DIT_EBUDGET", -6: "DIT_ENONFINITE"}
 DTYPE_F32, DTYPE_BF16 = 0, 1
 INDICATOR_MODULATED, INDICATOR_PATCH = 0, 1
-EPI_STORE, EPI_F32, EPI_GATED_RES, EPI_SILU = 0, 1, 2, 4
+EPI_STORE, EPI_F32, EPI_GATED_RES, EPI_SILU, EPI_FP8 = 0, 1, 2, 4, 8
 ABI_VERSION = 4
 POLICIES = {"gate": 0, "static": 1, "threshold": 2}
 SOLVERS = {"euler": 0, "unipc": 1}
@@ -32,7 +32,9 @@ K_CLASSES = ["gemm", "attn", "indicator", "reuse", "full_other", "once"]
 EXPORTS = ["dit_cache_create", "dit_cache_sample", "dit_cache_sample_ex", "dit_cache_sample_batch",
            "dit_gate_logit", "dit_cache_destroy",
            "dit_cache_last_error", "dit_cache_set_profiling", "dit_cache_get_stats",
-           "dit_cache_reset_stats", "dit_gemm_bf16", "dit_attention_bf16", "dit_attention_bf16_noalloc"]
+           "dit_cache_reset_stats", "dit_gemm_bf16", "dit_attention_bf16", "dit_attention_bf16_noalloc",
+           "dit_quant_fp8", "dit_gemm_fp8", "dit_select_blocks_ws_bytes", "dit_select_blocks_bf16",
+           "dit_attention_sparse_ws_bytes", "dit_attention_sparse_bf16"]
 
 
 class ModelConfigC(C.Structure):
@@ -66,6 +68,20 @@ class GemmDescC(C.Structure):
                 ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("flags", C.c_int32),
                 ("gate", C.c_void_p), ("rms_cols", C.c_int32), ("gelu_from", C.c_int32),
                 ("gap_at", C.c_int32), ("gap", C.c_int32)]
+
+
+class GemmFp8DescC(C.Structure):
+    _fields_ = [("A", C.c_void_p), ("lda", C.c_int64), ("a_scale", C.c_void_p), ("ld_as", C.c_int64),
+                ("W", C.c_void_p), ("ldw", C.c_int64), ("w_scale", C.c_void_p), ("ld_ws", C.c_int64),
+                ("bias", C.c_void_p), ("C", C.c_void_p), ("ldc", C.c_int64), ("c_scale", C.c_void_p),
+                ("ld_cs", C.c_int64), ("gate", C.c_void_p), ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32),
+                ("flags", C.c_int32), ("rms_cols", C.c_int32), ("gelu_from", C.c_int32), ("gap_at", C.c_int32),
+                ("gap", C.c_int32)]
+
+
+class SparseShapeC(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("Lq", C.c_int32), ("Lk", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("topk", C.c_int32), ("klen", C.c_void_p)]
 
 
 class DitError(RuntimeError):
@@ -105,10 +121,17 @@ def load(path: str = LIB_PATH):
                                        C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp]
     lib.dit_attention_bf16_noalloc.argtypes = [vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64,
                                                C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp]
+    i32, i64 = C.c_int32, C.c_int64
+    lib.dit_quant_fp8.argtypes = [vp, i32, i64, vp, i64, vp, i64, i32, i32, vp]
+    lib.dit_gemm_fp8.argtypes = [C.POINTER(GemmFp8DescC), vp]
+    shape = C.POINTER(SparseShapeC)
+    lib.dit_select_blocks_ws_bytes.argtypes = lib.dit_attention_sparse_ws_bytes.argtypes = [shape]
+    lib.dit_select_blocks_bf16.argtypes = [shape, vp, i64, vp, i64, i32, vp, vp, vp]
+    lib.dit_attention_sparse_bf16.argtypes = [shape, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, vp]
     for n in EXPORTS:
         f = getattr(lib, n)
         if n not in ("dit_cache_destroy", "dit_cache_last_error"):
-            f.restype = C.c_int
+            f.restype = C.c_size_t if n.endswith("_ws_bytes") else C.c_int
     _lib = lib
     return lib
 
@@ -321,6 +344,171 @@ def attention_bf16_noalloc(q, k, v, o, *, Lq, Lk, heads, ldq, ldk, ldv, ldo, fla
     st = lib.dit_attention_bf16_noalloc(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                         o.data_ptr(), ldo, Lq, Lk, heads, flags, _stream_ptr(stream))
     _check(st, None)
+
+
+# ---- 8-bit products and sparse attention: these calls only enqueue their work
+
+SPARSE_QB, SPARSE_KB = 128, 64
+
+
+def fp8_scale_ld(K: int) -> int:
+    """DIT_FP8_SCALE_LD: least row stride of the scale bytes of rows of K values."""
+    return (K + 511) // 512 * 4
+
+
+def _rows(t, name, rows, width, ld, esize):
+    """Row stride of a device tensor that holds `rows` rows of `width` elements (None: the tensor's own; a
+    tensor of one dimension holds them back to back): the library reads them through a raw pointer."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.element_size() != esize:
+        raise ValueError(f"{name} must have elements of {esize} bytes")
+    if ld is None:
+        ld = t.stride(0) if t.dim() == 2 and t.shape[0] > 1 else width
+    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    have = t.untyped_storage().nbytes() // esize - t.storage_offset()
+    if rows > 0 and (rows - 1) * ld + width > have:
+        raise ValueError(f"{name} must hold {rows} rows of {width} elements with stride {ld}")
+    return ld
+
+
+class _Call:
+    """Device and stream of one call: the tensors' device becomes the current one, the stream (default: that
+    device's current one) must be its own."""
+
+    def __init__(self, stream, first, *more):
+        import torch
+        self._dev = first.device
+        for t in more:
+            if t is not None and t.device != self._dev:
+                raise ValueError("all tensors of a call must be on one device")
+        if stream is not None and stream.device != self._dev:
+            raise ValueError("the stream belongs to another device than the tensors")
+        self._torch, self.stream = torch, stream
+        same = torch.cuda.current_device() == self._dev.index
+        self._guard = None if same else torch.cuda.device(self._dev)
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+        if self.stream is None:
+            self.stream = self._torch.cuda.current_stream(self._dev)
+        self.ptr = C.c_void_p(self.stream.cuda_stream)
+        return self
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+    def workspace(self, ws, nbytes, name):
+        """The caller's workspace, or one of the caching allocator's, taken on the call's own stream."""
+        if nbytes == 0:
+            return None
+        if ws is None:
+            with self._torch.cuda.stream(self.stream):
+                return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self._dev)
+        if not ws.is_cuda or ws.device != self._dev or not ws.is_contiguous() or ws.numel() * ws.element_size() < nbytes:
+            raise ValueError(f"{name} must be a contiguous tensor of {nbytes} bytes on the call's device")
+        return ws
+
+
+def quant_fp8(x, q, scale, *, M, K, ldx=None, ldq=None, lds=None, stream=None):
+    """dit_quant_fp8: rows of x (torch.float32, else bf16 as torch.bfloat16 or int16) to e4m3 bytes q and
+    E8M0 scale bytes (uint8 or torch's 8-bit float types)."""
+    lib = load()
+    f32 = x.element_size() == 4
+    if f32 and not x.is_floating_point():
+        raise ValueError("x must be float32 or bf16")
+    ldx = _rows(x, "x", M, K, ldx, 4 if f32 else 2)
+    ldq = _rows(q, "q", M, K, ldq, 1)
+    lds = _rows(scale, "scale", M, fp8_scale_ld(K), lds, 1)
+    with _Call(stream, x, q, scale) as call:
+        _check(lib.dit_quant_fp8(x.data_ptr(), DTYPE_F32 if f32 else DTYPE_BF16, ldx, q.data_ptr(), ldq,
+                                 scale.data_ptr(), lds, M, K, call.ptr))
+
+
+def gemm_fp8(A, a_scale, W, w_scale, bias, Cout, *, M, N, K, lda=None, ld_as=None, ldw=None, ld_ws=None, ldc=None,
+             c_scale=None, ld_cs=None, flags=EPI_STORE, gate=None, rms_cols=0, gelu_from=None, gap_at=0, gap=0,
+             stream=None):
+    """dit_gemm_fp8 on torch cuda tensors: 8-bit rows as uint8 or torch's 8-bit float types, bias and Cout as in
+    gemm_bf16 (Cout e4m3 with EPI_FP8, c_scale its scale bytes)."""
+    lib = load()
+    lda, ldw = _rows(A, "A", M, K, lda, 1), _rows(W, "W", N, K, ldw, 1)
+    ld_as = _rows(a_scale, "a_scale", M, fp8_scale_ld(K), ld_as, 1)
+    ld_ws = _rows(w_scale, "w_scale", N, fp8_scale_ld(K), ld_ws, 1)
+    width = N + (gap if gap and gap_at < N else 0)
+    ldc = _rows(Cout, "Cout", M, width, ldc, 4 if flags & EPI_F32 else 1 if flags & EPI_FP8 else 2)
+    if bias is not None:
+        _rows(bias, "bias", 1, N, None, 2)
+    if gate is not None:
+        _rows(gate, "gate", 1, N, None, 4)
+    if flags & EPI_FP8 and c_scale is not None:
+        ld_cs = _rows(c_scale, "c_scale", M, fp8_scale_ld(N), ld_cs, 1)
+    d = GemmFp8DescC(A.data_ptr(), lda, a_scale.data_ptr(), ld_as, W.data_ptr(), ldw, w_scale.data_ptr(), ld_ws,
+                     bias.data_ptr() if bias is not None else None, Cout.data_ptr(), ldc,
+                     c_scale.data_ptr() if c_scale is not None else None, ld_cs if ld_cs is not None else 0,
+                     gate.data_ptr() if gate is not None else None, M, N, K, flags, rms_cols,
+                     gelu_from if gelu_from is not None else 0x7FFFFFFF, gap_at, gap)
+    with _Call(stream, A, a_scale, W, w_scale, bias, Cout, c_scale, gate) as call:
+        _check(lib.dit_gemm_fp8(C.byref(d), call.ptr))
+
+
+def sparse_shape(*, Lq, Lk, heads, topk, kv_heads=None, batch=1, klen=None) -> SparseShapeC:
+    """dit_sparse_shape; klen: int32 cuda tensor [batch] or None."""
+    if klen is not None:
+        _rows(klen, "klen", 1, batch, None, 4)
+        if klen.is_floating_point():
+            raise ValueError("klen must be int32")
+    return SparseShapeC(batch, Lq, Lk, heads, kv_heads if kv_heads is not None else heads, topk,
+                        klen.data_ptr() if klen is not None else None)
+
+
+def select_blocks_ws_bytes(**shape) -> int:
+    return load().dit_select_blocks_ws_bytes(C.byref(sparse_shape(**shape)))
+
+
+def attention_sparse_ws_bytes(**shape) -> int:
+    return load().dit_attention_sparse_ws_bytes(C.byref(sparse_shape(**shape)))
+
+
+def _lists(idx, s):
+    if idx.is_floating_point():
+        raise ValueError("idx must be int32")
+    _rows(idx, "idx", 1, s.batch * s.heads * -(-s.Lq // SPARSE_QB) * s.topk, None, 4)
+    if not idx.is_contiguous():
+        raise ValueError("idx must be contiguous")
+
+
+def select_blocks_bf16(q, k, idx, *, first=0, ldq=None, ldk=None, ws=None, stream=None, **shape):
+    """dit_select_blocks_bf16: idx int32 [batch, heads, ceil(Lq / 128), topk]; shape as in sparse_shape; ws None:
+    a workspace of torch's caching allocator."""
+    lib = load()
+    s = sparse_shape(**shape)
+    ldq = _rows(q, "q", s.batch * s.Lq, s.heads * 128, ldq, 2)
+    ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2)
+    _lists(idx, s)
+    with _Call(stream, q, k, idx, shape.get("klen")) as call:
+        w = call.workspace(ws, lib.dit_select_blocks_ws_bytes(C.byref(s)) or 16, "ws")
+        _check(lib.dit_select_blocks_bf16(C.byref(s), q.data_ptr(), ldq, k.data_ptr(), ldk, first, idx.data_ptr(),
+                                          w.data_ptr(), call.ptr))
+
+
+def attention_sparse_bf16(q, k, v, o, idx, *, flags=0, ldq=None, ldk=None, ldv=None, ldo=None, ws=None, stream=None,
+                          **shape):
+    """dit_attention_sparse_bf16; idx as select_blocks_bf16 writes it, shape as in sparse_shape."""
+    lib = load()
+    s = sparse_shape(**shape)
+    ldq = _rows(q, "q", s.batch * s.Lq, s.heads * 128, ldq, 2)
+    ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2)
+    ldv = _rows(v, "v", s.batch * s.Lk, s.kv_heads * 128, ldv, 2)
+    ldo = _rows(o, "o", s.batch * s.Lq, s.heads * 128, ldo, 2)
+    _lists(idx, s)
+    with _Call(stream, q, k, v, o, idx, shape.get("klen")) as call:
+        w = call.workspace(ws, lib.dit_attention_sparse_ws_bytes(C.byref(s)), "ws")
+        _check(lib.dit_attention_sparse_bf16(C.byref(s), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                             o.data_ptr(), ldo, idx.data_ptr(), flags,
+                                             w.data_ptr() if w is not None else None, call.ptr))
 
 
 def gate_logit(gate_blob, features) -> float:

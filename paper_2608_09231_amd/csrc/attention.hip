@@ -18,18 +18,12 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"
 
 namespace dit {
 namespace {
-
-constexpr int D = 128;
-constexpr int KT = 64;        // keys per tile
-constexpr float RESCALE_SLACK = 8.f;  // log2 units a stale max may lag behind
-
-typedef __attribute__((address_space(3))) void lds_void_t;
-typedef __attribute__((address_space(1))) void glb_void_t;
 
 // Position of key k (0..31) inside its 32-key group of the transposed V: the
 // two 4-key runs a lane quarter needs for one MFMA k-step become adjacent.
@@ -39,7 +33,6 @@ __host__ __device__ constexpr int vt_slot(int k) { return 8 * ((k >> 2) & 3) + 4
 // stored at chunk c ^ (r & 15); V^T [128 d][64 keys], chunk c of row d at
 // c ^ ((d >> 1) & 7).  Both make the MFMA operand reads of 16 consecutive
 // rows hit 16 distinct 16-byte bank groups.
-__device__ __forceinline__ int k_off(int row, int c) { return row * 256 + ((c ^ (row & 15)) << 4); }
 __device__ __forceinline__ int v_off(int d, int c) { return d * 128 + ((c ^ ((d >> 1) & 7)) << 4); }
 
 // Rows of one joint sequence that lies in two pieces (the text rows of a
@@ -60,13 +53,6 @@ struct SeqMap {
 };
 
 constexpr int TILE_BYTES = 2 * KT * D * 2;
-
-// With q and k RMS-normalised to unit gain, |q.k| <= |q||k| <= 128, so a
-// logit q.k / sqrt(128) never exceeds sqrt(128) = 11.31 (bf16 rounding of q
-// and k adds < 1%).  A fixed shift of 11.5 (natural units) then replaces the
-// running maximum exactly (softmax is shift invariant) and keeps every
-// exp(s - 11.5) <= 1.
-constexpr float BOUNDED_SHIFT_LOG2 = 11.5f * 1.4426950408889634f;
 
 // What bounds it: at many keys the board's power (the clock sits near 2.05 GHz)
 // and the softmax beside the products (VALU and MFMA each about 0.6 busy); at
@@ -135,42 +121,6 @@ struct Shares {
 // Partial output of a piece: O^T in register order (wave, 16 blocks of 16 d x
 // 16 queries, lane, 4 d), then the queries' row sums and running maxima.
 constexpr int PIECE_FLOATS = QB * D + 2 * QB;
-
-// Lanes l, l ^ 16, l ^ 32, l ^ 48 combined, by lane swaps on the VALU (a
-// shuffle through LDS would hold up the fragment reads).
-template <typename F>
-__device__ __forceinline__ float over_quarters(float v, F op) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const uint32_t u = __float_as_uint(v);
-  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  const float w = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const uint32_t x = __float_as_uint(w);
-  const auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
-#else
-  return v;
-#endif
-}
-__device__ __forceinline__ float max_quarters(float v) {
-  return over_quarters(v, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float sum_quarters(float v) {
-  return over_quarters(v, [](float a, float b) { return a + b; });
-}
-
-// -m as the softmax's shift.  A query whose logits so far are all -inf
-// (overflow) has no maximum yet: exp2(-inf + 0) = 0 leaves its sums at zero,
-// where exp2(-inf + inf) would make them NaN for good.
-__device__ __forceinline__ float neg_shift(float m) { return m == -INFINITY ? 0.f : -m; }
-
-// 16 bytes per lane from base + off (bytes, valid up to `bytes`; zeros past
-// it) into LDS at dst + 16 lane.
-__device__ __forceinline__ void copy16(const void* base, uint32_t bytes, lds_void_t* dst, uint32_t off) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, (int)bytes, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, off, 0, 0, 0);
-#endif
-}
 
 template <bool BOUNDED>
 __global__ __launch_bounds__(64 * NW) void flash_attn_kernel(

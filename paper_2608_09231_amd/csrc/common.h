@@ -123,5 +123,30 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
 
+// ---- 8-bit floating point (e4m3) with power-of-two scales (E8M0 bytes) ----
+
+// Scale byte of values whose largest magnitude has the bits `top` (compared as
+// integers, so that a NaN stays the largest): the least e >= -127 with
+// top <= 448 * 2^e, plus 127; 255 where the largest is not finite.  448 =
+// 1.75 * 2^8: adding 0x1fffff to the bits carries into the exponent exactly
+// for mantissas above 1.75.
+__device__ __forceinline__ uint32_t e8m0_of(uint32_t top) {
+  const int e = (int)((top + 0x1fffffu) >> 23) - 8;
+  return top >= 0x7f800000u ? 255u : (uint32_t)(e < 0 ? 0 : e);
+}
+// 1 / 2^(byte - 127), exact; NaN for 255, which turns the whole block into NaNs.
+__device__ __forceinline__ float e8m0_inverse(uint32_t byte) {
+  return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float((254u - byte) << 23);
+}
+// Four floats of magnitude <= 448 (or NaN) to e4m3, round to nearest even.
+__device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+#else
+  return 0;
+#endif
+}
+
 #define DIT_LN_EPS 1e-6f
 #define DIT_RMS_EPS 1e-6f

@@ -1527,6 +1527,16 @@ dit_status run_batch(dit_cache* c, int S, float* latents, const void* text_emb, 
 
 }  // namespace
 
+namespace dit {
+dit_status component_fail(dit_status st, const char* msg) noexcept {
+  try {
+    g_create_error = msg;
+  } catch (...) {  // no memory for the message: the status says enough
+  }
+  return st;
+}
+}  // namespace dit
+
 // ------------------------------------------------------- components' scratch
 // Device memory of dit_attention_bf16_noalloc, which allocates nothing: the
 // transposed values, and the f32 pieces of a shared last round.  Its callers

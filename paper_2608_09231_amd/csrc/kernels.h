@@ -101,6 +101,33 @@ hipError_t launch_attn_f32(const float* q, int64_t ldq, const float* k, int64_t 
                            const float* v, int64_t ldv, float* o, int64_t ldo, int Lq, int Lk,
                            int heads, int head_dim, hipStream_t s);
 
+// ---- 8-bit products and sparse attention (enqueue only; arguments checked by
+// the C entry points) ----
+struct GemmFp8Args {
+  const void* A; int64_t lda;
+  const void* W; int64_t ldw;
+  const void* As; int64_t ldas;
+  const void* Ws; int64_t ldws;
+  const void* bias;
+  void* C; int64_t ldc;
+  void* Cs; int64_t ldcs;
+  const float* gate;
+  int M, N, K;
+  int flags, rms_cols, gelu_from, gap_at, gap;
+};
+hipError_t launch_quant_fp8(const void* x, bool bf16, int64_t ldx, void* q, int64_t ldq, void* scale, int64_t lds, int M,
+                            int K, hipStream_t s);
+hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu);
+size_t select_blocks_ws_bytes(const dit_sparse_shape& s);
+hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                int first, int32_t* idx, void* ws, hipStream_t st);
+size_t attention_sparse_ws_bytes(const dit_sparse_shape& s);
+hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, bool bounded,
+                                   void* ws, hipStream_t st);
+// Status and message of a failed component call (dit_cache_last_error(NULL)).
+dit_status component_fail(dit_status st, const char* msg) noexcept;
+
 // ---- streaming kernels, templated on the storage type (float or bf16) ----
 // out = S(LN(x) * (1 + scale) + shift) per row; rows < split use (sh0, sc0),
 // the others (sh1, sc1); mod vectors are f32.  scale == nullptr: plain LN.

@@ -1,0 +1,583 @@
+"""8-bit rows and their products, block selection and sparse attention against
+plain float64 forms, through the C ABI, at the sizes, strides and masks where
+they can go wrong."""
+import numpy as np
+import pytest
+
+from paper_2608_09231_amd import binding
+from tests import _operators as ref
+from tests._gpu import dev, host_bf16, torch_cuda
+from tests.test_gpu_kernels import bf16_bits, bits_to_f64
+
+pytestmark = pytest.mark.gpu
+
+BF16 = 2.0 ** -8    # half a step, relative
+FILL = 0x5A
+
+
+def rng(*seed):
+    return np.random.default_rng([77, *seed])
+
+
+def strided(torch, a, ld, fill=FILL):
+    """A device buffer of rows `ld` elements apart whose gaps hold `fill` bytes."""
+    M, K = a.shape
+    buf = np.full((M, ld), 0, a.dtype)
+    buf.view(np.uint8)[:] = fill
+    buf[:, :K] = a
+    return dev(torch, buf)
+
+
+def run_quant(torch, x, *, ldx=None, ldq=None, lds=None):
+    M, K = x.shape
+    ld = ldx or K
+    q = torch.full((M, ldq or K), FILL, dtype=torch.uint8, device="cuda")
+    s = torch.full((M, lds or binding.fp8_scale_ld(K)), FILL, dtype=torch.uint8, device="cuda")
+    binding.quant_fp8(strided(torch, x, ld), q, s, M=M, K=K)
+    q, s = q.cpu().numpy(), s.cpu().numpy()
+    nb = -(-K // 128)
+    assert (q[:, K:] == FILL).all() and (s[:, nb:] == FILL).all()
+    return q[:, :K], s[:, :nb]
+
+
+def check_quant(torch, x, **kw):
+    q, s = run_quant(torch, x, **kw)
+    x64 = bits_to_f64(x) if x.dtype == np.uint16 else x.astype(np.float64)
+    rq, rs = ref.quantise(x64)
+    np.testing.assert_array_equal(s, rs)
+    # -0 and +0 are one value; any NaN byte is a NaN
+    np.testing.assert_array_equal(ref.TABLE[q], ref.TABLE[rq])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,ldx,ldq,lds", [
+    (1, 16, None, None, None), (3, 128, None, None, None), (5, 144, 160, 176, 8), (37, 2608, 2616, 2624, 28),
+    (130, 1040, None, None, None), (1030, 1008, 1024, 1008, 12)])
+def test_quant_rows(M, K, ldx, ldq, lds, dtype):
+    torch = torch_cuda()
+    r = rng(M, K)
+    x = r.standard_normal((M, K)) * np.exp(3 * r.standard_normal((M, 1))) * np.exp(r.standard_normal(K))
+    check_quant(torch, bf16_bits(x) if dtype == "bf16" else x.astype(np.float32), ldx=ldx, ldq=ldq, lds=lds)
+
+
+def test_quant_borders_zeros_and_extremes():
+    """Blocks whose largest value is a scale's last (448 * 2^e) or the next above it, ties between two e4m3
+    values, blocks of zeros, the type's smallest and largest values."""
+    torch = torch_cuda()
+    rows = []
+    for e in (-150, -136, -135, -126, -20, 0, 60, 119):
+        top = np.float32(448) * np.float32(2.0) ** e if e > -149 else np.float32(1e-45)
+        for a in (top, np.nextafter(top, np.float32(np.inf)), np.nextafter(top, np.float32(0))):
+            row = np.zeros(128, np.float32)
+            row[17] = -a
+            row[:8] = a * np.array([1, 15 / 16, 0.5, 0.53125, 0.59375, 1 / 448, 1 / 458752, 3 / 917504], np.float32)
+            rows.append(row)
+    rows.append(np.zeros(128, np.float32))
+    rows.append(np.full(128, np.finfo(np.float32).max))
+    rows.append(np.full(128, -0.0, np.float32))
+    check_quant(torch, np.stack(rows).astype(np.float32))
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_quant_block_that_is_not_finite(bad):
+    torch = torch_cuda()
+    x = rng(5).standard_normal((6, 512)).astype(np.float32)
+    x[2, 200] = bad
+    check_quant(torch, x)
+    check_quant(torch, bf16_bits(np.where(np.isfinite(x), x, 0)) | np.where(np.isnan(x), 0x7FC0, np.where(
+        np.isinf(x), np.where(x > 0, 0x7F80, 0xFF80), 0)).astype(np.uint16))
+
+
+def test_quant_nothing_to_do():
+    torch = torch_cuda()
+    x = torch.zeros(4, 32, device="cuda")
+    q = torch.full((4, 32), FILL, dtype=torch.uint8, device="cuda")
+    s = torch.full((4, 4), FILL, dtype=torch.uint8, device="cuda")
+    binding.quant_fp8(x, q, s, M=0, K=32)
+    binding.quant_fp8(x, q, s, M=4, K=0)
+    assert int((q != FILL).sum()) == 0 and int((s != FILL).sum()) == 0
+
+
+# ---------------------------------------------------------------- products
+
+def operand(r, M, K, spread=1.0):
+    """8-bit rows with row and block scales of their own."""
+    x = r.standard_normal((M, K)) * np.exp(spread * r.standard_normal((M, 1))) / np.sqrt(K)
+    return ref.quantise(bits_to_f64(bf16_bits(x)))
+
+
+def padded_scale(s, K, ld=None):
+    out = np.full((s.shape[0], ld or binding.fp8_scale_ld(K)), 255, np.uint8)   # NaN scales past the last block
+    out[:, :s.shape[1]] = s
+    return out
+
+
+def run_gemm(M, N, K, *, out="bf16", act="none", rms_cols=0, gelu_from=None, bias=True, gap_at=0, gap=0, pad=0,
+             seed=0, operands=None, stream=None):
+    torch = torch_cuda()
+    r = rng(M, N, K, seed)
+    (aq, as_), (wq, ws) = operands or (operand(r, M, K), operand(r, N, K))
+    b_bits = bf16_bits(0.1 * r.standard_normal(N))
+    b = bits_to_f64(b_bits)
+    a, w = ref.values(aq, as_), ref.values(wq, ws)
+    y, d = ref.product(a, w, b if bias else None, f32=out == "f32", act=act, rms_cols=rms_cols, gelu_from=gelu_from)
+    flags = {"bf16": 0, "f32": binding.EPI_F32, "fp8": binding.EPI_FP8, "gated": binding.EPI_GATED_RES}[out]
+    flags |= binding.EPI_SILU if act == "silu" else 0
+    width = N + gap + pad
+    esize = {"bf16": 2, "gated": 2, "f32": 4, "fp8": 1}[out]
+    old_bits = bf16_bits(r.standard_normal((M + 1, width)))
+    C = dev(torch, old_bits) if out == "gated" else torch.full((M + 1, width * esize), FILL, dtype=torch.uint8,
+                                                               device="cuda")
+    if out != "gated":
+        C = C.view({"bf16": torch.int16, "f32": torch.float32, "fp8": torch.uint8}[out])
+    gate = r.standard_normal(N).astype(np.float32)
+    cs = torch.full((M + 1, binding.fp8_scale_ld(N)), FILL, dtype=torch.uint8, device="cuda") if out == "fp8" else None
+    binding.gemm_fp8(strided(torch, aq, K + (16 if pad else 0), 0x7F), dev(torch, padded_scale(as_, K)),
+                     strided(torch, wq, K + (48 if pad else 0), 0x7F), dev(torch, padded_scale(ws, K)),
+                     dev(torch, b_bits) if bias else None, C, M=M, N=N, K=K, flags=flags, c_scale=cs,
+                     gate=dev(torch, gate) if out == "gated" else None, rms_cols=rms_cols, gelu_from=gelu_from,
+                     gap_at=gap_at, gap=gap)
+    torch.cuda.synchronize()
+    host = C.cpu().numpy()
+    cols = np.arange(N) + np.where(np.arange(N) >= gap_at, gap, 0)
+    rest = np.delete(np.arange(width), cols)
+    if out == "gated":
+        old = bits_to_f64(old_bits)
+        got = host_bf16(C)
+        assert (got[M] == old[M]).all() and (got[:, rest] == old[:, rest]).all()
+        y, d = old[:M, cols] + gate * y, np.abs(gate) * d + 2.0 ** -22 * (np.abs(old[:M, cols]) + np.abs(gate * y))
+        got = got[:M, cols]
+    else:
+        raw = host.view(np.uint8).reshape(M + 1, width, esize)
+        assert (raw[M] == FILL).all() and (raw[:, rest] == FILL).all(), "bytes outside the output changed"
+        if out == "fp8":
+            scale = cs.cpu().numpy()
+            nb = N // 128
+            assert (scale[M] == FILL).all() and (scale[:, nb:] == FILL).all()
+            scale = scale[:M, :nb]
+            got = ref.values(host[:M, :N], scale)
+            # the scale is that of the largest value, up to what that may be off
+            s = np.repeat(2.0 ** (scale.astype(np.float64) - 127), 128, 1)
+            top = np.repeat((np.abs(y)).reshape(M, nb, 128).max(2), 128, 1)
+            off = np.repeat(d.reshape(M, nb, 128).max(2), 128, 1)
+            fits = (top - off <= 448 * s) & ((top + off > 224 * s) | (scale.repeat(128, 1) == 0))
+            assert (fits | np.isnan(top)).all()     # (rows that are not finite have their own test)
+            tol = np.maximum(2.0 ** -4 * (np.abs(y) + d), 2.0 ** -10 * s) + d
+            return host[:M], scale, got, y, tol
+        got = (host_bf16(C) if out == "bf16" else host.astype(np.float64))[:M, cols]
+    tol = d + (2.0 ** -24 if out == "f32" else BF16) * (np.abs(y) + d) + 1e-30
+    return host[:M], None, got, y, tol
+
+
+def check_gemm(*a, **kw):
+    _, _, got, y, tol = run_gemm(*a, **kw)
+    worst = np.max(np.abs(got - y) / tol)
+    assert worst <= 1, f"{worst} of the tolerance at {np.unravel_index(np.argmax(np.abs(got - y) / tol), y.shape)}"
+
+
+# one size for each kernel and edge: few rows (one and two blocks of 16), tiles of 64 and 128 rows, 256 x 256 tiles;
+# blocks of K cut short, fewer slices than stages
+SIZES = [(1, 8, 16), (1, 1000, 2320), (16, 72, 128), (17, 264, 400), (40, 136, 5120), (300, 2056, 272), (513, 1416, 1040),
+         (70, 13824, 656), (1500, 5640, 144), (2100, 4104, 528)]
+RING = [(4100, 4360, 16), (4100, 4360, 144), (4096, 4096, 1152), (4353, 3848, 912)]
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "gated"])
+@pytest.mark.parametrize("M,N,K", SIZES + RING)
+def test_gemm_sizes(M, N, K, out):
+    check_gemm(M, N, K, out=out, pad=8 if (M + K) % 3 else 0, bias=(M % 4) > 0)
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "silu", "rms"])
+@pytest.mark.parametrize("M,N,K", [(1, 128, 528), (19, 256, 400), (257, 1152, 272), (700, 7040, 1040), (4097, 4480, 272)])
+def test_gemm_fp8_output(M, N, K, act):
+    check_gemm(M, N, K, out="fp8", act=act, rms_cols=N if act == "rms" else 0, gelu_from=0 if act == "gelu" else None,
+               pad=16 if M % 2 else 0)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(3, 512, 400), (30, 640, 272), (300, 2688, 400), (2100, 4224, 272), (4100, 4352, 272)])
+def test_gemm_norm_gelu_and_gap(M, N, K, out):
+    """A fused projection: normed q and k columns, plain values, GELU past a gap; then per-column forms."""
+    check_gemm(M, N, K, out=out, rms_cols=256, gelu_from=384, gap_at=384, gap=128, seed=1)
+    check_gemm(M, N, K, out=out, rms_cols=128, gelu_from=204, gap_at=140, gap=12, pad=8 - (N + 12) % 8, seed=2)
+    check_gemm(M, N, K, out=out, act="silu", seed=3)
+
+
+def test_gemm_scales_across_the_range():
+    """Row scales over 2^-120 .. 2^120 whose products stay in range, and a smallest and a largest scale byte."""
+    r = rng(9)
+    for M, N, K in ((5, 64, 400), (300, 2048, 400), (4100, 4352, 400)):
+        a, w = operand(r, M, K), operand(r, N, K)
+        e = r.integers(-100, 100, K // 128 + 1)
+        a[1][:] = np.clip(a[1].astype(int) + e, 0, 254)
+        w[1][:] = np.clip(w[1].astype(int) - e, 0, 254)
+        for out in ("bf16", "f32"):
+            check_gemm(M, N, K, out=out, operands=(a, w), bias=False)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("M,N", [(4, 128), (300, 2048), (4100, 4352)])
+def test_gemm_nan_rows_stay_in_their_rows(M, N, out):
+    K = 272
+    r = rng(M, N, 3)
+    x = r.standard_normal((M, K))
+    x[3, 200] = np.inf
+    a = ref.quantise(x)
+    w = operand(r, N, K)
+    host, scale, got, y, tol = run_gemm(M, N, K, out=out, operands=(a, w))
+    assert np.isnan(got[3]).all()
+    rest = np.arange(M) != 3
+    assert (np.abs(got - y)[rest] <= tol[rest]).all()
+    if out == "fp8":
+        assert (scale[3] == 255).all()
+
+
+def test_gemm_no_rows_or_columns():
+    torch = torch_cuda()
+    z = torch.zeros(64, 64, dtype=torch.uint8, device="cuda")
+    C = torch.full((8, 8), 7.0, device="cuda")
+    for M, N in ((0, 8), (8, 0)):
+        binding.gemm_fp8(z, z, z, z, None, C, M=M, N=N, K=64, flags=binding.EPI_F32)
+    assert int((C != 7).sum()) == 0
+
+
+# ---------------------------------------------------------------- selection and attention
+
+def tokens(r, rows, heads, pad=0, scale=1.0):
+    """bf16 bits [rows, heads 128 + pad] (gaps NaN) and their float64 values."""
+    x = r.standard_normal((rows, heads, 128)) + r.standard_normal((rows // 40 + 1, heads, 128)).repeat(40, 0)[:rows]
+    x *= scale / np.sqrt((x ** 2).mean(2, keepdims=True))
+    bits = np.full((rows, heads * 128 + pad), 0x7FC0, np.uint16)
+    bits[:, :heads * 128] = bf16_bits(x.reshape(rows, -1))
+    return bits, bits_to_f64(bits[:, :heads * 128])
+
+
+def shape_of(Lq, Lk, heads, topk, kv_heads=None, batch=1, klen=None):
+    return dict(Lq=Lq, Lk=Lk, heads=heads, topk=topk, kv_heads=kv_heads, batch=batch, klen=klen)
+
+
+def on_device(torch, shape):
+    k = shape["klen"]
+    return dict(shape, klen=None if k is None else torch.tensor(k, dtype=torch.int32, device="cuda"))
+
+
+def run_select(torch, qb, kb, shape, first):
+    nqb = -(-shape["Lq"] // 128)
+    idx = torch.full((shape["batch"], shape["heads"], nqb, shape["topk"]), -77, dtype=torch.int32, device="cuda")
+    binding.select_blocks_bf16(dev(torch, qb), dev(torch, kb), idx, first=first, **on_device(torch, shape))
+    return idx.cpu().numpy()
+
+
+SELECT = [
+    (shape_of(1, 1, 1, 1), 0), (shape_of(1, 63, 2, 3), 0), (shape_of(127, 64, 1, 1), 1), (shape_of(129, 65, 3, 2), 0),
+    (shape_of(300, 5000, 4, 9, kv_heads=2), 2), (shape_of(1, 5000, 6, 17, kv_heads=3, batch=3, klen=[5000, 0, 4033]), 1),
+    (shape_of(2049, 1025, 2, 5, batch=2, klen=[1, 1025]), 0), (shape_of(700, 20000, 1, 33), 0),
+    (shape_of(130, 40000, 1, 600), 3), (shape_of(130, 70000, 1, 64, klen=[69999]), 1), (shape_of(64, 300000, 1, 7), 0)]
+
+
+@pytest.mark.parametrize("shape,first", SELECT)
+@pytest.mark.parametrize("pad", [0, 24])
+def test_select_blocks(shape, first, pad):
+    torch = torch_cuda()
+    r = rng(shape["Lq"], shape["Lk"])
+    qb, q = tokens(r, shape["batch"] * shape["Lq"], shape["heads"], pad)
+    kb, k = tokens(r, shape["batch"] * shape["Lk"], shape["kv_heads"] or shape["heads"], pad)
+    if shape["klen"]:   # rows past a sequence's keys may hold anything
+        for z, n in enumerate(shape["klen"]):
+            kb[z * shape["Lk"] + n:(z + 1) * shape["Lk"], :] = 0x7FC0
+    np.testing.assert_array_equal(run_select(torch, qb, kb, shape, first), ref.select(q, k, first=first, **shape))
+
+
+@pytest.mark.parametrize("Lk", [640, 5000, 40000, 70000])
+def test_select_ties_go_to_the_lowest_block(Lk):
+    """Small whole numbers, equal blocks: sums, means and products are exact, so ties are ties."""
+    torch = torch_cuda()
+    r = rng(Lk)
+    nkb = -(-Lk // 64)
+    kinds = r.integers(-2, 3, (4, 128)).astype(float)
+    k = kinds[r.integers(0, 4, nkb)].repeat(64, 0)[:Lk]
+    q = r.integers(-2, 3, (256, 128)).astype(float)
+    q[128:] = 0                                     # every product is zero
+    shape = shape_of(256, Lk, 1, min(nkb, 7))
+    got = run_select(torch, bf16_bits(q), bf16_bits(k), shape, 0)
+    np.testing.assert_array_equal(got, ref.select(q, k, **shape))
+    np.testing.assert_array_equal(got[0, 0, 1], np.arange(min(nkb, 7)))
+
+
+def test_select_infinities_and_nan():
+    torch = torch_cuda()
+    r = rng(4)
+    shape = shape_of(128, 64 * 6, 1, 3)
+    qb, q = tokens(r, 128, 1)
+    kb, k = tokens(r, 64 * 6, 1)
+    for block, bits in ((1, 0x7FC0), (2, 0x7F80), (4, 0xFF80)):
+        kb[64 * block + 5, 9] = bits
+    k = bits_to_f64(kb)
+    np.testing.assert_array_equal(run_select(torch, qb, kb, shape, 0), ref.select(q, k, **shape))
+    np.testing.assert_array_equal(run_select(torch, qb, kb, shape, 2), ref.select(q, k, first=2, **shape))
+
+
+def run_attention(torch, qb, kb, vb, idx, shape, bounded=False, pad=0):
+    H = shape["heads"] * 128
+    o = torch.full((shape["batch"] * shape["Lq"] + 3, H + pad), 0x2A2A, dtype=torch.int16, device="cuda")
+    binding.attention_sparse_bf16(dev(torch, qb), dev(torch, kb), dev(torch, vb), o, dev(torch, idx),
+                                  flags=binding.ATTN_BOUNDED_LOGITS if bounded else 0, **on_device(torch, shape))
+    raw = o.cpu().numpy()
+    rows = shape["batch"] * shape["Lq"]
+    assert (raw[rows:] == 0x2A2A).all() and (raw[:, H:] == 0x2A2A).all(), "rows or columns past the output changed"
+    return host_bf16(o)[:rows, :H]
+
+
+def check_attention(got, q, k, v, idx, shape):
+    y, tol = ref.attend(q, k, v, idx, **shape)
+    tol = tol + BF16 * (np.abs(y) + tol) + 1e-30
+    worst = np.max(np.abs(got - y) / tol, initial=0)
+    assert worst <= 1, f"{worst} of the tolerance"
+    return y
+
+
+ATTEND = [
+    shape_of(1, 1, 1, 1), shape_of(1, 4097, 3, 40), shape_of(1, 9000, 2, 140, batch=2, klen=[9000, 130]),
+    shape_of(5, 63, 2, 1), shape_of(33, 64, 1, 2), shape_of(128, 65, 2, 2), shape_of(129, 1000, 2, 7),
+    shape_of(300, 3000, 6, 11, kv_heads=2), shape_of(257, 517, 4, 9, kv_heads=1, batch=3, klen=[517, 0, 1]),
+    shape_of(1000, 2000, 8, 5, batch=2), shape_of(9000, 1500, 8, 6)]
+
+
+@pytest.mark.parametrize("bounded", [False, True])
+@pytest.mark.parametrize("shape", ATTEND)
+def test_sparse_attention(shape, bounded):
+    """Random lists with holes (-1 and blocks that do not exist), unordered, one block twice; keys past a
+    sequence's end hold NaN."""
+    torch = torch_cuda()
+    r = rng(shape["Lq"], shape["Lk"], shape["heads"])
+    G = shape["kv_heads"] or shape["heads"]
+    pad = 8 * (shape["Lq"] % 3)
+    qb, q = tokens(r, shape["batch"] * shape["Lq"], shape["heads"], pad)
+    kb, k = tokens(r, shape["batch"] * shape["Lk"], G, pad)
+    vb, v = tokens(r, shape["batch"] * shape["Lk"], G, pad, scale=2.0)
+    if shape["klen"]:
+        for z, n in enumerate(shape["klen"]):
+            kb[z * shape["Lk"] + n:(z + 1) * shape["Lk"], :] = 0x7FC0
+            vb[z * shape["Lk"] + n:(z + 1) * shape["Lk"], :] = 0x7F80
+    nqb, nkb = -(-shape["Lq"] // 128), -(-shape["Lk"] // 64)
+    idx = r.integers(0, nkb, (shape["batch"], shape["heads"], nqb, shape["topk"])).astype(np.int32)
+    idx[r.random(idx.shape) < 0.1] = -1
+    idx[r.random(idx.shape) < 0.05] = nkb + 3
+    idx[r.random(idx.shape) < 0.02] = -2 ** 31
+    if shape["topk"] > 1:
+        idx[..., -1] = idx[..., 0]
+        idx[0, 0, 0] = -1                           # a block of queries without keys
+    got = run_attention(torch, qb, kb, vb, idx, shape, bounded, pad)
+    y = check_attention(got, q, k, v, idx, shape)
+    if shape["topk"] > 1:
+        assert (got[:min(128, shape["Lq"]), :128] == 0).all() and (y[:min(128, shape["Lq"]), :128] == 0).all()
+
+
+@pytest.mark.parametrize("Lq", [1, 200])
+def test_sparse_attention_rising_logits(Lq):
+    """Logits that grow along the list by more than f32's exponent range in all: the running maximum moves at
+    every tile and old parts vanish; and logits far below zero, whose plain exponentials would."""
+    torch = torch_cuda()
+    r = rng(Lq, 8)
+    shape = shape_of(Lq, 64 * 12, 1, 12)
+    for sign in (1, -1):
+        k = np.repeat(np.arange(12), 64)[:, None] * np.ones(128) * 2 + r.standard_normal((64 * 12, 128)) * 0.1
+        q = sign * (1 + 0.1 * r.standard_normal((Lq, 128)))
+        v = r.standard_normal((64 * 12, 128))
+        (qb, kb, vb) = (bf16_bits(t) for t in (q, k, v))
+        idx = np.broadcast_to(np.arange(12, dtype=np.int32), (1, 1, -(-Lq // 128), 12)).copy()
+        got = run_attention(torch, qb, kb, vb, idx, shape)
+        check_attention(got, *(bits_to_f64(t) for t in (qb, kb, vb)), idx, shape)
+
+
+def test_sparse_attention_overflowing_logits():
+    """A key whose logit overflows to -inf weighs nothing; one listed alone leaves zeros."""
+    torch = torch_cuda()
+    shape = shape_of(64, 128, 1, 2)
+    q = np.full((64, 128), 2.0 ** 100)
+    k = np.zeros((128, 128))
+    k[:64] = -2.0 ** 100
+    v = rng(6).standard_normal((128, 128))
+    qb, kb, vb = (bf16_bits(t) for t in (q, k, v))
+    idx = np.array([[[[0, 1]]]], np.int32)
+    got = run_attention(torch, qb, kb, vb, idx, shape)
+    want = bits_to_f64(vb)[64:].mean(0)
+    assert np.abs(got - want).max() <= 2.0 ** -7 * np.abs(bits_to_f64(vb)).max()
+    idx[...] = 0
+    assert (run_attention(torch, qb, kb, vb, idx, shape) == 0).all()
+
+
+def test_sparse_attention_over_every_block_is_the_dense_one():
+    torch = torch_cuda()
+    Lq, Lk, heads = 700, 1500, 3
+    shape = shape_of(Lq, Lk, heads, 24)
+    r = rng(12)
+    qb, q = tokens(r, Lq, heads)
+    kb, k = tokens(r, Lk, heads)
+    vb, v = tokens(r, Lk, heads)
+    idx = run_select(torch, qb, kb, shape, 0)
+    assert (idx == np.arange(24)).all()
+    got = run_attention(torch, qb, kb, vb, idx, shape)
+    check_attention(got, q, k, v, idx, shape)
+    o = torch.empty((Lq, heads * 128), dtype=torch.int16, device="cuda")
+    ws = torch.empty(heads * 128 * 1536, dtype=torch.int16, device="cuda")
+    binding.attention_bf16(dev(torch, qb), dev(torch, kb), dev(torch, vb), o, Lq=Lq, Lk=Lk, heads=heads,
+                           ldq=heads * 128, ldk=heads * 128, ldv=heads * 128, ldo=heads * 128, vt_ws=ws)
+    # the two round their probabilities to bf16 around different maxima: twice one side's bound
+    y, tol = ref.attend(q, k, v, idx, **shape)
+    assert (np.abs(got - host_bf16(o)) <= 2 * (tol + BF16 * (np.abs(y) + tol))).all()
+
+
+# ---------------------------------------------------------------- together
+
+class Block:
+    """Attention half and MLP of one block on 8-bit products and chosen key blocks, its buffers and workspaces."""
+
+    def __init__(self, torch, seed, L=700, heads=2, F=512, topk=4):
+        r = rng(seed, 21)
+        H = self.H = heads * 128
+        self.t, self.L, self.heads, self.F, self.topk = torch, L, heads, F, topk
+        self.w = {}
+        for name, n, k in (("qkv", 3 * H, H), ("o", H, H), ("up", F, H), ("down", H, F)):
+            self.w[name] = self.rows(r.standard_normal((n, k)) / np.sqrt(k))
+        self.gate = dev(torch, r.standard_normal(H).astype(np.float32))
+        self.x0 = dev(torch, bf16_bits(r.standard_normal((L, H))))
+        e = lambda *s, dt=torch.int16: torch.empty(*s, dtype=dt, device="cuda")  # noqa: E731
+        self.x, self.qkv, self.att = e(L, H), e(L, 3 * H), e(L, H)
+        self.q8 = [e(L, n, dt=torch.uint8) for n in (H, H, H, F)]
+        self.s8 = [e(L, binding.fp8_scale_ld(n), dt=torch.uint8) for n in (H, H, H, F)]
+        self.idx = e(1, heads, -(-L // 128), topk, dt=torch.int32)
+        self.shape = dict(Lq=L, Lk=L, heads=heads, topk=topk)
+        self.ws = [e(max(16, f(**self.shape)), dt=torch.uint8)
+                   for f in (binding.select_blocks_ws_bytes, binding.attention_sparse_ws_bytes)]
+
+    def rows(self, x):
+        q, s = ref.quantise(x)
+        return dev(self.t, q), dev(self.t, padded_scale(s, x.shape[1])), ref.values(q, s)
+
+    def linear(self, i, name, out, N, K, **kw):
+        w = self.w[name]
+        binding.gemm_fp8(self.q8[i], self.s8[i], w[0], w[1], None, out, M=self.L, N=N, K=K, stream=self.stream, **kw)
+
+    def quant(self, i, x, K):
+        binding.quant_fp8(x, self.q8[i], self.s8[i], M=self.L, K=K, stream=self.stream)
+
+    def run(self, stream=None):
+        self.stream, H, F, L = stream, self.H, self.F, self.L
+        self.x.copy_(self.x0)
+        self.quant(0, self.x, H)
+        self.linear(0, "qkv", self.qkv, 3 * H, H, rms_cols=2 * H)
+        q, k, v = (self.qkv[:, i * H:(i + 1) * H] for i in range(3))
+        binding.select_blocks_bf16(q, k, self.idx, first=1, ws=self.ws[0], stream=stream, **self.shape)
+        binding.attention_sparse_bf16(q, k, v, self.att, self.idx, ws=self.ws[1], stream=stream,
+                                      flags=binding.ATTN_BOUNDED_LOGITS, **self.shape)
+        self.quant(1, self.att, H)
+        self.linear(1, "o", self.x, H, H, flags=binding.EPI_GATED_RES, gate=self.gate)
+        self.quant(2, self.x, H)
+        self.linear(2, "up", self.q8[3], F, H, flags=binding.EPI_FP8, c_scale=self.s8[3], gelu_from=0)
+        self.linear(3, "down", self.x, H, F, flags=binding.EPI_GATED_RES, gate=self.gate)
+        return self.x
+
+    def host8(self, i):
+        q, s = self.q8[i].cpu().numpy(), self.s8[i].cpu().numpy()
+        return ref.values(q, s[:, :-(-q.shape[1] // 128)])
+
+
+def test_a_block_on_all_four_operators():
+    """Each stage against float64 on the device's own input of that stage, so that every tolerance is one stage's."""
+    torch = torch_cuda()
+    b = Block(torch, 1)
+    H, L = b.H, b.L
+    out = host_bf16(b.run())
+    x0 = host_bf16(b.x0)
+    rq, rs = ref.quantise(x0)
+    np.testing.assert_array_equal(b.host8(0), ref.values(rq, rs))
+    y, d = ref.product(b.host8(0), b.w["qkv"][2], None, f32=False, rms_cols=2 * H)
+    qkv = host_bf16(b.qkv)
+    assert (np.abs(qkv - y) <= d + BF16 * (np.abs(y) + d) + 1e-30).all()
+    q, k, v = (qkv[:, i * H:(i + 1) * H] for i in range(3))
+    idx = b.idx.cpu().numpy()
+    np.testing.assert_array_equal(idx, ref.select(q, k, first=1, **b.shape))
+    check_attention(host_bf16(b.att), q, k, v, idx, b.shape)
+    rq, rs = ref.quantise(host_bf16(b.att))
+    np.testing.assert_array_equal(b.host8(1), ref.values(rq, rs))
+    gate = b.gate.cpu().numpy().astype(np.float64)
+    y, d = ref.product(b.host8(1), b.w["o"][2], None, f32=False)
+    mid, dm = x0 + gate * y, np.abs(gate) * d + 2.0 ** -22 * (np.abs(x0) + np.abs(gate * y))
+    dm = dm + BF16 * (np.abs(mid) + dm)
+    # the 8-bit rows of the middle residual lie within its error and their own half step
+    m8 = b.host8(2)
+    s = np.repeat(2.0 ** (b.s8[2].cpu().numpy()[:, :H // 128].astype(np.float64) - 127), 128, 1)
+    assert (np.abs(m8 - mid) <= dm + np.maximum(2.0 ** -4 * (np.abs(mid) + dm), 2.0 ** -10 * s)).all()
+    y, d = ref.product(m8, b.w["up"][2], None, f32=False, gelu_from=0)
+    u8 = b.host8(3)
+    s = np.repeat(2.0 ** (b.s8[3].cpu().numpy()[:, :b.F // 128].astype(np.float64) - 127), 128, 1)
+    assert (np.abs(u8 - y) <= d + np.maximum(2.0 ** -4 * (np.abs(y) + d), 2.0 ** -10 * s)).all()
+    y, d = ref.product(u8, b.w["down"][2], None, f32=False)
+    fin = mid + gate * y
+    tol = dm + np.abs(gate) * d + 2.0 ** -22 * (np.abs(mid) + np.abs(gate * y))
+    assert (np.abs(out - fin) <= tol + BF16 * (np.abs(fin) + tol)).all()
+
+
+def test_blocks_captured_into_two_graphs():
+    """Two blocks captured into graphs with their own workspaces, replayed in turn with eager work between: every
+    replay gives the eager bits."""
+    torch = torch_cuda()
+    blocks = [Block(torch, s) for s in (2, 3)]
+    want = [b.run().clone() for b in blocks]
+    other = Block(torch, 4)
+    stream = torch.cuda.Stream()
+    graphs = []
+    torch.cuda.synchronize()
+    for b in blocks:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            b.run(stream)
+        graphs.append(g)
+    for i in range(4):
+        for b, g, w in zip(blocks, graphs, want):
+            b.x.zero_()
+            b.idx.fill_(-1)
+            g.replay()
+            other.run()
+            torch.cuda.synchronize()
+            assert torch.equal(b.x, w), i
+
+
+def test_blocks_on_two_streams():
+    torch = torch_cuda()
+    blocks = [Block(torch, s, L=1500) for s in (5, 6)]
+    want = [b.run().clone() for b in blocks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for b, s in zip(blocks, streams):
+        for _ in range(6):
+            with torch.cuda.stream(s):
+                b.run(s)
+    torch.cuda.synchronize()
+    for b, w in zip(blocks, want):
+        assert torch.equal(b.x, w)
+
+
+def test_workspaces_of_the_caching_allocator():
+    """Without a workspace argument the binding takes one on the call's stream; results are those of a kept one."""
+    torch = torch_cuda()
+    r = rng(31)
+    shape = shape_of(1, 5000, 3, 30)
+    qb, _ = tokens(r, 1, 3)
+    kb, _ = tokens(r, 5000, 3)
+    q, k = dev(torch, qb), dev(torch, kb)
+    torch.cuda.synchronize()
+    outs = []
+    for stream in (None, torch.cuda.Stream()):
+        for _ in range(3):
+            idx = torch.empty(1, 3, 1, 30, dtype=torch.int32, device="cuda")
+            o = torch.empty(1, 384, dtype=torch.int16, device="cuda")
+            torch.cuda.synchronize()
+            binding.select_blocks_bf16(q, k, idx, stream=stream, **shape)
+            binding.attention_sparse_bf16(q, k, k, o, idx, stream=stream, **shape)
+            torch.cuda.synchronize()
+            outs.append((idx, o))
+    for idx, o in outs:
+        assert torch.equal(idx, outs[0][0]) and torch.equal(o, outs[0][1])

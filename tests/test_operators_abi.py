@@ -1,0 +1,176 @@
+"""Refusals and sizes of the 8-bit and sparse entry points: no GPU needed,
+nothing is launched."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from paper_2608_09231_amd import binding
+from tests import _operators as ref
+
+FAKE = 0x1000
+
+
+def gemm_desc(**kw):
+    d = dict(A=FAKE, lda=256, a_scale=FAKE, ld_as=4, W=FAKE, ldw=256, w_scale=FAKE, ld_ws=4, bias=None, C=FAKE,
+             ldc=512, c_scale=None, ld_cs=0, gate=None, M=64, N=512, K=256, flags=0, rms_cols=0, gelu_from=512,
+             gap_at=0, gap=0)
+    d.update(kw)
+    return binding.GemmFp8DescC(**d)
+
+
+@pytest.mark.parametrize("kw", [
+    {"K": 0}, {"K": 250}, {"K": -16}, {"M": -1}, {"N": -8}, {"N": 500}, {"lda": 128}, {"ldw": 240}, {"lda": 264},
+    {"ldw": 1 << 23}, {"ld_as": 0}, {"ld_ws": 6}, {"K": 528, "lda": 528, "ldw": 528}, {"ldc": 504}, {"ldc": 516},
+    {"gap": -4}, {"gap": 6, "gap_at": 8, "ldc": 600}, {"gap": 8, "gap_at": 6, "ldc": 600}, {"gap": 128, "gap_at": 256},
+    {"gap": 8, "gap_at": -4, "ldc": 600}, {"gelu_from": 6}, {"gelu_from": -4}, {"rms_cols": 100}, {"rms_cols": 640},
+    {"rms_cols": -128}, {"rms_cols": 128, "N": 200},
+    {"flags": 8, "c_scale": FAKE, "ld_cs": 4, "N": 200}, {"flags": 8, "c_scale": FAKE, "ld_cs": 0},
+    {"flags": 8, "c_scale": FAKE, "ld_cs": 4, "gelu_from": 64}, {"flags": 8, "c_scale": FAKE, "ld_cs": 4, "ldc": 520},
+    {"flags": 8, "c_scale": FAKE, "ld_cs": 4, "gap": 128, "gap_at": 128, "ldc": 640}])
+def test_gemm_fp8_refuses_shapes(kw):
+    lib = binding.load()
+    d = gemm_desc(**kw)
+    assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_ESHAPE, kw
+    assert lib.dit_cache_last_error(None)
+
+
+@pytest.mark.parametrize("kw", [
+    {"A": None}, {"W": None}, {"a_scale": None}, {"w_scale": None}, {"C": None}, {"flags": 16}, {"flags": 2},
+    {"flags": 8}, {"flags": 3, "gate": FAKE}, {"flags": 9, "c_scale": FAKE}, {"A": FAKE + 8}, {"C": FAKE + 8},
+    {"a_scale": FAKE + 2}, {"bias": FAKE + 1}, {"flags": 2, "gate": FAKE + 4},
+    {"flags": 8, "c_scale": FAKE + 1, "ld_cs": 4}])
+def test_gemm_fp8_refuses_pointers_and_flags(kw):
+    lib = binding.load()
+    d = gemm_desc(**kw)
+    assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_EINVAL, kw
+    assert lib.dit_gemm_fp8(None, None) == binding.DIT_EINVAL
+
+
+def test_quant_fp8_refuses():
+    lib = binding.load()
+    good = dict(x=FAKE, t=1, ldx=256, q=FAKE, ldq=256, s=FAKE, lds=4, M=4, K=256)
+    for st, kw in ((binding.DIT_EINVAL, {"x": None}), (binding.DIT_EINVAL, {"q": None}), (binding.DIT_EINVAL, {"s": None}),
+                   (binding.DIT_EINVAL, {"t": 2}), (binding.DIT_EINVAL, {"x": FAKE + 8}),
+                   (binding.DIT_EINVAL, {"q": FAKE + 4}), (binding.DIT_EINVAL, {"s": FAKE + 1}),
+                   (binding.DIT_ESHAPE, {"K": 24}), (binding.DIT_ESHAPE, {"K": -16}), (binding.DIT_ESHAPE, {"M": -1}),
+                   (binding.DIT_ESHAPE, {"ldx": 255}), (binding.DIT_ESHAPE, {"ldx": 260}), (binding.DIT_ESHAPE, {"ldq": 264}),
+                   (binding.DIT_ESHAPE, {"ldq": 240}), (binding.DIT_ESHAPE, {"lds": 5}), (binding.DIT_ESHAPE, {"lds": 0}),
+                   (binding.DIT_ESHAPE, {"K": 528, "ldx": 528, "ldq": 528})):
+        a = dict(good, **kw)
+        assert lib.dit_quant_fp8(a["x"], a["t"], a["ldx"], a["q"], a["ldq"], a["s"], a["lds"], a["M"], a["K"],
+                                 None) == st, kw
+
+
+SHAPE = dict(Lq=300, Lk=1000, heads=4, kv_heads=2, topk=5, batch=2)
+
+
+@pytest.mark.parametrize("st,shape,kw", [
+    (binding.DIT_ESHAPE, {"batch": -1}, {}), (binding.DIT_ESHAPE, {"Lq": -1}, {}), (binding.DIT_ESHAPE, {"Lk": -1}, {}),
+    (binding.DIT_ESHAPE, {"heads": 0}, {}), (binding.DIT_ESHAPE, {"kv_heads": 3}, {}),
+    (binding.DIT_ESHAPE, {"kv_heads": 0}, {}), (binding.DIT_ESHAPE, {"topk": 0}, {}),
+    (binding.DIT_ESHAPE, {"batch": 2 ** 30, "heads": 2 ** 20}, {}),
+    (binding.DIT_EINVAL, {}, {"q": None}), (binding.DIT_EINVAL, {}, {"k": None}), (binding.DIT_EINVAL, {}, {"idx": None}),
+    (binding.DIT_EINVAL, {}, {"q": FAKE + 8}), (binding.DIT_EINVAL, {}, {"idx": FAKE + 2}),
+    (binding.DIT_ESHAPE, {}, {"ldq": 504}), (binding.DIT_ESHAPE, {}, {"ldq": 516}), (binding.DIT_ESHAPE, {}, {"ldk": 128})])
+def test_sparse_calls_refuse(st, shape, kw):
+    lib = binding.load()
+    s = binding.sparse_shape(**dict(SHAPE, **shape))
+    a = dict(q=FAKE, ldq=512, k=FAKE, ldk=256, idx=FAKE)
+    a.update(kw)
+    assert lib.dit_select_blocks_bf16(C.byref(s), a["q"], a["ldq"], a["k"], a["ldk"], 0, a["idx"], FAKE, None) == st
+    assert lib.dit_attention_sparse_bf16(C.byref(s), a["q"], a["ldq"], a["k"], a["ldk"], FAKE, 256, FAKE, 512, a["idx"], 0,
+                                         FAKE, None) == st
+    if shape:
+        assert lib.dit_select_blocks_ws_bytes(C.byref(s)) == 0 and lib.dit_attention_sparse_ws_bytes(C.byref(s)) == 0
+
+
+def test_sparse_calls_refuse_their_own():
+    lib = binding.load()
+    s = binding.sparse_shape(**SHAPE)
+
+    def select(s=s, first=0, ws=FAKE):
+        return lib.dit_select_blocks_bf16(C.byref(s), FAKE, 512, FAKE, 256, first, FAKE, ws, None)
+
+    def attend(s=s, v=FAKE, ldv=256, o=FAKE, ldo=512, flags=0, ws=FAKE, ldk=256):
+        return lib.dit_attention_sparse_bf16(C.byref(s), FAKE, 512, FAKE, ldk, v, ldv, o, ldo, FAKE, flags, ws, None)
+
+    assert select(first=-1) == select(first=6) == select(ws=None) == select(ws=FAKE + 8) == binding.DIT_EINVAL
+    big = binding.sparse_shape(**dict(SHAPE, Lk=16384 * 64 + 1))
+    assert select(s=big) == binding.DIT_ESHAPE
+    many = binding.sparse_shape(**dict(SHAPE, batch=20000))
+    assert select(s=many) == binding.DIT_ESHAPE
+    assert lib.dit_attention_sparse_ws_bytes(C.byref(s)) > 0
+    assert attend(v=None) == attend(o=None) == attend(flags=2) == attend(ws=None) == attend(ws=FAKE + 4) == \
+        binding.DIT_EINVAL
+    assert attend(ldv=128) == attend(ldo=256) == attend(ldk=1 << 22) == binding.DIT_ESHAPE
+    assert lib.dit_select_blocks_bf16(None, FAKE, 512, FAKE, 256, 0, FAKE, FAKE, None) == binding.DIT_EINVAL
+    assert lib.dit_attention_sparse_bf16(None, FAKE, 512, FAKE, 256, FAKE, 256, FAKE, 512, FAKE, 0, FAKE,
+                                         None) == binding.DIT_EINVAL
+    assert lib.dit_attention_sparse_ws_bytes(None) == 0
+
+
+def test_select_workspace_holds_means_and_keys():
+    assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * (2 * 4 * 3 * 128 + 2 * 2 * 16 * 128 + 2 * 4 * 3 * 16)
+
+
+def test_sparse_workspace_is_for_few_lists_only():
+    assert binding.attention_sparse_ws_bytes(Lq=32760, Lk=32760, heads=40, topk=52) == 0
+    assert binding.attention_sparse_ws_bytes(Lq=1, Lk=32760, heads=40, topk=1) == 0
+
+
+def test_binding_refuses_host_tensors():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(4, 128)
+    b = torch.zeros(4, 128, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding.quant_fp8(x, b, b, M=4, K=128)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding.gemm_fp8(b, b, b, b, None, x, M=4, N=4, K=128)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding.select_blocks_bf16(x, x, b, Lq=4, Lk=4, heads=1, topk=1)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding.attention_sparse_bf16(x, x, x, x, b, Lq=4, Lk=4, heads=1, topk=1)
+
+
+class _Device:
+    """Stands in for a device tensor of one dimension or two."""
+
+    def __init__(self, t, device="cuda:0"):
+        self._t, self.is_cuda, self.device = t, True, device
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+
+def test_binding_checks_sizes_and_devices():
+    torch = pytest.importorskip("torch")
+    x = _Device(torch.zeros(4, 128, dtype=torch.bfloat16))
+    q = _Device(torch.zeros(4, 128, dtype=torch.uint8))
+    s = _Device(torch.zeros(4, 4, dtype=torch.uint8))
+    for kw, match in ((dict(M=5, K=128), "must hold"), (dict(M=4, K=256), "must hold"), (dict(M=4, K=128, ldx=200), "must hold"),
+                      (dict(M=4, K=128, ldq=130), "must hold")):
+        with pytest.raises(ValueError, match=match):
+            binding.quant_fp8(x, q, s, **kw)
+    with pytest.raises(ValueError, match="elements of"):
+        binding.quant_fp8(x, x, s, M=4, K=128)
+    with pytest.raises(ValueError, match="contiguous rows"):
+        binding.quant_fp8(_Device(torch.zeros(128, 128, dtype=torch.bfloat16).t()[:4]), q, s, M=4, K=128)
+    with pytest.raises(ValueError, match="one device"):
+        binding.quant_fp8(x, _Device(q._t, "cuda:1"), s, M=4, K=128)
+    with pytest.raises(ValueError, match="another device"):
+        binding.quant_fp8(x, q, s, M=4, K=128, stream=type("S", (), {"device": "cuda:1"})())
+
+
+def test_oracle_rounds_to_nearest_even():
+    """The oracle's quantiser against torch's conversion, which rounds to nearest even."""
+    torch = pytest.importorskip("torch")
+    x = np.random.default_rng(3).standard_normal((40, 128)) * 100
+    x[:, 0] = 448.0                                  # scale 1
+    x = np.clip(x, -448, 448)
+    x[1, 1:120] = (ref.TABLE[1:120] + ref.TABLE[2:121]) / 2          # ties
+    q, s = ref.quantise(x)
+    assert (s == 127).all()
+    t = torch.from_numpy(x).float().to(torch.float8_e4m3fn).double().numpy()
+    ok = x == x.astype(np.float32)
+    np.testing.assert_array_equal(ref.values(q, s)[ok], t[ok])
