@@ -123,6 +123,20 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
 
+// Largest of v over the 8 or 16 neighbouring lanes of a lane, on the VALU (data
+// parallel primitives: pairs, quads, halves of 8, 16).
+template <int LANES>
+__device__ __forceinline__ uint32_t max_over(uint32_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  static_assert(LANES == 8 || LANES == 16, "lanes");
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));   // lane ^ 1
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));   // lane ^ 2
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));  // 7 - lane, of 8
+  if (LANES == 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));  // 15 - lane
+#endif
+  return v;
+}
+
 // ---- 8-bit floating point (e4m3) with power-of-two scales (E8M0 bytes) ----
 
 // Scale byte of values whose largest magnitude has the bits `top` (compared as

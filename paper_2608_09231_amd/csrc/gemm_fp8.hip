@@ -80,8 +80,7 @@ __global__ __launch_bounds__(256) void quant_fp8_kernel(const T* __restrict__ x,
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  top = max_over<8>(top);
   const uint32_t byte = e8m0_of(top);
   const float inv = e8m0_inverse(byte);
   if (!in) return;
@@ -108,17 +107,35 @@ __device__ __forceinline__ void copy16_oob(const void* base, lds_void_t* dst, ui
 // The 128 x 128-deep step of one 16 x 16 block.  A lane holds row lr's 16-byte
 // chunks lq and lq + 4 of the block of 128 (the sum over k does not mind their
 // order, and these are the chunks that a swizzled LDS row serves without bank
-// conflicts).  sa and sw: scale bytes of the lane's rows in bits 0..7.
+// conflicts).  sa and sw: scale bytes of the lane's rows for four blocks of K; B: which.
+template <int B = 0>
 __device__ __forceinline__ f32x4_t mfma_scaled(const i32x8_t& a, const i32x8_t& w, const f32x4_t& c, int sa, int sw) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w, c, 0, 0, 0, sa, 0, sw);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w, c, 0, 0, B, sa, B, sw);
 #else
   return c;
 #endif
 }
 
-__device__ __forceinline__ i32x8_t frag8(const uint4& lo, const uint4& hi) {
-  return i32x8_t{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+// The same of a 32 x 32 block and 64 of K: lane (lr, lh) holds 32 of row lr.
+template <int B>
+__device__ __forceinline__ f32x16_t mfma_scaled32(const i32x8_t& a, const i32x8_t& w, const f32x16_t& c, int sa, int sw) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, w, c, 0, 0, B, sa, B, sw);
+#else
+  return c;
+#endif
+}
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x8_t frag8(i32x4_t lo, i32x4_t hi) {
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Both chunks of a fragment from LDS.  (Loads of a vector type keep their type
+// information; without it the compiler has every one of them wait for all copies
+// to LDS in flight.)
+__device__ __forceinline__ i32x8_t lds_frag(const char* lo, const char* hi) {
+  return frag8(*(const i32x4_t*)lo, *(const i32x4_t*)hi);
 }
 
 // The fragment widened to bf16, times its row's scale: four 32-deep operands.
@@ -153,18 +170,17 @@ __device__ __forceinline__ void tile_at(const Fp8Prob& P, int lt, int& tm, int& 
 
 // 256 x 256 tiles, 8 waves of 64 x 128, the whole 160 KB of LDS as three W and
 // two A slices of 128 of K (32 KB each, 16-byte chunks of a 128-byte row
-// XOR-swizzled by ((row >> 1) & 7)).
+// XOR-swizzled by ((row >> 1) & 7)).  32x32x64 MFMAs: a slice is two substeps of
+// eight, and a substep's six fragments are read under the MFMAs of the one
+// before it, evenly.
 //
-// A slice is one MFMA step: eight groups of four MFMAs, group j with W
-// fragment j and the wave's four A fragments.  W fragments are read two
-// groups ahead, each A fragment of the next slice right after its last MFMA.
-// The work-groups' waves meet before group 6, where the next slice's first
-// reads begin: by then every read of this slice is done, so its two units take
-// A slice kt + 2 and W slice kt + 3.  Slices past the last one are copied as
-// zeros (no memory traffic), which keeps every iteration and wait the same.
+// The waves meet after substep 0, whose reads were the last of their slice: its
+// units take A slice kt + 2 (in substep 1) and W slice kt + 3 (in the next
+// substep 0).  Slices past the last one are copied as zeros (no memory
+// traffic), which keeps every iteration and wait alike.
 template <int KIND>
 __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
-  constexpr int UNIT = 256 * 128, INS = 4, TM = 4, TN = 8;
+  constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4;
   __shared__ __attribute__((aligned(1024))) char smem[5 * UNIT];
   int tm, tn;
   tile_at(P, xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n), tm, tn);
@@ -174,27 +190,26 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const int lr = lane & 15, lq = lane >> 4;
+  const int lr = lane & 31, lh = lane >> 5;
 
   // copy j of this wave moves rows 8 (4 wave + j) .. + 7 of an operand's slice
   const uint8_t* Ab = P.A + (int64_t)m0 * P.lda;
   const uint8_t* Wb = P.W + (int64_t)n0 * P.ldw;
+  const int c0 = (lane & 7) ^ (lane >> 4);  // chunk of even copies; odd ones: c0 ^ 4
   uint32_t aoff[INS], woff[INS];
 #pragma unroll
   for (int j = 0; j < INS; ++j) {
     const int row = 8 * (wave * INS + j) + (lane >> 3);
-    const int c = (lane & 7) ^ ((row >> 1) & 7);
-    aoff[j] = (uint32_t)min(row, P.M - 1 - m0) * (uint32_t)P.lda + c * 16;
-    woff[j] = (uint32_t)min(row, P.N - 1 - n0) * (uint32_t)P.ldw + c * 16;
+    aoff[j] = (uint32_t)min(row, P.M - 1 - m0) * (uint32_t)P.lda + 16 * (c0 ^ (4 * (j & 1)));
+    woff[j] = (uint32_t)min(row, P.N - 1 - n0) * (uint32_t)P.ldw + 16 * (c0 ^ (4 * (j & 1)));
   }
+  auto issue1 = [&](const uint8_t* base, const uint32_t (&off)[INS], int u, int s, int j) {
+    copy16_oob(base, (lds_void_t*)(smem + u + (wave * INS + j) * 1024),
+               16 * (c0 ^ (4 * (j & 1))) < P.K - 128 * s ? off[j] : OOB, (uint32_t)s * 128);
+  };
   auto issue = [&](const uint8_t* base, const uint32_t (&off)[INS], int u, int s) {
-    char* d = smem + u;
-    const int left = P.K - 128 * s;
 #pragma unroll
-    for (int j = 0; j < INS; ++j) {
-      const int c = (lane & 7) ^ (((4 * j + (lane >> 4))) & 7);  // chunk of copy j (4 wave INS is a multiple of 8)
-      copy16_oob(base, (lds_void_t*)(d + (wave * INS + j) * 1024), 16 * c < left ? off[j] : OOB, (uint32_t)s * 128);
-    }
+    for (int j = 0; j < INS; ++j) issue1(base, off, u, s, j);
   };
   // scales of this wave's rows, four slices to a dword: lane l loads rows l (and
   // 64 + l of W), a lane permutation hands them to the lanes that multiply
@@ -211,22 +226,37 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
   int sa[TM], sw[TN];
   auto spread_scales = [&]() {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = __builtin_amdgcn_ds_bpermute(4 * (16 * i + lr), sna);
+    for (int i = 0; i < TM; ++i) sa[i] = __builtin_amdgcn_ds_bpermute(4 * lr + 128 * i, sna);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) sw[j] = __builtin_amdgcn_ds_bpermute(4 * (16 * (j & 3) + lr), j < 4 ? snw0 : snw1);
+    for (int j = 0; j < TN; ++j) sw[j] = __builtin_amdgcn_ds_bpermute(4 * lr + 128 * (j & 1), j < 2 ? snw0 : snw1);
   };
 
-  int loff[2];  // this lane's two chunks inside 16 rows of a unit
+  // this lane's chunks inside 32 rows of a unit: half lh of substep s, 32 of its 64 k
+  int loff[2][2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) loff[h] = lr * 128 + (((4 * h + lq) ^ ((lr >> 1) & 7)) << 4);
-  auto rd = [&](int at) {
-    return frag8(*(const uint4*)(smem + at + loff[0]), *(const uint4*)(smem + at + loff[1]));
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) loff[s][h] = lr * 128 + (((4 * s + 2 * h + lh) ^ ((lr >> 1) & 7)) << 4);
+  const int wa = wm * 64 * 128, ww = wn * 128 * 128;
+  auto rd = [&](int at, int s) { return lds_frag(smem + at + loff[s][0], smem + at + loff[s][1]); };
+  f32x16_t acc[TM][TN] = {};
+  // A substep's MFMAs, and between them one by one the fragment reads of the next
+  // substep (s of the slice in units uw, ua) in the order of their use and four
+  // copies.  The fences keep that order.
+  auto substep = [&](const i32x8_t(&a)[TM], const i32x8_t(&w)[TN], i32x8_t(&an)[TM], i32x8_t(&wn2)[TN], int uw, int ua,
+                     int s, auto b_, auto copy) {
+    constexpr int B = decltype(b_)::value;
+#pragma unroll
+    for (int q = 0; q < TM * TN; ++q) {
+      const int i = q & 1, j = q >> 1;
+      acc[i][j] = mfma_scaled32<B>(a[i], w[j], acc[i][j], sa[i], sw[j]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (q == 0 || q == 2) an[q >> 1] = rd(ua + wa + (q >> 1) * 4096, s);
+      else if (q < 6) wn2[q == 1 ? 0 : q - 2] = rd(uw + ww + (q == 1 ? 0 : q - 2) * 4096, s);
+      if (q & 1) copy(q >> 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
-  f32x4_t acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   // W slice kt in unit kt % 3, A slice kt in unit 3 + kt % 2
   int wu = 0, au = 3 * UNIT;
@@ -236,75 +266,65 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
   issue(Ab, aoff, 3 * UNIT, 0);
   issue(Wb, woff, UNIT, 1);
   issue(Ab, aoff, 4 * UNIT, 1);
-  issue(Wb, woff, 2 * UNIT, 2);
-  wait_vmcnt<3 * INS>();  // scales and slice 0 have landed
+  wait_vmcnt<2 * INS>();  // scales and slice 0 have landed
   barrier_no_fence();
-  i32x8_t a[TM], w[4];
-  const int wa = wm * 64 * 128, ww = wn * 128 * 128;
+  i32x8_t a0[TM], w0[TN], a1[TM], w1[TN];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) a[i] = rd(au + wa + i * 2048);
-  w[0] = rd(wu + ww);
-  w[1] = rd(wu + ww + 2048);
-  for (int kt = 0; kt < nk; ++kt) {
-    if ((kt & 3) == 0) {
-      spread_scales();
-    } else {
+  for (int i = 0; i < TM; ++i) a0[i] = rd(au + wa + i * 4096, 0);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = (int)((uint32_t)sa[i] >> 8);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sw[j] = (int)((uint32_t)sw[j] >> 8);
-    }
+  for (int j = 0; j < TN; ++j) w0[j] = rd(wu + ww + j * 4096, 0);
+  spread_scales();
+  // Slice kt, block B = kt % 4 of a dword of scales.
+  auto slice = [&](int kt, auto b_) {
+    constexpr int B = decltype(b_)::value;
     const int wn_ = next_w(wu), an_ = 7 * UNIT - au;
-#pragma unroll
-    for (int j = 0; j < 6; ++j) {
-      w[(j + 2) & 3] = rd(wu + ww + (j + 2) * 2048);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) acc[i][j] = mfma_scaled(a[i], w[j & 3], acc[i][j], sa[i], sw[j]);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    if constexpr (B == 0) load_scales((kt >> 2) + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    substep(a0, w0, a1, w1, wu, au, 1, b_, [&](int j) { issue1(Wb, woff, next_w(wn_), kt + 2, j); });
     // this wave's reads of slice kt and its copies of slice kt + 1 are done (W
     // slice kt + 2 may stay in flight); then everyone's are
     wait_vmcnt_lgkm0<INS>();
     barrier_no_fence();
-    issue(Ab, aoff, au, kt + 2);
-    if ((kt & 3) == 0) load_scales((kt >> 2) + 1);
-    issue(Wb, woff, wu, kt + 3);
-    __builtin_amdgcn_sched_barrier(0);
-    w[0] = rd(wn_ + ww);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) acc[i][6] = mfma_scaled(a[i], w[2], acc[i][6], sa[i], sw[6]);
-    __builtin_amdgcn_sched_barrier(0);
-    w[1] = rd(wn_ + ww + 2048);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      acc[i][7] = mfma_scaled(a[i], w[3], acc[i][7], sa[i], sw[7]);
-      __builtin_amdgcn_sched_barrier(0);
-      a[i] = rd(an_ + wa + i * 2048);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    substep(a1, w1, a0, w0, wn_, an_, 0, b_, [&](int j) { issue1(Ab, aoff, au, kt + 2, j); });
+    if constexpr (B == 3) spread_scales();
     wu = wn_;
     au = an_;
+  };
+  using std::integral_constant;
+  int kt = 0;
+  for (; kt + 4 <= nk; kt += 4) {
+    slice(kt, integral_constant<int, 0>{});
+    slice(kt + 1, integral_constant<int, 1>{});
+    slice(kt + 2, integral_constant<int, 2>{});
+    slice(kt + 3, integral_constant<int, 3>{});
   }
+  if (kt < nk) slice(kt, integral_constant<int, 0>{});
+  if (kt + 1 < nk) slice(kt + 1, integral_constant<int, 1>{});
+  if (kt + 2 < nk) slice(kt + 2, integral_constant<int, 2>{});
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
-  EpiLds<KIND> epi(P, m0 + 64 * wm, n0 + 128 * wn, lane & 31, lane >> 5, (float*)smem + wave * (32 * 128));
+  EpiLds<KIND> epi(P, m0 + 64 * wm, n0 + 128 * wn, lr, lh, (float*)smem + wave * (32 * 128));
   epi.prep();
   uint2 old[2][8][2];
   if (epi.gated) { epi.load_old(0, old[0]); epi.load_old(1, old[1]); }
-  epi.slab_pass16(acc[0], acc[1], 0, old[0], lr, lq);
-  epi.slab_pass16(acc[2], acc[3], 1, old[1], lr, lq);
+  epi.slab_pass(acc[0], 0, old[0]);
+  epi.slab_pass(acc[1], 1, old[1]);
 }
 
-// BM x 128 tiles, four waves of BM / 2 x 64, two work-groups per CU, ST slices
-// of 128 of K in LDS.  For launches that 256 x 256 tiles would not fill, short
-// K, and (WIDE) f32 outputs.
-template <int BM, int ST, int KIND, bool WIDE>
-__global__ __launch_bounds__(256, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
-  constexpr int TM = BM / 32, TN = 4, NW = 4;
+// BM x 128 tiles, waves of 64 x 64 (BM = 64: 32 x 64), a ring of slices of 128 of K
+// in LDS: two work-groups of 64 x 128 (three slices) or 128 x 128 (two) per CU, or
+// one of 256 x 128 (three).  For launches that 256 x 256 tiles would not fill, and
+// (WIDE) f32 outputs.  What bounds it is the way of a slice from L2 to LDS, so
+// slices in flight count: the waves meet before every step kt; slice kt + 1 has
+// landed, and slice kt, whose fragments are all in registers, gives its place to
+// slice kt + ST.  The fragments of kt + 1 are read under the MFMAs of kt.
+template <int BM, int KIND, bool WIDE>
+__global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
+  constexpr int ST = BM == 128 ? 2 : 3;
+  constexpr int NW = BM == 256 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
+  constexpr int TM = WM / 16, TN = 4, NF = TM + TN;
   constexpr int SLICE = (BM + 128) * 128;
-  constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW;
+  constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW, INS = A_INS + W_INS;
   constexpr int EPI = BM * 128 * 4;
   __shared__ __attribute__((aligned(1024))) char smem[ST * SLICE > EPI ? ST * SLICE : EPI];
   int tm, tn;
@@ -319,103 +339,103 @@ __global__ __launch_bounds__(256, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
 
   const uint8_t* Ab = P.A + (int64_t)m0 * P.lda;
   const uint8_t* Wb = P.W + (int64_t)n0 * P.ldw;
-  uint32_t aoff[A_INS], woff[W_INS];
-  int ac[A_INS], wc[W_INS];
+  // copy j of this wave: rows 8 (A_INS wave + j) .. + 7 of A, then the like of W
+  uint32_t off[INS];
+  int ch[INS];
 #pragma unroll
-  for (int j = 0; j < A_INS; ++j) {
-    const int row = 8 * (wave * A_INS + j) + (lane >> 3);
-    ac[j] = 16 * ((lane & 7) ^ ((row >> 1) & 7));
-    aoff[j] = (uint32_t)min(row, P.M - 1 - m0) * (uint32_t)P.lda + ac[j];
+  for (int j = 0; j < INS; ++j) {
+    const int row = 8 * (j < A_INS ? wave * A_INS + j : wave * W_INS + j - A_INS) + (lane >> 3);
+    ch[j] = 16 * ((lane & 7) ^ ((row >> 1) & 7));
+    off[j] = (uint32_t)min(row, (j < A_INS ? P.M - 1 - m0 : P.N - 1 - n0)) * (uint32_t)(j < A_INS ? P.lda : P.ldw) + ch[j];
   }
-#pragma unroll
-  for (int j = 0; j < W_INS; ++j) {
-    const int row = 8 * (wave * W_INS + j) + (lane >> 3);
-    wc[j] = 16 * ((lane & 7) ^ ((row >> 1) & 7));
-    woff[j] = (uint32_t)min(row, P.N - 1 - n0) * (uint32_t)P.ldw + wc[j];
-  }
-  auto issue = [&](int s) {
-    char* d = smem + (s % ST) * SLICE;
-    const int left = P.K - 128 * s;
-#pragma unroll
-    for (int j = 0; j < A_INS; ++j)
-      copy16_oob(Ab, (lds_void_t*)(d + (wave * A_INS + j) * 1024), ac[j] < left ? aoff[j] : OOB, (uint32_t)s * 128);
-#pragma unroll
-    for (int j = 0; j < W_INS; ++j)
-      copy16_oob(Wb, (lds_void_t*)(d + BM * 128 + (wave * W_INS + j) * 1024), wc[j] < left ? woff[j] : OOB,
-                 (uint32_t)s * 128);
+  auto issue1 = [&](int u, int s, int j) {
+    const int at = j < A_INS ? (wave * A_INS + j) * 1024 : BM * 128 + (wave * W_INS + j - A_INS) * 1024;
+    copy16_oob(j < A_INS ? Ab : Wb, (lds_void_t*)(smem + u + at), ch[j] < P.K - 128 * s ? off[j] : OOB, (uint32_t)s * 128);
   };
-  const uint8_t *sap[TM], *swp[TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i) sap[i] = P.As + (int64_t)min(m0 + wm * (BM / 2) + 16 * i + lr, P.M - 1) * P.ldas;
-#pragma unroll
-  for (int j = 0; j < TN; ++j) swp[j] = P.Ws + (int64_t)min(n0 + 64 * wn + 16 * j + lr, P.N - 1) * P.ldws;
-  int sa[TM], sw[TN], sna[TM], snw[TN];
+  // scales of this wave's rows, four slices to a dword: lane l loads rows l, a lane
+  // permutation hands them to the lanes that multiply (A's fragments, then W's)
+  const uint8_t* sap = P.As + (int64_t)min(m0 + WM * wm + (lane & (WM - 1)), P.M - 1) * P.ldas;
+  const uint8_t* swp = P.Ws + (int64_t)min(n0 + 64 * wn + lane, P.N - 1) * P.ldws;
+  int sna, snw, sc[NF];
   auto load_scales = [&](int g) {
     const int at = 4 * min(g, (nk - 1) >> 2);
+    sna = *(const int*)(sap + at);
+    snw = *(const int*)(swp + at);
+  };
+  auto spread_scales = [&]() {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sna[i] = *(const int*)(sap[i] + at);
-#pragma unroll
-    for (int j = 0; j < TN; ++j) snw[j] = *(const int*)(swp[j] + at);
+    for (int f = 0; f < NF; ++f)
+      sc[f] = __builtin_amdgcn_ds_bpermute(4 * lr + 64 * (f < TM ? f : f - TM), f < TM ? sna : snw);
   };
   int loff[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) loff[h] = lr * 128 + (((4 * h + lq) ^ ((lr >> 1) & 7)) << 4);
+  auto rd = [&](int u, int f) {  // fragment f: A, then W
+    const int at = u + (f < TM ? wm * WM * 128 + f * 2048 : BM * 128 + wn * 64 * 128 + (f - TM) * 2048);
+    return lds_frag(smem + at + loff[0], smem + at + loff[1]);
+  };
   f32x4_t acc[TM][TN] = {};
 
   load_scales(0);
 #pragma unroll
-  for (int s = 0; s < ST - 1; ++s) issue(s);
-  for (int kt = 0; kt < nk; ++kt) {
-    // slice kt has landed and this wave's reads of slice kt - 1 are done; then everyone's
-    wait_vmcnt_lgkm0<(ST - 2) * (A_INS + W_INS)>();
+  for (int s = 0; s < ST; ++s)
+#pragma unroll
+    for (int j = 0; j < INS; ++j) issue1(s * SLICE, s, j);
+  wait_vmcnt<(ST - 1) * INS>();  // scales and slice 0 have landed
+  barrier_no_fence();
+  i32x8_t f0[NF], f1[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) f0[f] = rd(0, f);
+  spread_scales();
+  int u = 0;  // place of slice kt
+  auto step = [&](int kt, const i32x8_t(&f)[NF], i32x8_t(&fn)[NF], auto b_) {
+    constexpr int B = decltype(b_)::value;
+    const int un = u == (ST - 1) * SLICE ? 0 : u + SLICE;
+    // this wave's reads of slice kt and its copies of slice kt + 1 are done (those
+    // of the next ST - 2 may stay in flight); then everyone's are
+    wait_vmcnt_lgkm0<(ST - 2) * INS>();
     barrier_no_fence();
-    if ((kt & 3) == 0) {
+    if constexpr (B == 0) load_scales((kt >> 2) + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    [[maybe_unused]] bf16x8_t aw[WIDE ? TM : 1][4], wv[4];
+    if constexpr (WIDE)
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = sna[i];
+      for (int i = 0; i < TM; ++i) widen(f[i], sc[i] >> (8 * B), aw[i]);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) sw[j] = snw[j];
-      load_scales((kt >> 2) + 1);
-    } else {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = (int)((uint32_t)sa[i] >> 8);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sw[j] = (int)((uint32_t)sw[j] >> 8);
-    }
-    issue(kt + ST - 1);
-    const char* sA = smem + (kt % ST) * SLICE + wm * (BM / 2) * 128;
-    const char* sW = smem + (kt % ST) * SLICE + BM * 128 + wn * 64 * 128;
-    i32x8_t a[TM], w[TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-      a[i] = frag8(*(const uint4*)(sA + i * 2048 + loff[0]), *(const uint4*)(sA + i * 2048 + loff[1]));
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-      w[j] = frag8(*(const uint4*)(sW + j * 2048 + loff[0]), *(const uint4*)(sW + j * 2048 + loff[1]));
-    if constexpr (WIDE) {
-      bf16x8_t aw[TM][4];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) widen(a[i], sa[i], aw[i]);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        bf16x8_t wv[4];
-        widen(w[j], sw[j], wv);
+    for (int q = 0; q < TM * TN; ++q) {
+      const int i = q % TM, j = q / TM;
+      if constexpr (WIDE) {
+        if (i == 0) widen(f[TM + j], sc[TM + j] >> (8 * B), wv);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[i][t], wv[t], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[i][t], wv[t], acc[i][j], 0, 0, 0);
+      } else {
+        acc[i][j] = mfma_scaled<B>(f[i], f[TM + j], acc[i][j], sc[i], sc[TM + j]);
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int i = 0; i < TM; ++i) acc[i][j] = mfma_scaled(a[i], w[j], acc[i][j], sa[i], sw[j]);
+      __builtin_amdgcn_sched_barrier(0);
+      // in the order of their use: A 0, W 0, the other A, the other W
+      if (q < NF) fn[q == 0 ? 0 : q == 1 ? TM : q <= TM ? q - 1 : q] = rd(un, q == 0 ? 0 : q == 1 ? TM : q <= TM ? q - 1 : q);
+      if (q >= TM * TN - INS) issue1(u, kt + ST, q - (TM * TN - INS));
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (B == 3) spread_scales();
+    u = un;
+  };
+  using std::integral_constant;
+  int kt = 0;
+  for (; kt + 4 <= nk; kt += 4) {
+    step(kt, f0, f1, integral_constant<int, 0>{});
+    step(kt + 1, f1, f0, integral_constant<int, 1>{});
+    step(kt + 2, f0, f1, integral_constant<int, 2>{});
+    step(kt + 3, f1, f0, integral_constant<int, 3>{});
   }
+  if (kt < nk) step(kt, f0, f1, integral_constant<int, 0>{});
+  if (kt + 1 < nk) step(kt + 1, f1, f0, integral_constant<int, 1>{});
+  if (kt + 2 < nk) step(kt + 2, f0, f1, integral_constant<int, 2>{});
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
-  // The tile in LDS as slabs of 32 (BM = 32: 8) rows x 128, one per wave, columns
-  // XOR 16 ((row >> 2) & 3): then each wave has whole 128-column rows.
+  // The tile in LDS as slabs of BM / NW rows x 128, one per wave, columns XOR 16
+  // ((row >> 2) & 3): then each wave has whole 128-column rows.
   float* tile = (float*)smem;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -423,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        tile[(wm * (BM / 2) + 16 * i + 4 * lq + r) * 128 + ((64 * wn + 16 * j + lr) ^ (lq << 4))] = acc[i][j][r];
+        tile[(wm * WM + 16 * i + 4 * lq + r) * 128 + ((64 * wn + 16 * j + lr) ^ (lq << 4))] = acc[i][j][r];
   __syncthreads();
   constexpr int ROWS = BM / NW;
   EpiLds<KIND> epi(P, m0 + ROWS * wave, n0, lane & 31, lane >> 5, tile + ROWS * wave * 128);
@@ -463,8 +483,8 @@ __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
   const int s0 = ks * per, s1 = min(steps, s0 + per);
   f32x4_t acc[RB][4] = {};
   auto load16 = [&](const uint8_t* p, int k) {
-    const uint4 v = *(const uint4*)(p + min(k, P.K - 16));
-    return k < P.K ? v : make_uint4(0, 0, 0, 0);
+    const i32x4_t v = *(const i32x4_t*)(p + min(k, P.K - 16));
+    return k < P.K ? v : i32x4_t{0, 0, 0, 0};
   };
   auto load = [&](const uint8_t* p, int s) { return frag8(load16(p, 128 * s + 16 * lq), load16(p, 128 * s + 64 + 16 * lq)); };
   constexpr int U = 2;  // steps whose loads are in flight together
@@ -555,8 +575,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
   uint32_t byte = 127;
   float inv = 1.f;
   if constexpr (KIND == EPI_K_FP8) {
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    top = max_over<16>(top);
     byte = e8m0_of(top);
     inv = e8m0_inverse(byte);
   }
@@ -646,20 +665,32 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu) {
     return one ? go(gemm_fp8_small_kernel<64, 1, EPI_K_ANY, false>, 16, 64, 512)
                : go(gemm_fp8_small_kernel<64, 2, EPI_K_ANY, false>, 32, 64, 512);
   }
-  const bool half = tiles(128, 128) < 2 * n_cu;
-  if (f32) return half ? go(gemm_fp8_tile_kernel<64, 3, EPI_K_ANY, true>, 64, 128, 256)
-                       : go(gemm_fp8_tile_kernel<128, 2, EPI_K_ANY, true>, 128, 128, 256);
+  if (f32) return go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true>, 64, 128, 256);
   const bool plain = !(g.flags & DIT_EPI_SILU);
   const bool store = plain && !gated && !fp8 && (g.gelu_from >= g.N || g.gelu_from % 128 == 0) &&
                      (g.gap == 0 || g.gap_at % 128 == 0);
   const bool only_gate = plain && gated && g.rms_cols == 0 && g.gelu_from >= g.N && g.gap == 0;
-  if (tiles(256, 256) >= n_cu)
+  // Rounds of the chip times a tile's time: 4 us and, per slice of 128 of K,
+  struct { int bm, bn, per_cu; double slice_us; } const cfg[] = {
+      {64, 128, 2, 0.62}, {128, 128, 2, 1.0}, {256, 128, 1, 0.95}, {256, 256, 1, 1.5}};
+  int best = 0;
+  double best_us = 1e30;
+  for (int c = 0; c < 4; ++c) {
+    const int64_t slots = (int64_t)n_cu * cfg[c].per_cu;
+    const double us = (double)((tiles(cfg[c].bm, cfg[c].bn) + slots - 1) / slots) * ((g.K + 127) / 128 * cfg[c].slice_us + 4);
+    if (us < best_us) { best_us = us; best = c; }
+  }
+  if (best == 3)
     return go(fp8 ? gemm_fp8_ring_kernel<EPI_K_FP8> : store ? gemm_fp8_ring_kernel<EPI_K_STORE>
               : only_gate ? gemm_fp8_ring_kernel<EPI_K_GATED> : gemm_fp8_ring_kernel<EPI_K_ANY>, 256, 256, 512);
-  if (half) return go(fp8 ? gemm_fp8_tile_kernel<64, 3, EPI_K_FP8, false> : gemm_fp8_tile_kernel<64, 3, EPI_K_ANY, false>,
-                      64, 128, 256);
-  return go(fp8 ? gemm_fp8_tile_kernel<128, 2, EPI_K_FP8, false> : gemm_fp8_tile_kernel<128, 2, EPI_K_ANY, false>, 128, 128,
-            256);
+  if (best == 2)
+    return go(fp8 ? gemm_fp8_tile_kernel<256, EPI_K_FP8, false> : store ? gemm_fp8_tile_kernel<256, EPI_K_STORE, false>
+              : gemm_fp8_tile_kernel<256, EPI_K_ANY, false>, 256, 128, 512);
+  if (best == 1)
+    return go(fp8 ? gemm_fp8_tile_kernel<128, EPI_K_FP8, false> : store ? gemm_fp8_tile_kernel<128, EPI_K_STORE, false>
+              : gemm_fp8_tile_kernel<128, EPI_K_ANY, false>, 128, 128, 256);
+  return go(fp8 ? gemm_fp8_tile_kernel<64, EPI_K_FP8, false> : store ? gemm_fp8_tile_kernel<64, EPI_K_STORE, false>
+              : gemm_fp8_tile_kernel<64, EPI_K_ANY, false>, 64, 128, 256);
 }
 
 }  // namespace dit

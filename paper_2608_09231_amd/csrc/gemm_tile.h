@@ -206,17 +206,25 @@ struct EpiLdsT {
             }
         continue;
       } else if constexpr (KIND == EPI_K_FP8) {
+        // (the flags are wave-uniform: one branch each, not one per value)
+        if (gelu_u) {
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[hh][e] = gelu_tanh_f(v[hh][e]);
+        }
+        if (silu) {
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[hh][e] = silu_f(v[hh][e]);
+        }
         uint32_t top = 0;
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (gelu_u) v[hh][e] = gelu_tanh_f(v[hh][e]);
-            if (silu) v[hh][e] = silu_f(v[hh][e]);
-            top = max(top, __float_as_uint(v[hh][e]) & 0x7fffffffu);
-          }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+          for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(v[hh][e]) & 0x7fffffffu);
+        top = max_over<16>(top);
         const uint32_t byte = e8m0_of(top);
         const float inv = e8m0_inverse(byte);
         if (m < P.M && ncol0 < P.N) {
