@@ -8,6 +8,7 @@ fails loudly when the library has not been built: there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -363,12 +364,18 @@ def _rows(t, name, rows, width, ld, esize):
         raise ValueError(f"{name} must be a device tensor")
     if t.element_size() != esize:
         raise ValueError(f"{name} must have elements of {esize} bytes")
-    if ld is None:
-        ld = t.stride(0) if t.dim() == 2 and t.shape[0] > 1 else width
-    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+    shape = t.shape
+    if ld is None and len(shape) == 2:
+        have, wide = shape
+        step, unit = t.stride()
+        if unit == 1 and have >= rows and wide >= width:
+            return step if have > 1 else max(step, width)
+        ld = step if have > 1 else width
+    elif ld is None:
+        ld = width
+    if len(shape) and shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    have = t.untyped_storage().nbytes() // esize - t.storage_offset()
-    if rows > 0 and (rows - 1) * ld + width > have:
+    if rows > 0 and (rows - 1) * ld + width > t.untyped_storage().nbytes() // esize - t.storage_offset():
         raise ValueError(f"{name} must hold {rows} rows of {width} elements with stride {ld}")
     return ld
 
@@ -377,24 +384,24 @@ class _Call:
     """Device and stream of one call: the tensors' device becomes the current one, the stream (default: that
     device's current one) must be its own."""
 
+    __slots__ = ("stream", "ptr", "_dev", "_guard", "_torch")
+
     def __init__(self, stream, first, *more):
         import torch
-        self._dev = first.device
+        dev = first.device
         for t in more:
-            if t is not None and t.device != self._dev:
+            if t is not None and t.device != dev:
                 raise ValueError("all tensors of a call must be on one device")
-        if stream is not None and stream.device != self._dev:
+        if stream is not None and stream.device != dev:
             raise ValueError("the stream belongs to another device than the tensors")
-        self._torch, self.stream = torch, stream
-        same = torch.cuda.current_device() == self._dev.index
-        self._guard = None if same else torch.cuda.device(self._dev)
+        self._torch, self._dev, self.stream = torch, dev, stream
+        self._guard = None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
 
     def __enter__(self):
         if self._guard is not None:
             self._guard.__enter__()
-        if self.stream is None:
-            self.stream = self._torch.cuda.current_stream(self._dev)
-        self.ptr = C.c_void_p(self.stream.cuda_stream)
+        self.ptr = self._torch._C._cuda_getCurrentRawStream(self._dev.index) if self.stream is None \
+            else self.stream.cuda_stream
         return self
 
     def __exit__(self, *exc):
@@ -406,8 +413,11 @@ class _Call:
         if nbytes == 0:
             return None
         if ws is None:
-            with self._torch.cuda.stream(self.stream):
-                return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self._dev)
+            torch = self._torch
+            if self.stream is None:
+                return torch.empty(nbytes, dtype=torch.uint8, device=self._dev)
+            with torch.cuda.stream(self.stream):
+                return torch.empty(nbytes, dtype=torch.uint8, device=self._dev)
         if not ws.is_cuda or ws.device != self._dev or not ws.is_contiguous() or ws.numel() * ws.element_size() < nbytes:
             raise ValueError(f"{name} must be a contiguous tensor of {nbytes} bytes on the call's device")
         return ws
@@ -464,20 +474,31 @@ def sparse_shape(*, Lq, Lk, heads, topk, kv_heads=None, batch=1, klen=None) -> S
                         klen.data_ptr() if klen is not None else None)
 
 
+@functools.lru_cache(256)
+def _ws_bytes(name, *sizes):
+    """A workspace's size depends on the shape's numbers alone."""
+    return getattr(load(), name)(C.byref(SparseShapeC(*sizes, None)))
+
+
+def _ws_of(name, s):
+    return _ws_bytes(name, s.batch, s.Lq, s.Lk, s.heads, s.kv_heads, s.topk)
+
+
 def select_blocks_ws_bytes(**shape) -> int:
-    return load().dit_select_blocks_ws_bytes(C.byref(sparse_shape(**shape)))
+    return _ws_of("dit_select_blocks_ws_bytes", sparse_shape(**shape))
 
 
 def attention_sparse_ws_bytes(**shape) -> int:
-    return load().dit_attention_sparse_ws_bytes(C.byref(sparse_shape(**shape)))
+    return _ws_of("dit_attention_sparse_ws_bytes", sparse_shape(**shape))
 
 
 def _lists(idx, s):
-    if idx.is_floating_point():
+    if not idx.is_cuda:
+        raise ValueError("idx must be a device tensor")
+    if idx.element_size() != 4 or idx.is_floating_point():
         raise ValueError("idx must be int32")
-    _rows(idx, "idx", 1, s.batch * s.heads * -(-s.Lq // SPARSE_QB) * s.topk, None, 4)
-    if not idx.is_contiguous():
-        raise ValueError("idx must be contiguous")
+    if not idx.is_contiguous() or idx.numel() < s.batch * s.heads * -(-s.Lq // SPARSE_QB) * s.topk:
+        raise ValueError("idx must be contiguous and hold every list")
 
 
 def select_blocks_bf16(q, k, idx, *, first=0, ldq=None, ldk=None, ws=None, stream=None, **shape):
@@ -489,7 +510,7 @@ def select_blocks_bf16(q, k, idx, *, first=0, ldq=None, ldk=None, ws=None, strea
     ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2)
     _lists(idx, s)
     with _Call(stream, q, k, idx, shape.get("klen")) as call:
-        w = call.workspace(ws, lib.dit_select_blocks_ws_bytes(C.byref(s)) or 16, "ws")
+        w = call.workspace(ws, _ws_of("dit_select_blocks_ws_bytes", s) or 16, "ws")
         _check(lib.dit_select_blocks_bf16(C.byref(s), q.data_ptr(), ldq, k.data_ptr(), ldk, first, idx.data_ptr(),
                                           w.data_ptr(), call.ptr))
 
@@ -505,7 +526,7 @@ def attention_sparse_bf16(q, k, v, o, idx, *, flags=0, ldq=None, ldk=None, ldv=N
     ldo = _rows(o, "o", s.batch * s.Lq, s.heads * 128, ldo, 2)
     _lists(idx, s)
     with _Call(stream, q, k, v, o, idx, shape.get("klen")) as call:
-        w = call.workspace(ws, lib.dit_attention_sparse_ws_bytes(C.byref(s)), "ws")
+        w = call.workspace(ws, _ws_of("dit_attention_sparse_ws_bytes", s), "ws")
         _check(lib.dit_attention_sparse_bf16(C.byref(s), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                              o.data_ptr(), ldo, idx.data_ptr(), flags,
                                              w.data_ptr() if w is not None else None, call.ptr))

@@ -232,6 +232,33 @@ struct SparseArgs {
 // A piece of an item: its unnormalised outputs [rows][128], row sums and running maxima.
 __host__ __device__ __forceinline__ int64_t piece_floats(int rows) { return (int64_t)rows * (D + 2); }
 
+// 16 bytes per lane from base + off (valid up to `bytes`; zeros past it) to LDS at
+// dst + 16 lane, as an instruction that the compiler does not see through: it
+// would have every transposing read of LDS wait for all copies in flight.  The
+// kernel's own waits and barriers order them.  (No registers come back; the
+// address escapes, so that the barriers' memory clobbers cover what is written.)
+__device__ __forceinline__ void copy16_unseen(const void* base, uint32_t bytes, const void* dst, uint32_t off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const uint64_t b = (uint64_t)base;
+  const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, bytes, 0x00020000u};
+  const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)dst;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(l), "v"(off), "s"(r));
+#endif
+}
+
+// Largest of three in one instruction (a NaN gives way to a number, as with fmaxf,
+// which the compiler makes of several to quiet signalling NaNs first).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+#else
+  return fmaxf(fmaxf(a, b), c);
+#endif
+}
+
 // The valid entries of one list, in their order; every wave walks it alike.
 struct ListCursor {
   const int32_t* p;
@@ -252,18 +279,63 @@ struct ListCursor {
   }
 };
 
-// Four waves of 32 queries on one list, two work-groups per CU; K and V tiles of
-// 64 keys in XOR-swizzled LDS rows of 256 bytes, two of each.  The products
-// and the softmax are those of the dense kernel (S^T = K Q^T, O^T = V^T P^T);
-// V^T fragments are read from the row-major tile by transposing LDS reads, so no
-// transposed copy of V is made.
-template <bool BOUNDED>
-__global__ __launch_bounds__(256, 2) void attn_sparse_kernel(SparseArgs P) {
+// Transposed V fragment from LDS: four keys from p and four from 16 rows further down.
+__device__ __forceinline__ bf16x8_t vt_frag(const char* p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int TILE = KT * D * 2;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // K, V of even tiles, then of odd ones
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+  const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
+  const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 16 * 256)));
+  return __builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y));
+#else
+  return bf16x8_t{};
+#endif
+}
+
+// A wave's 32 queries (block rows wrow ..), 16 per group, d blocks of 16: normalised to o, or as a part of the list.
+__device__ __forceinline__ void store_rows(const SparseArgs& P, const f32x4_t (&acc)[8][2], const float (&l)[2],
+                                           const float (&m)[2], int unit, int z, int h, int qb, int wrow, int lr, int lq) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const int row = wrow + 16 * g + lr, qi = qb * QBLK + row;
+    const float ls = sum_quarters(l[g]);
+    if (qi >= P.Lq) continue;
+    if (P.parts == 1) {
+      const float inv = ls == 0.f ? 0.f : 1.f / ls;  // no key: zeros
+      bf16_t* op = P.o + ((int64_t)z * P.Lq + qi) * P.ldo + h * D + 4 * lq;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+        *(uint2*)(op + 16 * dt) = make_uint2(pack_bf16x2(acc[dt][g][0] * inv, acc[dt][g][1] * inv),
+                                             pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
+    } else {
+      float* w = P.ws + unit * piece_floats(P.rows);
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(w + row * D + 16 * dt + 4 * lq) = acc[dt][g];
+      if (lq == 0) {
+        w[P.rows * D + row] = ls;
+        w[P.rows * D + P.rows + row] = m[g];
+      }
+    }
+  }
+}
+
+// One work-group per list (or part of one): TP groups of four waves, each with tiles
+// of 64 keys of K and V of its own in XOR-swizzled LDS rows of 256 bytes, two of
+// each; the products are those of the dense kernel (S^T = K Q^T, O^T = V^T P^T,
+// probabilities from one to the other in registers).  V^T fragments are read from
+// the row-major tile by transposing LDS reads, so no transposed copy of V is made.
+//
+// TP = 1: two work-groups per CU, one's softmax beside the other's products.  TP =
+// 2: one per CU, for launches that leave no second one; the groups take tiles in
+// turn, and their outputs meet in LDS.
+template <bool BOUNDED, int TP>
+__global__ __launch_bounds__(256 * TP, 2) void attn_sparse_kernel(SparseArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int TILE = KT * D * 2, STAGE = 2 * TILE;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * TP * STAGE];  // [group][stage][K | V]
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = TP == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 8);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;  // of its group
   const int lr = lane & 15, lq = lane >> 4;
   const int unit = xcd_remap(blockIdx.x, P.items * P.parts);
   const int item = unit / P.parts, part = unit - item * P.parts;
@@ -286,17 +358,19 @@ __global__ __launch_bounds__(256, 2) void attn_sparse_kernel(SparseArgs P) {
     ko[c] = (uint32_t)row * (uint32_t)P.ldk * 2u + ch;
     vo[c] = (uint32_t)row * (uint32_t)P.ldv * 2u + ch;
   }
-  auto issue = [&](int kb, int st) {  // rows past the last key read zeros
+  // Rows past the last key are zeros; so is all of no tile (kb < 0), copied to keep
+  // the number of copies in flight the same.
+  auto issue = [&](int kb, int at) {
     const uint32_t last = min(nkeys - kb * KBLK, KBLK) - 1;
-    const bf16_t* kp = kbase + (int64_t)kb * KBLK * P.ldk;
-    const bf16_t* vp = vbase + (int64_t)kb * KBLK * P.ldv;
-    char* d = smem + st * 2 * TILE + wave * 4096;
+    const int64_t row = (int64_t)max(kb, 0) * KBLK;
+    const uint32_t kn = kb < 0 ? 0u : last * (uint32_t)P.ldk * 2u + 2u * D;
+    const uint32_t vn = kb < 0 ? 0u : last * (uint32_t)P.ldv * 2u + 2u * D;
+    char* d = smem + 2 * grp * STAGE + at + wave * 4096;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) copy16(kp, last * (uint32_t)P.ldk * 2u + 2u * D, (lds_void_t*)(d + c * 1024), ko[c]);
+    for (int c = 0; c < 4; ++c) copy16_unseen(kbase + row * P.ldk, kn, d + c * 1024, ko[c]);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) copy16(vp, last * (uint32_t)P.ldv * 2u + 2u * D, (lds_void_t*)(d + TILE + c * 1024), vo[c]);
+    for (int c = 0; c < 4; ++c) copy16_unseen(vbase + row * P.ldv, vn, d + TILE + c * 1024, vo[c]);
   };
-
   bf16x8_t qf[2][4];
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
@@ -304,16 +378,27 @@ __global__ __launch_bounds__(256, 2) void attn_sparse_kernel(SparseArgs P) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) qf[g][s] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 32 * s));
   }
-  int koff[4], voff[8];
+  // Key blocks of the group's tile and of any (the first group's comes first).  The
+  // queries arrive with the list: waited for later, they would wait for the copies, too.
+  auto take = [&](int& any) {
+    any = list.next();
+    if constexpr (TP == 1) return any;
+    const int second = any < 0 ? -1 : list.next();
+    return grp ? second : any;
+  };
+  int any, cur = take(any);
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(qf[g][s]));
+  issue(cur, 0);
+  int koff[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) koff[s] = k_off(lr, 4 * s + lq);
   // V^T fragment (d = 16 dt + lr; keys 4 lq .. + 3 of a 16-key block): lane 4 k + j of a
-  // quarter addresses row 4 lq + k, columns 16 dt + 4 j, and receives column lr
-#pragma unroll
-  for (int dt = 0; dt < 8; ++dt) {
-    const int row = 4 * lq + (lr >> 2);
-    voff[dt] = TILE + k_off(row, 2 * dt + ((lr & 3) >> 1)) + 8 * (lr & 1);
-  }
+  // quarter addresses row 4 lq + k, columns 16 dt + 4 j, and receives column lr.  The
+  // chunk 2 dt + (j >> 1) enters the swizzled address by XOR.
+  const int voff = k_off(4 * lq + (lr >> 2), (lr & 3) >> 1) + 8 * (lr & 1);
   f32x4_t acc[8][2];
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) acc[dt][0] = acc[dt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -321,45 +406,45 @@ __global__ __launch_bounds__(256, 2) void attn_sparse_kernel(SparseArgs P) {
   m[0] = m[1] = BOUNDED ? BOUNDED_SHIFT_LOG2 : -INFINITY;
   const bf16x2_t ones = {(__bf16)1.f, (__bf16)1.f};
 
-  int cur = list.next();
-  if (cur >= 0) issue(cur, 0);
-  int st = 0;
-  while (cur >= 0) {
-    const int nxt = list.next();
+  int at = 0;
+  while (any >= 0) {
+    const int nxt = take(any);
     // this tile has landed and everyone is done with the one before it
     __builtin_amdgcn_s_waitcnt(0);
     barrier_no_fence();
-    if (nxt >= 0) issue(nxt, st ^ 1);
-    if (active) {
-      const char* sk = smem + st * 2 * TILE;
+    issue(nxt, at ^ STAGE);
+    if (active && cur >= 0) {
+      const char* sk = smem + 2 * grp * STAGE + at;
+      const int keys = nkeys - cur * KBLK;
       f32x4_t s[4][2];
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
         s[kb][0] = s[kb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t] + kb * 16 * 256));
+        for (int t4 = 0; t4 < 4; ++t4) {
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t4] + kb * 16 * 256));
 #pragma unroll
-          for (int g = 0; g < 2; ++g) s[kb][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t], s[kb][g], 0, 0, 0);
+          for (int g = 0; g < 2; ++g) s[kb][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t4], s[kb][g], 0, 0, 0);
         }
       }
-      if ((cur + 1) * KBLK > nkeys) {
+      if (keys < KBLK) {
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (cur * KBLK + 16 * kb + 4 * lq + r >= nkeys) s[kb][0][r] = s[kb][1][r] = -INFINITY;
+            if (16 * kb + 4 * lq + r >= keys) s[kb][0][r] = s[kb][1][r] = -INFINITY;
       }
       bf16x8_t pf[2][2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         if constexpr (!BOUNDED) {
-          float mx = -INFINITY;
+          float mx = s[0][g][0];
 #pragma unroll
           for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[kb][g][r]);
+            for (int r = 0; r < 4; r += 2) mx = max3(mx, s[kb][g][r], s[kb][g][r + 1]);
           mx = max_quarters(mx) * P.scale_log2;
+          // (kept unless the new one is well above it: softmax is shift invariant)
           const bool up = mx > m[g] + RESCALE_SLACK;
           if (__builtin_amdgcn_ballot_w64(up)) {
             const float mn = up ? mx : m[g];
@@ -391,43 +476,439 @@ __global__ __launch_bounds__(256, 2) void attn_sparse_kernel(SparseArgs P) {
       for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          typedef short s4 __attribute__((ext_vector_type(4)));
-          typedef __attribute__((address_space(3))) s4* lds_s4;
-          const char* p = sk + voff[dt] + ks * 32 * 256;
-          const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)p);
-          const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p + 16 * 256));
-          const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
-          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(a.x, a.y, b.x, b.y));
+          const bf16x8_t vf = vt_frag(sk + TILE + (voff ^ (dt << 5)) + ks * 32 * 256);
 #pragma unroll
           for (int g = 0; g < 2; ++g) acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[ks][g], acc[dt][g], 0, 0, 0);
         }
     }
-    st ^= 1;
     cur = nxt;
+    at ^= STAGE;
   }
-  if (!active) return;
+  if constexpr (TP == 2) {
+    __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
+    __syncthreads();
+    f32x4_t* so = (f32x4_t*)smem + (wave * 64 + lane) * 17;  // the second group's outputs, lane by lane
+    float* sm = (float*)(so + 16);
+    if (grp) {
 #pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    const int row = 32 * wave + 16 * g + lr, qi = qb * QBLK + row;
-    const float ls = sum_quarters(l[g]);
-    if (qi >= P.Lq) continue;
-    if (P.parts == 1) {
-      const float inv = ls == 0.f ? 0.f : 1.f / ls;  // no key: zeros
-      bf16_t* op = P.o + ((int64_t)z * P.Lq + qi) * P.ldo + h * D + 4 * lq;
+      for (int g = 0; g < 2; ++g) {
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt)
-        *(uint2*)(op + 16 * dt) = make_uint2(pack_bf16x2(acc[dt][g][0] * inv, acc[dt][g][1] * inv),
-                                             pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
-    } else {
-      float* w = P.ws + unit * piece_floats(P.rows);
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(w + row * D + 16 * dt + 4 * lq) = acc[dt][g];
-      if (lq == 0) {
-        w[P.rows * D + row] = ls;
-        w[P.rows * D + P.rows + row] = m[g];
+        for (int dt = 0; dt < 8; ++dt) so[8 * g + dt] = acc[dt][g];
+        sm[g] = l[g];
+        sm[2 + g] = m[g];
       }
     }
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const float mn = fmaxf(m[g], sm[2 + g]), shift = neg_shift(mn);
+      const float a = __builtin_amdgcn_exp2f(m[g] + shift), b = __builtin_amdgcn_exp2f(sm[2 + g] + shift);
+      l[g] = a * l[g] + b * sm[g];
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        const f32x4_t x = so[8 * g + dt];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[dt][g][r] = a * acc[dt][g][r] + b * x[r];
+      }
+      m[g] = mn;
+    }
   }
+  if (active) store_rows(P, acc, l, m, unit, z, h, qb, 32 * wave, lr, lq);
+#endif
+}
+
+// At most 16 NG queries a sequence (single tokens, say): what bounds it is the way
+// of K and V from memory.  Each of four waves takes all queries and its own share
+// of the list, 32 keys at a time in its own two buffers of LDS: no wave waits for
+// another until their four parts meet at the end.
+template <bool BOUNDED, int NG>
+__global__ __launch_bounds__(256, 1) void attn_few_kernel(SparseArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int HK = 32, TILE = HK * D * 2, STAGE = 2 * TILE, ROWS = 16 * NG, LD = D + 4;
+  __shared__ __attribute__((aligned(1024))) char smem[8 * STAGE];  // [wave][stage][K | V]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lq = lane >> 4;
+  const int unit = xcd_remap(blockIdx.x, P.items * P.parts);
+  const int item = unit / P.parts, part = unit - item * P.parts;  // one query block: item = z heads + h
+  const int z = item / P.heads, h = item - z * P.heads, g_ = h / (P.heads / P.kv_heads);
+  const int nkeys = keys_of(P.klen, z, P.Lk), nkb = (nkeys + KBLK - 1) / KBLK;
+  const int shares = 4 * P.parts, share = 4 * part + wave;
+  const int p0 = (int)((int64_t)P.topk * share / shares), p1 = (int)((int64_t)P.topk * (share + 1) / shares);
+  ListCursor list(P.idx + (int64_t)item * P.topk + p0, p1 - p0, nkb);
+
+  const bf16_t* kbase = P.k + (int64_t)z * P.Lk * P.ldk + g_ * D;
+  const bf16_t* vbase = P.v + (int64_t)z * P.Lk * P.ldv + g_ * D;
+  bf16x8_t qf[NG][4];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const bf16_t* qp = P.q + ((int64_t)z * P.Lq + min(16 * g + lr, P.Lq - 1)) * P.ldq + h * D + 8 * lq;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) qf[g][s] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 32 * s));
+  }
+  // first key of the next 32; -1: none
+  int kb = list.next(), half = 0;
+#pragma unroll
+  for (int g = 0; g < NG; ++g)  // the queries arrive with the list: waited for later, they would wait for the copies, too
+#pragma unroll
+    for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(qf[g][s]));
+  auto next = [&]() {
+    const int k = kb < 0 ? -1 : kb * KBLK + 32 * half;
+    if (kb >= 0 && (half || k + 32 >= nkeys)) {  // a block's second half may hold no key
+      kb = list.next();
+      half = 0;
+    } else {
+      half = 1;
+    }
+    return k;
+  };
+  // copy c: rows 4 c .. + 3; rows past the last key, and all of none, are zeros
+  auto issue = [&](int k, int st) {
+    const uint32_t rows = k < 0 ? 0u : (uint32_t)min(nkeys - k, HK);
+    const bf16_t* kp = kbase + (int64_t)max(k, 0) * P.ldk;
+    const bf16_t* vp = vbase + (int64_t)max(k, 0) * P.ldv;
+    const uint32_t kn = rows ? (rows - 1) * (uint32_t)P.ldk * 2u + 2u * D : 0u;
+    const uint32_t vn = rows ? (rows - 1) * (uint32_t)P.ldv * 2u + 2u * D : 0u;
+    char* d = smem + (2 * wave + st) * STAGE;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t row = 4 * c + (lane >> 4), ch = ((lane & 15) ^ (row & 15)) << 4;
+      copy16_unseen(kp, kn, d + c * 1024, row * (uint32_t)P.ldk * 2u + ch);
+      copy16_unseen(vp, vn, d + TILE + c * 1024, row * (uint32_t)P.ldv * 2u + ch);
+    }
+  };
+  int koff[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) koff[s] = k_off(lr, 4 * s + lq);
+  const int voff = k_off(4 * lq + (lr >> 2), (lr & 3) >> 1) + 8 * (lr & 1);  // as in attn_sparse_kernel
+  f32x4_t acc[8][NG] = {};
+  float m[NG], l[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) { m[g] = BOUNDED ? BOUNDED_SHIFT_LOG2 : -INFINITY; l[g] = 0.f; }
+  const bf16x2_t ones = {(__bf16)1.f, (__bf16)1.f};
+
+  int cur = next(), st = 0;
+  issue(cur, 0);
+  while (cur >= 0) {
+    const int nxt = next();
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the other buffer is read
+    asm volatile("" ::: "memory");
+    issue(nxt, st ^ 1);
+    wait_vmcnt<16>();  // this one has landed
+    asm volatile("" ::: "memory");
+    const char* sk = smem + (2 * wave + st) * STAGE;
+    f32x4_t s[2][NG];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t] + b * 16 * 256));
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+          s[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t], t ? s[b][g] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+    if (cur + HK > nkeys) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (cur + 16 * b + 4 * lq + r >= nkeys)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) s[b][g][r] = -INFINITY;
+    }
+    bf16x8_t pf[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if constexpr (!BOUNDED) {
+        float mx = s[0][g][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; r += 2) mx = max3(mx, s[b][g][r], s[b][g][r + 1]);
+        mx = max_quarters(mx) * P.scale_log2;
+        const bool up = mx > m[g] + RESCALE_SLACK;
+        if (__builtin_amdgcn_ballot_w64(up)) {
+          const float mn = up ? mx : m[g];
+          const float a = up ? __builtin_amdgcn_exp2f(m[g] - mn) : 1.f;
+          l[g] *= a;
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[dt][g][r] *= a;
+          m[g] = mn;
+        }
+      }
+      const float mneg = BOUNDED ? -BOUNDED_SHIFT_LOG2 : neg_shift(m[g]);
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4_t& x = s[e >> 1][g];
+        w[e] = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * (e & 1)], P.scale_log2, mneg)),
+                           __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * (e & 1) + 1], P.scale_log2, mneg)));
+        // the sum takes exactly the rounded values that the second product uses
+        l[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[e]), ones, l[g], false);
+      }
+      pf[g] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      const bf16x8_t vf = vt_frag(sk + TILE + (voff ^ (dt << 5)));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[g], acc[dt][g], 0, 0, 0);
+    }
+    cur = nxt;
+    st ^= 1;
+  }
+  // the waves' parts in LDS; then eight threads a row, 16 columns each
+  __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
+  __syncthreads();
+  float* so = (float*)smem;                // [wave][row][LD]
+  float* sl = so + 4 * ROWS * LD;          // [wave][row]: sums, then maxima
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const float ls = sum_quarters(l[g]);
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(so + (wave * ROWS + 16 * g + lr) * LD + 16 * dt + 4 * lq) = acc[dt][g];
+    if (lq == 0) {
+      sl[wave * ROWS + 16 * g + lr] = ls;
+      sl[(4 + wave) * ROWS + 16 * g + lr] = m[g];
+    }
+  }
+  __syncthreads();
+  const int row = tid >> 3, c = 4 * (tid & 7);
+  if (row >= P.Lq) return;
+  float mx = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sl[(4 + w) * ROWS + row]);
+  const float shift = neg_shift(mx);
+  float den = 0.f;
+  f32x4_t y[4] = {};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sl[(4 + w) * ROWS + row] + shift);
+    den += f * sl[w * ROWS + row];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4_t x = *(const f32x4_t*)(so + (w * ROWS + row) * LD + c + 32 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[i][e] += f * x[e];
+    }
+  }
+  if (P.parts == 1) {
+    const float inv = den == 0.f ? 0.f : 1.f / den;  // no key: zeros
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(uint2*)(P.o + ((int64_t)z * P.Lq + row) * P.ldo + h * D + c + 32 * i) =
+          make_uint2(pack_bf16x2(y[i][0] * inv, y[i][1] * inv), pack_bf16x2(y[i][2] * inv, y[i][3] * inv));
+  } else {
+    float* w = P.ws + unit * piece_floats(P.rows);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(f32x4_t*)(w + row * D + c + 32 * i) = y[i];
+    if (c == 0) {
+      w[P.rows * D + row] = den;
+      w[P.rows * D + P.rows + row] = mx;
+    }
+  }
+#endif
+}
+
+// attn_sparse_kernel for long lists of bounded logits, two work-groups per CU; K and V tiles in
+// LDS: three K, two V.
+//
+// Iteration t issues the score product of tile t + 1 and the PV product of tile
+// t - 1 on MFMA with the softmax of tile t, which depends on neither, between
+// them in 32 fenced slots of two MFMAs, one fragment read AHEAD slots before its use
+// and a share of the softmax.  Its copies are V of tile t and K of tile t + 3.
+__global__ __launch_bounds__(256, 2) void attn_sparse_long_kernel(SparseArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int TILE = KT * D * 2, VBASE = 3 * TILE;
+  __shared__ __attribute__((aligned(1024))) char smem[5 * TILE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lq = lane >> 4;
+  const int unit = xcd_remap(blockIdx.x, P.items * P.parts);
+  const int item = unit / P.parts, part = unit - item * P.parts;
+  const int hz = item / P.nqb, qb = item - hz * P.nqb;
+  const int z = hz / P.heads, h = hz - z * P.heads, g_ = h / (P.heads / P.kv_heads);
+  const int nkeys = keys_of(P.klen, z, P.Lk), nkb = (nkeys + KBLK - 1) / KBLK;
+  const int p0 = (int)((int64_t)P.topk * part / P.parts), p1 = (int)((int64_t)P.topk * (part + 1) / P.parts);
+  ListCursor list(P.idx + (int64_t)item * P.topk + p0, p1 - p0, nkb);
+
+  const int q0 = qb * QBLK + 32 * wave;
+  const bool active = q0 < P.Lq;  // wave-uniform; idle waves copy and meet the others
+  const bf16_t* kbase = P.k + (int64_t)z * P.Lk * P.ldk + g_ * D;
+  const bf16_t* vbase = P.v + (int64_t)z * P.Lk * P.ldv + g_ * D;
+  // copy c of this wave: rows 4 (4 wave + c) .. + 3 of a tile
+  uint32_t ko[4], vo[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int row = 4 * (4 * wave + c) + (lane >> 4);
+    const uint32_t ch = ((lane & 15) ^ (row & 15)) << 4;
+    ko[c] = (uint32_t)row * (uint32_t)P.ldk * 2u + ch;
+    vo[c] = (uint32_t)row * (uint32_t)P.ldv * 2u + ch;
+  }
+  // Rows past the last key, and all rows of no tile (kb < 0), are zeros.
+  struct Src {
+    const bf16_t* p;
+    uint32_t bytes;
+  };
+  auto src = [&](const bf16_t* base, int64_t ld, int kb) {
+    const int rows = min(nkeys - kb * KBLK, KBLK);
+    return Src{base + (int64_t)max(kb, 0) * KBLK * ld, kb < 0 ? 0u : (uint32_t)(rows - 1) * (uint32_t)ld * 2u + 2u * D};
+  };
+  auto copy = [&](const Src& x, int at, uint32_t off, int c) {
+    copy16_unseen(x.p, x.bytes, smem + at + (4 * wave + c) * 1024, off);
+  };
+
+  bf16x8_t qf[2][4];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const bf16_t* qp = P.q + ((int64_t)z * P.Lq + min(q0 + 16 * g + lr, P.Lq - 1)) * P.ldq + h * D + 8 * lq;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) qf[g][s] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 32 * s));
+  }
+  int koff[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) koff[s] = k_off(lr, 4 * s + lq);
+  // V^T fragment (d = 16 dt + lr; keys 4 lq .. + 3 of a 16-key block): lane 4 k + j of a
+  // quarter addresses row 4 lq + k, columns 16 dt + 4 j, and receives column lr.  The
+  // chunk 2 dt + (j >> 1) enters the swizzled address by XOR.
+  const int voff = k_off(4 * lq + (lr >> 2), (lr & 3) >> 1) + 8 * (lr & 1);
+  // A tile's fragments in the order of their use, K 0..15 and V^T 0..15, so that four
+  // independent accumulators stand between the steps of a dependent chain.
+  auto k_kb = [](int i) { return 2 * (i >> 3) + (i & 1); };
+  auto k_s = [](int i) { return (i >> 1) & 3; };
+  auto v_dt = [](int i) { return 2 * (i >> 2) + (i & 1); };
+  auto v_ks = [](int i) { return (i >> 1) & 1; };
+  auto k_frag = [&](int at, int i) {
+    return __builtin_bit_cast(bf16x8_t, *(const uint4*)(smem + at + koff[k_s(i)] + k_kb(i) * 16 * 256));
+  };
+  auto v_frag = [&](int at, int i) { return vt_frag(smem + (voff ^ (v_dt(i) << 5)) + at + v_ks(i) * 32 * 256); };
+  f32x4_t acc[8][2], sb[2][4][2];
+  bf16x8_t pb[2][2][2];
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt) acc[dt][0] = acc[dt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float l[2] = {0.f, 0.f};
+  const bf16x2_t ones = {(__bf16)1.f, (__bf16)1.f};
+  auto score_step = [&](int i, const bf16x8_t& kf, f32x4_t (&s)[4][2]) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x4_t& c = s[k_kb(i)][g];
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][k_s(i)], k_s(i) ? c : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    }
+  };
+  auto pv_step = [&](int i, const bf16x8_t& vf, const bf16x8_t (&pf)[2][2]) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      acc[v_dt(i)][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[v_ks(i)][g], acc[v_dt(i)][g], 0, 0, 0);
+  };
+  // Step i of 16 of a tile's softmax: two probabilities of a query group.
+  struct Soft {
+    float sum[2];
+    uint32_t w[4];
+  };
+  auto exp_step = [&](int i, const f32x4_t (&s)[4][2], bf16x8_t (&pf)[2][2], Soft& x) {
+    const int g = i >> 3, ks = (i >> 2) & 1, e = i & 3;
+    const f32x4_t& c = s[2 * ks + (e >> 1)][g];
+    x.w[e] = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(c[2 * (e & 1)], P.scale_log2, -BOUNDED_SHIFT_LOG2)),
+                         __builtin_amdgcn_exp2f(__builtin_fmaf(c[2 * (e & 1) + 1], P.scale_log2, -BOUNDED_SHIFT_LOG2)));
+    // formed here: the branches between iterations would otherwise draw the softmax
+    // past the barrier, away from the MFMAs
+    asm volatile("" : "+v"(x.w[e]));
+    // the sum takes exactly the rounded values that the second product uses
+    x.sum[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.w[e]), ones, (i & 7) ? x.sum[g] : 0.f, false);
+    if (e == 3) pf[ks][g] = __builtin_bit_cast(bf16x8_t, make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]));
+  };
+  // keys of a tile past the sequence's last one; all of no tile (kb < 0)
+  auto keys_in = [&](int kb) { return kb < 0 ? 0 : nkeys - kb * KBLK; };
+  auto mask = [&](int keys, f32x4_t (&s)[4][2]) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (16 * b + 4 * lq + r >= keys) s[b][0][r] = s[b][1][r] = -INFINITY;
+  };
+
+  // Key blocks of tiles t .. t + 3 (-1: none), K places of tiles t, t + 1, t + 2.
+  // Tiles come in pairs; a last one without keys adds nothing.
+  int i0 = -1, i1 = -1, i2 = -1, i3 = -1;
+  int ks0 = 0, ks1 = TILE, ks2 = 2 * TILE;
+  for (int u = 0; u < 3; ++u) {
+    i0 = i1; i1 = i2;
+    i2 = list.next();
+    const Src x = src(kbase, P.ldk, i2);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) copy(x, u * TILE, ko[c], c);
+  }
+  i3 = list.next();
+  const Src none = src(vbase, P.ldv, -1);  // "tile - 1"
+#pragma unroll
+  for (int c = 0; c < 4; ++c) copy(none, VBASE + TILE, vo[c], c);
+  // End of an iteration: its copies have landed and the waves meet.  Fragments still
+  // on their way are of K of tile t + 2, which stays for another iteration.
+  auto meet = [&]() {
+    wait_vmcnt<0>();
+    barrier_no_fence();
+    i0 = i1; i1 = i2; i2 = i3;
+    i3 = list.next();
+    const int k = ks0;
+    ks0 = ks1; ks1 = ks2; ks2 = k;
+  };
+  constexpr int AHEAD = 4;
+  bf16x8_t fr[AHEAD];
+  auto iter = [&](auto par) {
+    constexpr int B = decltype(par)::value;
+    const Src vs = src(vbase, P.ldv, i0), kn = src(kbase, P.ldk, i3);
+    if (keys_in(i0) < KBLK) mask(keys_in(i0), sb[B]);
+    Soft x;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (i < 16) score_step(i, fr[i % AHEAD], sb[B ^ 1]);
+      else pv_step(i - 16, fr[i % AHEAD], pb[B ^ 1]);
+      const int n = i + AHEAD;
+      fr[i % AHEAD] = n < 16 ? k_frag(ks1, n) : n < 32 ? v_frag(VBASE + (B ^ 1) * TILE, n - 16) : k_frag(ks2, n - 32);
+      if (i % 2 == 0 && i < 16) {
+        if (i < 8) copy(vs, VBASE + B * TILE, vo[i / 2], i / 2);
+        else copy(kn, ks0, ko[i / 2 - 4], i / 2 - 4);
+      }
+      if (i & 1) exp_step(i >> 1, sb[B], pb[B], x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) l[g] += x.sum[g];
+    meet();
+  };
+  wait_vmcnt<0>();
+  barrier_no_fence();
+  if (active) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) score_step(i, k_frag(0, i), sb[0]);
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) fr[f] = k_frag(ks1, f);
+    pb[1][0][0] = pb[1][0][1] = pb[1][1][0] = pb[1][1][1] = __builtin_bit_cast(bf16x8_t, make_uint4(0, 0, 0, 0));
+    wait_vmcnt_lgkm0<0>();
+    barrier_no_fence();  // K of tile 0 is read: its place is free
+    while (i0 >= 0) {
+      iter(std::integral_constant<int, 0>{});
+      iter(std::integral_constant<int, 1>{});
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) pv_step(i, v_frag(VBASE + TILE, i), pb[1]);
+  } else {
+    barrier_no_fence();
+    for (int par = 0; par || i0 >= 0; par ^= 1) {
+      const Src vs = src(vbase, P.ldv, i0), kn = src(kbase, P.ldk, i3);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) copy(vs, VBASE + par * TILE, vo[c], c);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) copy(kn, ks0, ko[c], c);
+      meet();
+    }
+  }
+  const float m[2] = {BOUNDED_SHIFT_LOG2, BOUNDED_SHIFT_LOG2};
+  if (active) store_rows(P, acc, l, m, unit, z, h, qb, 32 * wave, lr, lq);
 #endif
 }
 
@@ -440,18 +921,37 @@ __global__ __launch_bounds__(256) void sparse_combine_kernel(SparseArgs P) {
   if (row >= P.rows || qi >= P.Lq) return;
   const int64_t pf = piece_floats(P.rows);
   const float* w = P.ws + (int64_t)item * P.parts * pf;
+  // parts in groups whose loads are in flight together, first their maxima
+  constexpr int U = 8;
   float mx = -INFINITY;
-  for (int p = 0; p < P.parts; ++p) mx = fmaxf(mx, w[p * pf + P.rows * D + P.rows + row]);
+  for (int p = 0; p < P.parts; p += U) {
+    float v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) v[i] = w[min(p + i, P.parts - 1) * pf + P.rows * D + P.rows + row];
+#pragma unroll
+    for (int i = 0; i < U; ++i) mx = fmaxf(mx, v[i]);
+  }
   const float shift = neg_shift(mx);
   float den = 0.f;
   f32x4_t y = {};
-  for (int p = 0; p < P.parts; ++p) {
-    const float* x = w + p * pf;
-    const float f = __builtin_amdgcn_exp2f(x[P.rows * D + P.rows + row] + shift);
-    const f32x4_t t = *(const f32x4_t*)(x + row * D + c);
-    den += f * x[P.rows * D + row];
+  for (int p = 0; p < P.parts; p += U) {
+    f32x4_t v[U];
+    float f[U], s[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] += f * t[e];
+    for (int i = 0; i < U; ++i) {
+      const float* x = w + min(p + i, P.parts - 1) * pf;
+      v[i] = *(const f32x4_t*)(x + row * D + c);
+      f[i] = x[P.rows * D + P.rows + row];
+      s[i] = x[P.rows * D + row];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (p + i >= P.parts) break;
+      const float a = __builtin_amdgcn_exp2f(f[i] + shift);
+      den += a * s[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += a * v[i][e];
+    }
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;
   *(uint2*)(P.o + ((int64_t)z * P.Lq + qi) * P.ldo + h * D + c) =
@@ -497,14 +997,17 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
   return hipGetLastError();
 }
 
-// Work-groups that share one list: enough for two per CU of the chip.
+// Work-groups that share one list, so that the launch fills the chip's 256 CUs, of
+// at least MIN_PART entries each.  (By the shape alone: the workspace's size does
+// not depend on the device.)
+constexpr int MIN_PART = 4;
 int sparse_parts(const dit_sparse_shape& s) {
   const int64_t items = (int64_t)s.batch * s.heads * blocks_of(s.Lq, QBLK);
   if (items == 0) return 1;
-  const int64_t p = 512 / items;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(p, s.topk));
+  const int64_t p = 256 / items;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(p, s.topk / MIN_PART));
 }
-int sparse_rows(const dit_sparse_shape& s) { return std::min(QBLK, (s.Lq + 31) / 32 * 32); }
+int sparse_rows(const dit_sparse_shape& s) { return std::min(QBLK, (s.Lq + 15) / 16 * 16); }
 
 size_t attention_sparse_ws_bytes(const dit_sparse_shape& s) {
   const int parts = sparse_parts(s);
@@ -512,9 +1015,11 @@ size_t attention_sparse_ws_bytes(const dit_sparse_shape& s) {
   return (size_t)s.batch * s.heads * blocks_of(s.Lq, QBLK) * parts * piece_floats(sparse_rows(s)) * sizeof(float);
 }
 
+constexpr int LONG_LIST = 16;  // entries from which the pipelined kernel is the faster one
+
 hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                    const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, bool bounded,
-                                   void* ws, hipStream_t st) {
+                                   void* ws, hipStream_t st, int n_cu) {
   SparseArgs P{};
   P.q = (const bf16_t*)q; P.ldq = ldq; P.k = (const bf16_t*)k; P.ldk = ldk;
   P.v = (const bf16_t*)v; P.ldv = ldv; P.o = (bf16_t*)o; P.ldo = ldo;
@@ -528,8 +1033,15 @@ hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int
   P.rows = sparse_rows(s);
   P.ws = (float*)ws;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
-  hipLaunchKernelGGL((bounded ? attn_sparse_kernel<true> : attn_sparse_kernel<false>), dim3(P.items * P.parts), dim3(256),
-                     0, st, P);
+  const int64_t groups = (int64_t)P.items * P.parts;
+  const bool two = s.Lq > 32 && groups <= n_cu;
+  void (*fn)(SparseArgs);
+  if (s.Lq <= 16) fn = bounded ? attn_few_kernel<true, 1> : attn_few_kernel<false, 1>;
+  else if (s.Lq <= 32) fn = bounded ? attn_few_kernel<true, 2> : attn_few_kernel<false, 2>;
+  else if (two) fn = bounded ? attn_sparse_kernel<true, 2> : attn_sparse_kernel<false, 2>;
+  else if (bounded && s.topk >= LONG_LIST) fn = attn_sparse_long_kernel;
+  else fn = bounded ? attn_sparse_kernel<true, 1> : attn_sparse_kernel<false, 1>;
+  hipLaunchKernelGGL(fn, dim3((uint32_t)groups), dim3(two ? 512 : 256), 0, st, P);
   if (P.parts > 1)
     hipLaunchKernelGGL(sparse_combine_kernel, dim3(P.items, (P.rows + 7) / 8), dim3(256), 0, st, P);
   return hipGetLastError();

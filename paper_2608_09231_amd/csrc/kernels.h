@@ -124,7 +124,7 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
 size_t attention_sparse_ws_bytes(const dit_sparse_shape& s);
 hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                    const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, bool bounded,
-                                   void* ws, hipStream_t st);
+                                   void* ws, hipStream_t st, int n_cu);
 // Status and message of a failed component call (dit_cache_last_error(NULL)).
 dit_status component_fail(dit_status st, const char* msg) noexcept;
 

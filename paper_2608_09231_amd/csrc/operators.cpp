@@ -153,7 +153,8 @@ dit_status dit_attention_sparse_bf16(const dit_sparse_shape* s, const void* q, i
   if (dit::attention_sparse_ws_bytes(*s) && (!ws || !aligned(ws, 16)))
     return component_fail(DIT_EINVAL, "needs a 16-byte aligned workspace");
   return launched(dit::launch_attention_sparse(*s, q, ldq, k, ldk, v, ldv, o, ldo, idx,
-                                               (flags & DIT_ATTN_BOUNDED_LOGITS) != 0, ws, (hipStream_t)hip_stream));
+                                               (flags & DIT_ATTN_BOUNDED_LOGITS) != 0, ws, (hipStream_t)hip_stream,
+                                               compute_units()));
 }
 
 }  // extern "C"
