@@ -29,21 +29,37 @@ __device__ __forceinline__ int keys_of(const int32_t* klen, int z, int Lk) {
 
 // Means of the rows of one block and head, float64: a bf16 has 8 bits, so these
 // sums are exact for any sane range, whatever their order, and the choice of
-// blocks does not hang on rounding.  256 threads: 16 rows at a time, 8 columns
-// a thread.  Rows past the sequence's keys do not count.
+// blocks does not hang on rounding.  256 threads: 16 rows at a time, 8 columns a
+// thread, all loads in flight together.  One launch for the query blocks and the
+// key blocks behind them.  Rows past the sequence's keys do not count.
+//
+// Means are laid out in groups of 16 blocks as the score products read them:
+// lane (b, lq) of a wave holds d = 8 t + 2 lq + e of block b for step 2 t + e, one
+// 16-byte load per t that is contiguous over the wave.  Work-groups run over the
+// heads first, so that those in flight together read whole rows; where 8 divides
+// the heads, a head's blocks then share an XCD, whose L2 puts the lines of their
+// 16-byte pieces together (the rows pass it by).  Bound by the copy rate: 32760
+// tokens, 40 heads (674 MB) 127 us, 5.3 TB/s; rows through L2 139 us, blocks first 154 us.
+__host__ __device__ __forceinline__ int64_t mean_doubles(int blocks) { return (int64_t)((blocks + 15) / 16) * 16 * D; }
+struct MeanArgs {
+  const bf16_t* x[2]; int64_t ld[2];
+  double* out[2];
+  int L[2], heads[2], blocks[2];
+  int queries, total;  // work-groups (block, head, sequence): of queries, of both
+  const int32_t* klen;
+};
 template <int BLK>
-__global__ __launch_bounds__(256) void block_mean_kernel(const bf16_t* __restrict__ x, int64_t ldx,
-                                                         double* __restrict__ out, int L, const int32_t* klen) {
-  __shared__ double part[16][D];
-  const int blk = blockIdx.x, h = blockIdx.y, z = blockIdx.z, nb = gridDim.x, H = gridDim.y;
-  const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-  const int n = min(keys_of(klen, z, L) - blk * BLK, BLK);
-  const bf16_t* p = x + ((int64_t)z * L + (int64_t)blk * BLK) * ldx + h * D + 8 * c;
+__device__ __forceinline__ void block_mean(const MeanArgs& P, int kind, int unit, double (&part)[16][D]) {
+  const int H = P.heads[kind], h = unit % H, bz = unit / H, z = bz / P.blocks[kind], blk = bz - z * P.blocks[kind];
+  const int tid = threadIdx.x, c = tid & 15, r0 = tid >> 4, L = P.L[kind];
+  const int n = min((kind ? keys_of(P.klen, z, L) : L) - blk * BLK, BLK);
+  const int64_t ld = P.ld[kind];
+  const bf16_t* p = P.x[kind] + ((int64_t)z * L + (int64_t)blk * BLK) * ld + h * D + 8 * c;
   uint4 u[BLK / 16];
 #pragma unroll
   for (int i = 0; i < BLK / 16; ++i) {
     const int r = r0 + 16 * i;
-    u[i] = r < n ? *(const uint4*)(p + (int64_t)r * ldx) : make_uint4(0, 0, 0, 0);
+    u[i] = r < n ? ld_stream(p + (int64_t)r * ld) : make_uint4(0, 0, 0, 0);
   }
   double s[8] = {};
 #pragma unroll
@@ -56,12 +72,19 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const bf16_t* __restric
 #pragma unroll
   for (int e = 0; e < 8; ++e) part[r0][8 * c + e] = s[e];
   __syncthreads();
-  if (threadIdx.x < D) {
+  if (tid < D) {
     double t = 0.;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += part[i][threadIdx.x];
-    out[(((int64_t)z * H + h) * nb + blk) * D + threadIdx.x] = t / (double)max(n, 1);
+    for (int i = 0; i < 16; ++i) t += part[i][tid];
+    double* o = P.out[kind] + (z * H + h) * mean_doubles(P.blocks[kind]) + (blk >> 4) * 16 * D;
+    o[(tid >> 3) * 128 + (((tid >> 1) & 3) * 16 + (blk & 15)) * 2 + (tid & 1)] = t / (double)max(n, 1);
   }
+}
+__global__ __launch_bounds__(256) void block_mean_kernel(MeanArgs P) {
+  __shared__ double part[16][D];
+  const int unit = blockIdx.x;
+  if (unit < P.queries) block_mean<QBLK>(P, 0, unit, part);
+  else block_mean<KBLK>(P, 1, unit - P.queries, part);
 }
 
 // Order-preserving integer of a score: NaN counts as -inf, and no score gives 0
@@ -72,8 +95,9 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return u >> 63 ? ~u : u | (1ull << 63);
 }
 
-// Keys of 16 NI query blocks x 64 key blocks per wave on f64 MFMAs (16x16x4; lane
-// (lr, lq) holds d = 16 t + 4 lq + e of its row for step 4 t + e).
+typedef double f64x2_t __attribute__((ext_vector_type(2)));
+
+// Keys of 16 NI query blocks x 64 key blocks per wave on f64 MFMAs.
 template <int NI>
 __global__ __launch_bounds__(256) void block_score_kernel(const double* __restrict__ qm, const double* __restrict__ km,
                                                           uint64_t* __restrict__ keys, int nqb, int nkb, int heads,
@@ -86,20 +110,21 @@ __global__ __launch_bounds__(256) void block_score_kernel(const double* __restri
   const double* qp[NI];
   const double* kp[4];
 #pragma unroll
-  for (int i = 0; i < NI; ++i) qp[i] = qm + ((int64_t)hz * nqb + min(q0 + 16 * i + lr, nqb - 1)) * D + 4 * lq;
+  for (int i = 0; i < NI; ++i) qp[i] = qm + hz * mean_doubles(nqb) + min(q0 / 16 + i, (nqb - 1) / 16) * 16 * D + 2 * lane;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    kp[j] = km + (((int64_t)z * kv_heads + h / (heads / kv_heads)) * nkb + min(k0 + 16 * j + lr, nkb - 1)) * D + 4 * lq;
+    kp[j] = km + ((int64_t)z * kv_heads + h / (heads / kv_heads)) * mean_doubles(nkb) +
+            min(k0 / 16 + j, (nkb - 1) / 16) * 16 * D + 2 * lane;
   f64x4_t acc[NI][4] = {};
-#pragma unroll 2
-  for (int t = 0; t < D / 16; ++t) {
-    f64x4_t a[NI], b[4];
+#pragma unroll 4
+  for (int t = 0; t < D / 8; ++t) {
+    f64x2_t a[NI], b[4];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) a[i] = *(const f64x4_t*)(qp[i] + 16 * t);
+    for (int i = 0; i < NI; ++i) a[i] = *(const f64x2_t*)(qp[i] + 128 * t);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = *(const f64x4_t*)(kp[j] + 16 * t);
+    for (int j = 0; j < 4; ++j) b[j] = *(const f64x2_t*)(kp[j] + 128 * t);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -122,37 +147,28 @@ __global__ __launch_bounds__(256) void block_score_kernel(const double* __restri
 #endif
 }
 
-// The topk largest keys of each row, in the order of their blocks; equal keys go to
-// the lowest block.  A work-group of NW waves per row, R keys a lane.  The
-// threshold is found bit by bit from the top: a bit stays set while at least
-// topk keys reach it, and the search ends as soon as exactly topk do.
+// The topk largest keys of a row, in the order of their blocks; equal keys go to the
+// lowest block.  NW waves, R keys a lane (wave w holds blocks 64 R w + 64 r + lane).
+// The threshold is found bit by bit from the top: a bit stays set while at least
+// topk keys reach it, and the search ends as soon as exactly topk do.  red: 2 NW
+// ints of LDS (NW > 1).
 template <int NW, int R>
-__global__ __launch_bounds__(64 * NW) void block_topk_kernel(const uint64_t* __restrict__ keys, int32_t* __restrict__ idx,
-                                                             int nkb, int topk) {
-  __shared__ int red[2][NW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = blockIdx.x;
-  uint64_t key[R];  // wave w holds keys w 64 R ..: block index = base + 64 r + lane
+__device__ __forceinline__ void topk_row(const uint64_t (&key)[R], int32_t* __restrict__ o, int topk, int* red) {
+  const int tid = threadIdx.x % (64 * NW), lane = tid & 63, wave = tid >> 6;
   const int base = wave * 64 * R;
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int j = base + 64 * r + lane;
-    key[r] = j < nkb ? keys[row * nkb + j] : 0;
-  }
   int flip = 0;
-  // sum over the work-group of a wave-uniform count; `before`: that of the waves before this one
+  // sum over the waves of a wave-uniform count; `before`: that of the waves before this one
   auto total = [&](int c, int& before) {
+    before = 0;
     if constexpr (NW == 1) {
-      before = 0;
       return c;
     } else {
-      if (lane == 0) red[flip][wave] = c;
+      if (lane == 0) red[flip * NW + wave] = c;
       __syncthreads();
       int t = 0;
-      before = 0;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const int x = red[flip][w];
+        const int x = red[flip * NW + w];
         if (w < wave) before += x;
         t += x;
       }
@@ -166,15 +182,54 @@ __global__ __launch_bounds__(64 * NW) void block_topk_kernel(const uint64_t* __r
     for (int r = 0; r < R; ++r) c += __popcll(__ballot(key[r] >= t));
     return total(c, b);
   };
-  const int want = min(topk, count(1));
+  auto count_high = [&](uint32_t t) {  // keys whose upper half is >= t
+    int c = 0, b;
+#pragma unroll
+    for (int r = 0; r < R; ++r) c += __popcll(__ballot((uint32_t)(key[r] >> 32) >= t));
+    return total(c, b);
+  };
+  // (every key of a block is at least 2^32: that of -inf is 0x000fffffffffffff)
+  const int have = count_high(1), want = min(topk, have);
   uint64_t T = 1;
-  bool exact = false;
-  if (want > 0) {
-    for (int b = 63; b >= 0; --b) {
-      const uint64_t cand = (T & ~1ull) | (1ull << b);
-      const int c = count(cand);
-      if (c >= want) T = cand;
+  bool exact = want == have;  // every block that there is
+  if (want > 0 && !exact) {
+    // on the upper halves first, from the highest bit in which they differ
+    uint32_t t = 0;
+    int b = 31;
+    if constexpr (NW == 1) {
+      uint32_t hi = 0, lo = ~0u;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const uint32_t x = (uint32_t)(key[r] >> 32);
+        hi = max(hi, x);
+        lo = min(lo, x ? x : ~0u);
+      }
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+      }
+      hi = __builtin_amdgcn_readfirstlane(hi);
+      lo = __builtin_amdgcn_readfirstlane(lo);
+      b = hi == lo ? -1 : 31 - __builtin_clz(hi ^ lo);
+      t = b < 0 ? hi : b == 31 ? 0 : hi & (~0u << (b + 1));
+    }
+#pragma unroll 1
+    for (; b >= 0; --b) {
+      const uint32_t cand = t | (1u << b);
+      const int c = count_high(cand);
+      if (c >= want) t = cand;
       if (c == want) { exact = true; break; }
+    }
+    T = (uint64_t)t << 32;
+    if (!exact) {
+#pragma unroll 1
+      for (b = 31; b >= 0; --b) {
+        const uint64_t cand = T | (1ull << b);
+        const int c = count(cand);
+        if (c >= want) T = cand;
+        if (c == want) { exact = true; break; }
+      }
     }
   }
   // keys above T, and of those equal to it the first `ties`
@@ -204,13 +259,146 @@ __global__ __launch_bounds__(64 * NW) void block_topk_kernel(const uint64_t* __r
   }
   int at;
   total(mine, at);
-  int32_t* o = idx + row * topk;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (sel[r] >> lane & 1) o[at + __popcll(sel[r] & below)] = base + 64 * r + lane;
     at += __popcll(sel[r]);
   }
   for (int j = want + tid; j < topk; j += 64 * NW) o[j] = -1;
+}
+
+// Scores and choice in one for at most 64 R key blocks: 16 query blocks of a head, their
+// means in registers, their keys in LDS.  Four waves take 16 key blocks in turn
+// (f64 16x16x4 MFMAs, the next block's means on their way), then four rows each.
+template <int R>
+__global__ __launch_bounds__(256, R == 16 ? 1 : 2) void block_select_kernel(const double* __restrict__ qm, const double* __restrict__ km,
+                                                              int32_t* __restrict__ idx, int nqb, int nkb, int heads,
+                                                              int kv_heads, int Lk, int first, int topk,
+                                                              const int32_t* klen) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ uint64_t keys[16][64 * R + 2];
+  const int hz = blockIdx.y, z = hz / heads, h = hz - z * heads;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
+  const int q0 = blockIdx.x * 16;
+  const int nvalid = (keys_of(klen, z, Lk) + KBLK - 1) / KBLK;
+  const double* qp = qm + hz * mean_doubles(nqb) + (int64_t)blockIdx.x * 16 * D + 2 * lane;
+  const double* kh = km + ((int64_t)z * kv_heads + h / (heads / kv_heads)) * mean_doubles(nkb) + 2 * lane;
+  f64x2_t a[D / 8], b[2][D / 8];
+#pragma unroll
+  for (int t = 0; t < D / 8; ++t) a[t] = *(const f64x2_t*)(qp + 128 * t);
+  auto load = [&](int k0, f64x2_t (&x)[D / 8]) {
+    const double* p = kh + min(k0 >> 4, (nkb - 1) >> 4) * 16 * D;
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) x[t] = *(const f64x2_t*)(p + 128 * t);
+  };
+  auto block = [&](int k0, const f64x2_t (&x)[D / 8]) {
+    f64x4_t s = {}, u = {};  // two chains
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) {
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(a[t][0], x[t][0], s, 0, 0, 0);
+      u = __builtin_amdgcn_mfma_f64_16x16x4f64(a[t][1], x[t][1], u, 0, 0, 0);
+    }
+    const int k = k0 + lr;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)  // f64 accumulators: row 4 r + lq
+      keys[4 * r + lq][k] = k >= nvalid ? 0 : k < first ? ~0ull : score_key(s[r] + u[r]);
+  };
+  load(16 * wave, b[0]);
+  for (int k0 = 16 * wave; k0 < 64 * R; k0 += 128) {
+    load(k0 + 64, b[1]);
+    __builtin_amdgcn_sched_barrier(0);  // the loads stay ahead of the products
+    block(k0, b[0]);
+    if constexpr (R > 1) {
+      load(k0 + 128, b[0]);
+      __builtin_amdgcn_sched_barrier(0);
+      block(k0 + 64, b[1]);
+    }
+  }
+  __syncthreads();
+  // The wave's four rows in step, on the upper halves of their keys: one row's chain
+  // of counts would leave the wave waiting.  (A bit above the highest in which a row's keys
+  // differ is set in all of them or in none: trying it changes nothing.)
+  uint32_t hi[4][R], t[4], top[4], low[4], differ = 0;
+  int want[4];
+  bool exact[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    top[i] = 0;
+    low[i] = ~0u;
+    int have = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      hi[i][r] = (uint32_t)(keys[4 * wave + i][64 * r + lane] >> 32);
+      have += __popcll(__ballot(hi[i][r] != 0));
+      top[i] = max(top[i], hi[i][r]);
+      low[i] = min(low[i], hi[i][r] ? hi[i][r] : ~0u);
+    }
+    want[i] = min(topk, have);
+    exact[i] = want[i] == have;  // every block that there is
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], o, 64));
+      low[i] = min(low[i], (uint32_t)__shfl_xor((int)low[i], o, 64));
+    }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = __builtin_amdgcn_readfirstlane(top[i]), y = __builtin_amdgcn_readfirstlane(low[i]);
+    const uint32_t d = exact[i] ? 0 : x ^ y;
+    // bits that all of the row's keys share
+    t[i] = exact[i] ? 1 : d == 0 ? x : x & ~(~0u >> __builtin_clz(d));
+    differ |= d;
+  }
+#pragma unroll 1
+  for (int bit = differ ? 31 - __builtin_clz(differ) : -1; bit >= 0; --bit) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t cand = t[i] | (1u << bit);
+      int c = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) c += __popcll(__ballot(hi[i][r] >= cand));
+      if (!exact[i] && c >= want[i]) { t[i] = cand; exact[i] = c == want[i]; }
+    }
+    if (exact[0] && exact[1] && exact[2] && exact[3]) break;
+  }
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int q = q0 + 4 * wave + i;
+    if (q >= nqb) break;
+    int32_t* o = idx + ((int64_t)hz * nqb + q) * topk;
+    if (!exact[i]) {  // upper halves that are equal at the threshold
+      uint64_t key[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) key[r] = keys[4 * wave + i][64 * r + lane];
+      topk_row<1, R>(key, o, topk, nullptr);
+      continue;
+    }
+    int at = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint64_t sel = __ballot(hi[i][r] >= t[i]);
+      if (sel >> lane & 1) o[at + __popcll(sel & below)] = 64 * r + lane;
+      at += __popcll(sel);
+    }
+    for (int j = want[i] + lane; j < topk; j += 64) o[j] = -1;
+  }
+#endif
+}
+
+// Rows of more key blocks, from keys in memory: a work-group of NW waves per row.
+template <int NW, int R>
+__global__ __launch_bounds__(64 * NW) void block_topk_kernel(const uint64_t* __restrict__ keys, int32_t* __restrict__ idx,
+                                                             int nkb, int topk) {
+  __shared__ int red[2 * NW];
+  const int64_t row = blockIdx.x;
+  uint64_t key[R];
+  const int base = (threadIdx.x >> 6) * 64 * R + (threadIdx.x & 63);
+#pragma unroll
+  for (int r = 0; r < R; ++r) key[r] = base + 64 * r < nkb ? keys[row * nkb + base + 64 * r] : 0;
+  topk_row<NW, R>(key, idx + row * topk, topk, red);
 }
 
 // ---------------------------------------------------------------- attention
@@ -962,10 +1150,13 @@ int blocks_of(int n, int b) { return n / b + (n % b != 0); }
 
 }  // namespace
 
-// Means of the query blocks and of the key blocks (f64), then one key per pair.
+// Key blocks up to which scores and choice are one kernel, whose LDS holds the keys.
+constexpr int SELECT_BLOCKS = 1024;
+
+// Means of the query blocks and of the key blocks (f64), then, past SELECT_BLOCKS, one key per pair.
 size_t select_blocks_ws_bytes(const dit_sparse_shape& s) {
   const size_t nqb = blocks_of(s.Lq, QBLK), nkb = blocks_of(s.Lk, KBLK), b = s.batch;
-  return 8 * (b * s.heads * nqb * D + b * s.kv_heads * nkb * D + b * s.heads * nqb * nkb);
+  return 8 * (b * s.heads * mean_doubles((int)nqb) + b * s.kv_heads * mean_doubles((int)nkb) + (nkb > SELECT_BLOCKS ? b * s.heads * nqb * nkb : 0));
 }
 
 hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
@@ -974,26 +1165,38 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
   const int64_t rows = (int64_t)s.batch * s.heads * nqb;
   if (rows == 0) return hipSuccess;
   double* qm = (double*)ws;
-  double* km = qm + rows * D;
-  uint64_t* keys = (uint64_t*)(km + (int64_t)s.batch * s.kv_heads * nkb * D);
-  if (nkb > 0) {
-    hipLaunchKernelGGL(block_mean_kernel<QBLK>, dim3(nqb, s.heads, s.batch), dim3(256), 0, st, (const bf16_t*)q, ldq, qm,
-                       s.Lq, (const int32_t*)nullptr);
-    hipLaunchKernelGGL(block_mean_kernel<KBLK>, dim3(nkb, s.kv_heads, s.batch), dim3(256), 0, st, (const bf16_t*)k, ldk,
-                       km, s.Lk, s.klen);
-    hipLaunchKernelGGL(block_score_kernel<2>, dim3((nkb + 63) / 64, (nqb + 127) / 128, s.batch * s.heads), dim3(256), 0,
-                       st, qm, km, keys, nqb, nkb, s.heads, s.kv_heads, s.Lk, first, s.klen);
+  double* km = qm + (int64_t)s.batch * s.heads * mean_doubles(nqb);
+  uint64_t* keys = (uint64_t*)(km + (int64_t)s.batch * s.kv_heads * mean_doubles(nkb));
+  if (nkb == 0) {  // lists of -1
+    hipLaunchKernelGGL((block_topk_kernel<1, 1>), dim3((uint32_t)rows), dim3(64), 0, st, keys, idx, 0, s.topk);
+    return hipGetLastError();
   }
-  const dim3 grid((uint32_t)rows);
-#define DIT_TOPK(NW, R) \
-  hipLaunchKernelGGL((block_topk_kernel<NW, R>), grid, dim3(64 * NW), 0, st, keys, idx, nkb, s.topk)
-  if (nkb <= 64) DIT_TOPK(1, 1);
-  else if (nkb <= 256) DIT_TOPK(1, 4);
-  else if (nkb <= 512) DIT_TOPK(1, 8);
-  else if (nkb <= 1024) DIT_TOPK(1, 16);
-  else if (nkb <= 4096) DIT_TOPK(4, 16);
-  else DIT_TOPK(16, 16);
-#undef DIT_TOPK
+  MeanArgs a{};
+  a.x[0] = (const bf16_t*)q; a.ld[0] = ldq; a.out[0] = qm; a.L[0] = s.Lq; a.heads[0] = s.heads; a.blocks[0] = nqb;
+  a.x[1] = (const bf16_t*)k; a.ld[1] = ldk; a.out[1] = km; a.L[1] = s.Lk; a.heads[1] = s.kv_heads; a.blocks[1] = nkb;
+  a.klen = s.klen;
+  const int64_t total = rows + (int64_t)s.batch * s.kv_heads * nkb;
+  if (total > 0x7fffffff) return hipErrorInvalidValue;
+  a.queries = (int)rows;
+  a.total = (int)total;
+  hipLaunchKernelGGL(block_mean_kernel, dim3(a.total), dim3(256), 0, st, a);
+  if (nkb <= SELECT_BLOCKS) {
+#define DIT_SELECT(R)                                                                                                  \
+  hipLaunchKernelGGL(block_select_kernel<R>, dim3((nqb + 15) / 16, s.batch * s.heads), dim3(256), 0, st, qm, km, idx, nqb, \
+                     nkb, s.heads, s.kv_heads, s.Lk, first, s.topk, s.klen)
+    if (nkb <= 64) DIT_SELECT(1);
+    else if (nkb <= 256) DIT_SELECT(4);
+    else if (nkb <= 512) DIT_SELECT(8);
+    else DIT_SELECT(16);
+#undef DIT_SELECT
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(block_score_kernel<2>, dim3((nkb + 63) / 64, (nqb + 127) / 128, s.batch * s.heads), dim3(256), 0, st,
+                     qm, km, keys, nqb, nkb, s.heads, s.kv_heads, s.Lk, first, s.klen);
+  if (nkb <= 4096)
+    hipLaunchKernelGGL((block_topk_kernel<4, 16>), dim3((uint32_t)rows), dim3(256), 0, st, keys, idx, nkb, s.topk);
+  else
+    hipLaunchKernelGGL((block_topk_kernel<16, 16>), dim3((uint32_t)rows), dim3(1024), 0, st, keys, idx, nkb, s.topk);
   return hipGetLastError();
 }
 

@@ -100,9 +100,10 @@ def test_sparse_calls_refuse_their_own():
     assert select(s=big) == binding.DIT_ESHAPE
     many = binding.sparse_shape(**dict(SHAPE, batch=20000))
     assert select(s=many) == binding.DIT_ESHAPE
-    assert lib.dit_attention_sparse_ws_bytes(C.byref(s)) > 0
-    assert attend(v=None) == attend(o=None) == attend(flags=2) == attend(ws=None) == attend(ws=FAKE + 4) == \
-        binding.DIT_EINVAL
+    assert attend(v=None) == attend(o=None) == attend(flags=2) == binding.DIT_EINVAL
+    split = binding.sparse_shape(**dict(SHAPE, topk=64))      # few lists that are shared
+    assert lib.dit_attention_sparse_ws_bytes(C.byref(split)) > 0
+    assert attend(s=split, ws=None) == attend(s=split, ws=FAKE + 4) == binding.DIT_EINVAL
     assert attend(ldv=128) == attend(ldo=256) == attend(ldk=1 << 22) == binding.DIT_ESHAPE
     assert lib.dit_select_blocks_bf16(None, FAKE, 512, FAKE, 256, 0, FAKE, FAKE, None) == binding.DIT_EINVAL
     assert lib.dit_attention_sparse_bf16(None, FAKE, 512, FAKE, 256, FAKE, 256, FAKE, 512, FAKE, 0, FAKE,
@@ -111,7 +112,11 @@ def test_sparse_calls_refuse_their_own():
 
 
 def test_select_workspace_holds_means_and_keys():
-    assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * (2 * 4 * 3 * 128 + 2 * 2 * 16 * 128 + 2 * 4 * 3 * 16)
+    means = 2 * 4 * 16 * 128 + 2 * 2 * 16 * 128      # in groups of 16 blocks
+    assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * means
+    nkb = 1025                                       # keys leave LDS
+    means += 2 * 2 * (1040 - 16) * 128
+    assert binding.select_blocks_ws_bytes(**dict(SHAPE, Lk=64 * nkb)) == 8 * (means + 2 * 4 * 3 * nkb)
 
 
 def test_sparse_workspace_is_for_few_lists_only():
