@@ -147,6 +147,13 @@ __global__ __launch_bounds__(256) void block_score_kernel(const double* __restri
 #endif
 }
 
+// Largest of a wave's values, the same in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max_over<16>(v);
+  return max(max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16)),
+             max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
+}
+
 // The topk largest keys of a row, in the order of their blocks; equal keys go to the
 // lowest block.  NW waves, R keys a lane (wave w holds blocks 64 R w + 64 r + lane).
 // The threshold is found bit by bit from the top: a bit stays set while at least
@@ -204,13 +211,8 @@ __device__ __forceinline__ void topk_row(const uint64_t (&key)[R], int32_t* __re
         hi = max(hi, x);
         lo = min(lo, x ? x : ~0u);
       }
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
-      }
-      hi = __builtin_amdgcn_readfirstlane(hi);
-      lo = __builtin_amdgcn_readfirstlane(lo);
+      hi = wave_max(hi);
+      lo = ~wave_max(~lo);
       b = hi == lo ? -1 : 31 - __builtin_clz(hi ^ lo);
       t = b < 0 ? hi : b == 31 ? 0 : hi & (~0u << (b + 1));
     }
@@ -268,10 +270,10 @@ __device__ __forceinline__ void topk_row(const uint64_t (&key)[R], int32_t* __re
 }
 
 // Scores and choice in one for at most 64 R key blocks: 16 query blocks of a head, their
-// means in registers, their keys in LDS.  Four waves take 16 key blocks in turn
-// (f64 16x16x4 MFMAs, the next block's means on their way), then four rows each.
-template <int R>
-__global__ __launch_bounds__(256, R == 16 ? 1 : 2) void block_select_kernel(const double* __restrict__ qm, const double* __restrict__ km,
+// means in registers, their keys in LDS.  NW waves take 16 key blocks in turn (f64
+// 16x16x4 MFMAs), then 16 / NW rows each.
+template <int R, int NW>
+__global__ __launch_bounds__(64 * NW, R == 16 && NW == 8 ? 2 : 4) void block_select_kernel(const double* __restrict__ qm, const double* __restrict__ km,
                                                               int32_t* __restrict__ idx, int nqb, int nkb, int heads,
                                                               int kv_heads, int Lk, int first, int topk,
                                                               const int32_t* klen) {
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(256, R == 16 ? 1 : 2) void block_select_kernel(cons
   const int nvalid = (keys_of(klen, z, Lk) + KBLK - 1) / KBLK;
   const double* qp = qm + hz * mean_doubles(nqb) + (int64_t)blockIdx.x * 16 * D + 2 * lane;
   const double* kh = km + ((int64_t)z * kv_heads + h / (heads / kv_heads)) * mean_doubles(nkb) + 2 * lane;
-  f64x2_t a[D / 8], b[2][D / 8];
+  f64x2_t a[D / 8], b[D / 8];
 #pragma unroll
   for (int t = 0; t < D / 8; ++t) a[t] = *(const f64x2_t*)(qp + 128 * t);
   auto load = [&](int k0, f64x2_t (&x)[D / 8]) {
@@ -303,32 +305,26 @@ __global__ __launch_bounds__(256, R == 16 ? 1 : 2) void block_select_kernel(cons
     for (int r = 0; r < 4; ++r)  // f64 accumulators: row 4 r + lq
       keys[4 * r + lq][k] = k >= nvalid ? 0 : k < first ? ~0ull : score_key(s[r] + u[r]);
   };
-  load(16 * wave, b[0]);
-  for (int k0 = 16 * wave; k0 < 64 * R; k0 += 128) {
-    load(k0 + 64, b[1]);
-    __builtin_amdgcn_sched_barrier(0);  // the loads stay ahead of the products
-    block(k0, b[0]);
-    if constexpr (R > 1) {
-      load(k0 + 128, b[0]);
-      __builtin_amdgcn_sched_barrier(0);
-      block(k0 + 64, b[1]);
-    }
+  for (int k0 = 16 * wave; k0 < 64 * R; k0 += 16 * NW) {
+    load(k0, b);
+    block(k0, b);
   }
   __syncthreads();
-  // The wave's four rows in step, on the upper halves of their keys: one row's chain
+  // The wave's rows in step, on the upper halves of their keys: one row's chain
   // of counts would leave the wave waiting.  (A bit above the highest in which a row's keys
   // differ is set in all of them or in none: trying it changes nothing.)
-  uint32_t hi[4][R], t[4], top[4], low[4], differ = 0;
-  int want[4];
-  bool exact[4];
+  constexpr int ROWS = 16 / NW;
+  uint32_t hi[ROWS][R], t[ROWS], top[ROWS], low[ROWS], differ = 0;
+  int want[ROWS];
+  bool exact[ROWS];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < ROWS; ++i) {
     top[i] = 0;
     low[i] = ~0u;
     int have = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      hi[i][r] = (uint32_t)(keys[4 * wave + i][64 * r + lane] >> 32);
+      hi[i][r] = (uint32_t)(keys[ROWS * wave + i][64 * r + lane] >> 32);
       have += __popcll(__ballot(hi[i][r] != 0));
       top[i] = max(top[i], hi[i][r]);
       low[i] = min(low[i], hi[i][r] ? hi[i][r] : ~0u);
@@ -337,15 +333,8 @@ __global__ __launch_bounds__(256, R == 16 ? 1 : 2) void block_select_kernel(cons
     exact[i] = want[i] == have;  // every block that there is
   }
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], o, 64));
-      low[i] = min(low[i], (uint32_t)__shfl_xor((int)low[i], o, 64));
-    }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t x = __builtin_amdgcn_readfirstlane(top[i]), y = __builtin_amdgcn_readfirstlane(low[i]);
+  for (int i = 0; i < ROWS; ++i) {
+    const uint32_t x = wave_max(top[i]), y = ~wave_max(~low[i]);
     const uint32_t d = exact[i] ? 0 : x ^ y;
     // bits that all of the row's keys share
     t[i] = exact[i] ? 1 : d == 0 ? x : x & ~(~0u >> __builtin_clz(d));
@@ -354,25 +343,28 @@ __global__ __launch_bounds__(256, R == 16 ? 1 : 2) void block_select_kernel(cons
 #pragma unroll 1
   for (int bit = differ ? 31 - __builtin_clz(differ) : -1; bit >= 0; --bit) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
       const uint32_t cand = t[i] | (1u << bit);
       int c = 0;
 #pragma unroll
       for (int r = 0; r < R; ++r) c += __popcll(__ballot(hi[i][r] >= cand));
       if (!exact[i] && c >= want[i]) { t[i] = cand; exact[i] = c == want[i]; }
     }
-    if (exact[0] && exact[1] && exact[2] && exact[3]) break;
+    bool all = true;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) all &= exact[i];
+    if (all) break;
   }
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int q = q0 + 4 * wave + i;
+  for (int i = 0; i < ROWS; ++i) {
+    const int q = q0 + ROWS * wave + i;
     if (q >= nqb) break;
     int32_t* o = idx + ((int64_t)hz * nqb + q) * topk;
     if (!exact[i]) {  // upper halves that are equal at the threshold
       uint64_t key[R];
 #pragma unroll
-      for (int r = 0; r < R; ++r) key[r] = keys[4 * wave + i][64 * r + lane];
+      for (int r = 0; r < R; ++r) key[r] = keys[ROWS * wave + i][64 * r + lane];
       topk_row<1, R>(key, o, topk, nullptr);
       continue;
     }
@@ -1160,7 +1152,7 @@ size_t select_blocks_ws_bytes(const dit_sparse_shape& s) {
 }
 
 hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
-                                int first, int32_t* idx, void* ws, hipStream_t st) {
+                                int first, int32_t* idx, void* ws, hipStream_t st, int n_cu) {
   const int nqb = blocks_of(s.Lq, QBLK), nkb = blocks_of(s.Lk, KBLK);
   const int64_t rows = (int64_t)s.batch * s.heads * nqb;
   if (rows == 0) return hipSuccess;
@@ -1181,9 +1173,14 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
   a.total = (int)total;
   hipLaunchKernelGGL(block_mean_kernel, dim3(a.total), dim3(256), 0, st, a);
   if (nkb <= SELECT_BLOCKS) {
-#define DIT_SELECT(R)                                                                                                  \
-  hipLaunchKernelGGL(block_select_kernel<R>, dim3((nqb + 15) / 16, s.batch * s.heads), dim3(256), 0, st, qm, km, idx, nqb, \
-                     nkb, s.heads, s.kv_heads, s.Lk, first, s.topk, s.klen)
+    // More waves a work-group where there is at most one per CU: 4608 tokens, 24 heads (72)
+    // 12.0 us with 16 waves, 14.0 with 8; 32760 tokens, 40 heads (640) 58.9 and 54.0.
+    const int64_t groups = (int64_t)((nqb + 15) / 16) * s.batch * s.heads;
+    const bool few = groups <= n_cu;
+#define DIT_SELECT(R)                                                                                                \
+  hipLaunchKernelGGL((few ? block_select_kernel<R, 16> : block_select_kernel<R, 8>),                                  \
+                     dim3((nqb + 15) / 16, s.batch * s.heads), dim3(few ? 1024 : 512), 0, st, qm, km, idx, nqb, nkb, \
+                     s.heads, s.kv_heads, s.Lk, first, s.topk, s.klen)
     if (nkb <= 64) DIT_SELECT(1);
     else if (nkb <= 256) DIT_SELECT(4);
     else if (nkb <= 512) DIT_SELECT(8);

@@ -120,7 +120,7 @@ hipError_t launch_quant_fp8(const void* x, bool bf16, int64_t ldx, void* q, int6
 hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu);
 size_t select_blocks_ws_bytes(const dit_sparse_shape& s);
 hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
-                                int first, int32_t* idx, void* ws, hipStream_t st);
+                                int first, int32_t* idx, void* ws, hipStream_t st, int n_cu);
 size_t attention_sparse_ws_bytes(const dit_sparse_shape& s);
 hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                    const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, bool bounded,

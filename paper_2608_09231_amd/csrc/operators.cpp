@@ -132,7 +132,7 @@ dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int6
   if (first < 0 || first > s->topk) return component_fail(DIT_EINVAL, "first must lie in [0, topk]");
   if (s->Lk > 16384 * DIT_SPARSE_KB || s->batch > 65535 || s->heads > 65535 || (int64_t)s->batch * s->heads > 65535)
     return component_fail(DIT_ESHAPE, "too many key blocks, sequences or heads");
-  return launched(dit::launch_select_blocks(*s, q, ldq, k, ldk, first, idx, ws, (hipStream_t)hip_stream));
+  return launched(dit::launch_select_blocks(*s, q, ldq, k, ldk, first, idx, ws, (hipStream_t)hip_stream, compute_units()));
 }
 
 size_t dit_attention_sparse_ws_bytes(const dit_sparse_shape* s) {
