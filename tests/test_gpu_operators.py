@@ -188,6 +188,58 @@ def test_gemm_sizes(M, N, K, out):
     check_gemm(M, N, K, out=out, pad=8 if (M + K) % 3 else 0, bias=(M % 4) > 0)
 
 
+# sizes whose tiles of 128 x 128 (510) and of 256 x 128 (160) fill the chip's CUs once
+@pytest.mark.parametrize("out", ["bf16", "f32", "gated"])
+@pytest.mark.parametrize("M,N,K", [(1920, 4352, 400), (1913, 4312, 1168), (512, 10240, 272), (500, 10232, 1168)])
+def test_gemm_sizes_of_one_round(M, N, K, out):
+    check_gemm(M, N, K, out=out, pad=8 if M % 8 else 0, bias=M % 8 == 0)
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "rms"])
+@pytest.mark.parametrize("M,N,K", [(1913, 4352, 656), (500, 10240, 400)])
+def test_gemm_fp8_output_of_one_round(M, N, K, act):
+    check_gemm(M, N, K, out="fp8", act=act, rms_cols=N if act == "rms" else 0, gelu_from=0 if act == "gelu" else None)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "gated", "fp8"])
+@pytest.mark.parametrize("M,N", [(1050, 128), (1030, 1152), (4200, 4224)])
+def test_gemm_rows_far_apart(M, N, out):
+    """Rows 4 MiB apart, so that offsets pass 32 bits in every operand: the bits of dense rows."""
+    torch = torch_cuda()
+    K, far = 272, 1 << 22
+    r = rng(M, N)
+    esize = {"bf16": 2, "gated": 2, "f32": 4, "fp8": 1}[out]
+    flags = {"bf16": 0, "f32": binding.EPI_F32, "fp8": binding.EPI_FP8, "gated": binding.EPI_GATED_RES}[out]
+    x = dev(torch, r.standard_normal((M, K)).astype(np.float32))
+    w = dev(torch, r.standard_normal((N, K)).astype(np.float32))
+    gate = dev(torch, r.standard_normal(N).astype(np.float32))
+    start = dev(torch, r.integers(0, 100, (M, N * esize)).astype(np.uint8))
+    res = []
+    for apart in (False, True):
+        bufs = []
+        for t in (x, w):
+            n = t.shape[0]
+            q = torch.empty(n, far if apart else K, dtype=torch.uint8, device="cuda")
+            s = torch.empty(n, binding.fp8_scale_ld(K), dtype=torch.uint8, device="cuda")
+            src = torch.empty(n, far // 4 if apart else K, device="cuda")
+            src[:, :K] = t
+            binding.quant_fp8(src, q, s, M=n, K=K)
+            torch.cuda.synchronize()
+            bufs += [q, s]
+        del src
+        C = torch.empty(M, far if apart else N * esize, dtype=torch.uint8, device="cuda")
+        C[:, :N * esize] = start
+        cs = torch.zeros(M, binding.fp8_scale_ld(N), dtype=torch.uint8, device="cuda")
+        binding.gemm_fp8(bufs[0], bufs[1], bufs[2], bufs[3], None,
+                         C.view({1: torch.uint8, 2: torch.int16, 4: torch.float32}[esize]), M=M, N=N, K=K, flags=flags,
+                         gate=gate if out == "gated" else None, c_scale=cs if out == "fp8" else None)
+        res.append([t.clone() for t in (bufs[0][:, :K], bufs[1][:, :3], bufs[2][:, :K], C[:, :N * esize], cs)])
+        del C, bufs, q
+    torch.cuda.empty_cache()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("act", ["none", "gelu", "silu", "rms"])
 @pytest.mark.parametrize("M,N,K", [(1, 128, 528), (19, 256, 400), (257, 1152, 272), (700, 7040, 1040), (4097, 4480, 272)])
 def test_gemm_fp8_output(M, N, K, act):
@@ -231,6 +283,21 @@ def test_gemm_nan_rows_stay_in_their_rows(M, N, out):
     assert (np.abs(got - y)[rest] <= tol[rest]).all()
     if out == "fp8":
         assert (scale[3] == 255).all()
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N", [(4, 128), (300, 2048), (1920, 4352), (4100, 4352)])
+def test_gemm_scale_of_255_is_nan(M, N, out):
+    """Also above finite values, in rows of either operand."""
+    K = 400
+    r = rng(M, N, 4)
+    a, w = operand(r, M, K), operand(r, N, K)
+    a[1][2, 1] = w[1][5, 3] = 255
+    _, _, got, y, tol = run_gemm(M, N, K, out=out, operands=(a, w), bias=False)
+    assert np.isnan(got[2]).all() and np.isnan(got[:, 5]).all()
+    rest = np.ones(y.shape, bool)
+    rest[2], rest[:, 5] = False, False
+    assert (np.abs(got - y)[rest] <= tol[rest]).all()
 
 
 def test_gemm_no_rows_or_columns():
@@ -286,6 +353,19 @@ def test_select_blocks(shape, first, pad):
     if shape["klen"]:   # rows past a sequence's keys may hold anything
         for z, n in enumerate(shape["klen"]):
             kb[z * shape["Lk"] + n:(z + 1) * shape["Lk"], :] = 0x7FC0
+    np.testing.assert_array_equal(run_select(torch, qb, kb, shape, first), ref.select(q, k, first=first, **shape))
+
+
+@pytest.mark.parametrize("Lk,topk", [(700, 3), (9000, 20), (21000, 40), (40000, 64)])
+@pytest.mark.parametrize("first", [0, 2])
+def test_select_blocks_of_many_heads(Lk, topk, first):
+    """More lists than the chip has CUs."""
+    torch = torch_cuda()
+    r = rng(Lk, 2)
+    shape = shape_of(131, Lk, 136, topk, kv_heads=1, batch=2, klen=[Lk, Lk - 333])
+    qb, q = tokens(r, 2 * 131, 136)
+    kb, k = tokens(r, 2 * Lk, 1)
+    kb[2 * Lk - 333:] = 0x7FC0
     np.testing.assert_array_equal(run_select(torch, qb, kb, shape, first), ref.select(q, k, first=first, **shape))
 
 
@@ -372,6 +452,87 @@ def test_sparse_attention(shape, bounded):
     y = check_attention(got, q, k, v, idx, shape)
     if shape["topk"] > 1:
         assert (got[:min(128, shape["Lq"]), :128] == 0).all() and (y[:min(128, shape["Lq"]), :128] == 0).all()
+
+
+@pytest.mark.parametrize("bounded", [False, True])
+@pytest.mark.parametrize("shape", [
+    shape_of(40, 1500, 90, 20, kv_heads=2, batch=3, klen=[1500, 0, 1025]), shape_of(130, 1100, 132, 17, kv_heads=4),
+    shape_of(97, 4000, 260, 16, kv_heads=1), shape_of(33, 900, 300, 70, kv_heads=3)])
+def test_sparse_attention_of_many_lists(shape, bounded):
+    """More lists than the chip has CUs, of 16 and more entries; every count of tiles from none on, blocks of
+    queries that leave waves without rows."""
+    torch = torch_cuda()
+    r = rng(shape["Lq"], shape["Lk"], shape["heads"])
+    G = shape["kv_heads"]
+    qb, q = tokens(r, shape["batch"] * shape["Lq"], shape["heads"])
+    kb, k = tokens(r, shape["batch"] * shape["Lk"], G)
+    vb, v = tokens(r, shape["batch"] * shape["Lk"], G, scale=2.0)
+    for z, n in enumerate(shape["klen"] or []):
+        kb[z * shape["Lk"] + n:(z + 1) * shape["Lk"], :] = 0x7FC0
+        vb[z * shape["Lk"] + n:(z + 1) * shape["Lk"], :] = 0x7F80
+    nqb, nkb = -(-shape["Lq"] // 128), -(-shape["Lk"] // 64)
+    idx = r.integers(0, nkb, (shape["batch"], shape["heads"], nqb, shape["topk"])).astype(np.int32)
+    kept = np.arange(shape["heads"]) % (shape["topk"] + 1)     # entries of a head's lists
+    idx[r.permuted(np.broadcast_to(np.arange(shape["topk"]), idx.shape), axis=3) >= kept[:, None, None]] = -1
+    got = run_attention(torch, qb, kb, vb, idx, shape, bounded)
+    check_attention(got, q, k, v, idx, shape)
+    assert (got[:, :128] == 0).all()
+
+
+@pytest.mark.parametrize("Lq", [16, 17, 20, 32])
+def test_sparse_attention_of_few_queries(Lq):
+    torch = torch_cuda()
+    r = rng(Lq, 41)
+    for heads, Lk, topk in ((2, 3000, 37), (200, 700, 5)):
+        shape = shape_of(Lq, Lk, heads, topk, kv_heads=2, batch=2, klen=[Lk, Lk - 90])
+        qb, q = tokens(r, 2 * Lq, heads)
+        kb, k = tokens(r, 2 * Lk, 2)
+        vb, v = tokens(r, 2 * Lk, 2)
+        kb[2 * Lk - 90:], vb[2 * Lk - 90:] = 0x7FC0, 0x7F80
+        idx = r.integers(-1, -(-Lk // 64), (2, heads, 1, topk)).astype(np.int32)
+        for bounded in (False, True):
+            check_attention(run_attention(torch, qb, kb, vb, idx, shape, bounded), q, k, v, idx, shape)
+
+
+@pytest.mark.parametrize("Lq,heads,topk", [(1, 2, 6), (40, 2, 6), (300, 100, 16)])
+def test_rows_far_apart(Lq, heads, topk):
+    """Rows of up to 8 MiB, so that offsets pass 32 bits in every operand: the bits of dense rows."""
+    torch = torch_cuda()
+    Lk, far = 650, (1 << 22) - 8
+    r = rng(Lq, 55)
+    rows = [dev(torch, tokens(r, n, g)[0]) for n, g in ((Lq, heads), (Lk, 2), (Lk, 2))]
+    shape = dict(Lq=Lq, Lk=Lk, heads=heads, topk=topk, kv_heads=2)
+    res = []
+    for apart in (False, True):
+        q, k, v = (torch.empty(t.shape[0], far if apart else t.shape[1], dtype=torch.int16, device="cuda") for t in rows)
+        for t, x in zip((q, k, v), rows):
+            t[:, :x.shape[1]] = x
+        idx = torch.empty(1, heads, -(-Lq // 128), topk, dtype=torch.int32, device="cuda")
+        o = torch.empty(Lq, far if apart else heads * 128, dtype=torch.int16, device="cuda")
+        binding.select_blocks_bf16(q, k, idx, **shape)
+        binding.attention_sparse_bf16(q, k, v, o, idx, flags=binding.ATTN_BOUNDED_LOGITS, **shape)
+        res.append((idx, o[:, :heads * 128].clone()))
+        del q, k, v, o, t
+    torch.cuda.empty_cache()
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
+
+
+def test_lengths_of_zero():
+    """No keys: lists of -1 and rows of zeros.  No queries, no sequences: nothing is written."""
+    torch = torch_cuda()
+    x = torch.full((200, 256), 0x7FC0, dtype=torch.int16, device="cuda")
+    for Lq, Lk, batch, klen in ((200, 0, 1, None), (100, 70, 2, [0, -3]), (0, 64, 1, None), (200, 64, 0, None)):
+        kl = None if klen is None else torch.tensor(klen, dtype=torch.int32, device="cuda")
+        shape = dict(Lq=Lq, Lk=Lk, heads=2, topk=3, batch=batch, klen=kl)
+        idx = torch.full((2, 2, 2, 3), 1, dtype=torch.int32, device="cuda")
+        o = torch.full((200, 256), 0x2A2A, dtype=torch.int16, device="cuda")
+        ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+        n = batch * 2 * -(-Lq // 128) * 3
+        binding.select_blocks_bf16(x, x, idx, ws=ws, **shape)
+        assert (idx.view(-1)[:n] == -1).all() and (idx.view(-1)[n:] == 1).all()
+        idx.fill_(0)
+        binding.attention_sparse_bf16(x, x, x, o, idx, ws=ws, **shape)
+        assert (o[:batch * Lq] == 0).all() and (o[batch * Lq:] == 0x2A2A).all()
 
 
 @pytest.mark.parametrize("Lq", [1, 200])
