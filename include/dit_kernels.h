@@ -138,7 +138,7 @@ dit_status dit_attention_bf16_noalloc(const void* q, int64_t ldq, const void* k,
  *   q      device e4m3 [M, K], row stride ldq bytes
  * Errors: DIT_EINVAL (null pointers, bad type, x or q not 16-byte or scale not
  * 4-byte aligned), DIT_ESHAPE (negative sizes, K % 16, a stride below the row
- * or, in bytes, no multiple of 16, lds), DIT_EHIP. */
+ * or, in bytes, no multiple of 16, lds, K above 2^30, M * ceil(K / 1024) above 2^26 - 4), DIT_EHIP. */
 dit_status dit_quant_fp8(const void* x, int32_t x_dtype, int64_t ldx, void* q, int64_t ldq, void* scale,
                          int64_t lds, int32_t M, int32_t K, void* hip_stream);
 
@@ -165,7 +165,8 @@ enum { DIT_EPI_FP8 = 8 };
  * row or no multiple of 8, rms_cols no multiple of 128 or above N, gelu_from < N
  * no multiple of 4, gap or gap_at no multiple of 4 or negative; with
  * DIT_EPI_FP8: N or gelu_from < N no multiple of 128, ldc no multiple of 16, a
- * gap; with rms_cols: N no multiple of 128), DIT_EHIP. */
+ * gap; with rms_cols: N no multiple of 128; ceil(M / 64) * ceil(N / 128) of 2^23
+ * or more), DIT_EHIP. */
 typedef struct dit_gemm_fp8_desc {
   const void* A; int64_t lda;
   const void* a_scale; int64_t ld_as;
@@ -209,8 +210,9 @@ typedef struct dit_sparse_shape {
  *   ws  device, dit_select_blocks_ws_bytes(s), 16-byte aligned
  * Errors: DIT_EINVAL (null pointers, alignment of 16 bytes, first outside [0,
  * topk]), DIT_ESHAPE (negative sizes; heads no multiple of kv_heads; topk < 1;
- * strides below the row or no multiple of 8; more than 16384 key blocks, 65535
- * sequences or heads, or 2^31 - 1 lists), DIT_EHIP. */
+ * strides below the row or no multiple of 8; more than 2^22 lists; more than
+ * 16384 key blocks a sequence, 65535 batch * heads, or 2^24 - 1 lists and key
+ * blocks of all key heads together), DIT_EHIP. */
 size_t dit_select_blocks_ws_bytes(const dit_sparse_shape* s);
 dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                   int32_t first, int32_t* idx, void* ws, void* hip_stream);
@@ -222,8 +224,8 @@ dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int6
  * and in the product), sums and outputs are f32 until the one rounding of o.
  *   ws  device, dit_attention_sparse_ws_bytes(s) (may be 0: then NULL will do),
  *       16-byte aligned
- * Errors: as dit_select_blocks_bf16 (without `first` and the limits of 16384 and
- * 65535), strides of 2^22 or more, bad flags. */
+ * Errors: as dit_select_blocks_bf16 (without `first` and the last three
+ * limits), strides of 2^22 or more, bad flags. */
 size_t dit_attention_sparse_ws_bytes(const dit_sparse_shape* s);
 dit_status dit_attention_sparse_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                      const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx,

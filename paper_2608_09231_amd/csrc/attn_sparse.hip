@@ -45,7 +45,7 @@ struct MeanArgs {
   const bf16_t* x[2]; int64_t ld[2];
   double* out[2];
   int L[2], heads[2], blocks[2];
-  int queries, total;  // work-groups (block, head, sequence): of queries, of both
+  int queries;  // work-groups (block, head, sequence) of queries; those of keys follow
   const int32_t* klen;
 };
 template <int BLK>
@@ -694,6 +694,7 @@ __global__ __launch_bounds__(256 * TP, 2) void attn_sparse_kernel(SparseArgs P) 
       m[g] = mn;
     }
   }
+  __builtin_amdgcn_s_waitcnt(0);  // no copy outlives its work-group
   if (active) store_rows(P, acc, l, m, unit, z, h, qb, 32 * wave, lr, lq);
 #endif
 }
@@ -1092,47 +1093,72 @@ __global__ __launch_bounds__(256, 2) void attn_sparse_long_kernel(SparseArgs P) 
 #endif
 }
 
-// Adds the pieces of an item in the order of its list and stores the normalised
-// output.  32 threads a row, 4 columns each.
+// Joins the pieces of an item's rows and stores the normalised output.  PG x 32
+// threads a row, 4 columns each; each of the PG takes consecutive pieces, U at a time,
+// whose loads are in flight together, and the PG meet in LDS in their order.
+template <int PG>
 __global__ __launch_bounds__(256) void sparse_combine_kernel(SparseArgs P) {
-  const int item = blockIdx.x, row = blockIdx.y * 8 + (threadIdx.x >> 5), c = 4 * (threadIdx.x & 31);
+  constexpr int U = 8, RB = 8 / PG;
+  const int item = blockIdx.x, tid = threadIdx.x, pg = (tid >> 5) % PG, c = 4 * (tid & 31);
+  const int row = blockIdx.y * RB + (tid >> 5) / PG;
   const int hz = item / P.nqb, qb = item - hz * P.nqb;
   const int z = hz / P.heads, h = hz - z * P.heads, qi = qb * QBLK + row;
-  if (row >= P.rows || qi >= P.Lq) return;
+  const bool in = row < P.rows && qi < P.Lq;
   const int64_t pf = piece_floats(P.rows);
+  const int per = (P.parts + PG - 1) / PG, p0 = pg * per, p1 = in ? min(P.parts, p0 + per) : 0;
   const float* w = P.ws + (int64_t)item * P.parts * pf;
-  // parts in groups whose loads are in flight together, first their maxima
-  constexpr int U = 8;
-  float mx = -INFINITY;
-  for (int p = 0; p < P.parts; p += U) {
-    float v[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = w[min(p + i, P.parts - 1) * pf + P.rows * D + P.rows + row];
-#pragma unroll
-    for (int i = 0; i < U; ++i) mx = fmaxf(mx, v[i]);
-  }
-  const float shift = neg_shift(mx);
-  float den = 0.f;
+  float mx = -INFINITY, den = 0.f;
   f32x4_t y = {};
-  for (int p = 0; p < P.parts; p += U) {
+  // one more piece (or sum of pieces) of weight 2^m
+  auto rescale = [&](float nm) {
+    const float a = __builtin_amdgcn_exp2f(mx + neg_shift(nm));
+    den *= a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] *= a;
+    mx = nm;
+  };
+  auto add = [&](float m, float s, const f32x4_t& v) {
+    const float a = __builtin_amdgcn_exp2f(m + neg_shift(mx));
+    den += a * s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += a * v[e];
+  };
+  for (int p = p0; p < p1; p += U) {
     f32x4_t v[U];
-    float f[U], s[U];
+    float m[U], s[U], nm = mx;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const float* x = w + min(p + i, P.parts - 1) * pf;
+      const float* x = w + min(p + i, p1 - 1) * pf;
       v[i] = *(const f32x4_t*)(x + row * D + c);
-      f[i] = x[P.rows * D + P.rows + row];
       s[i] = x[P.rows * D + row];
+      m[i] = x[P.rows * D + P.rows + row];
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (p + i >= P.parts) break;
-      const float a = __builtin_amdgcn_exp2f(f[i] + shift);
-      den += a * s[i];
+    for (int i = 0; i < U; ++i) nm = fmaxf(nm, m[i]);
+    rescale(nm);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += a * v[i][e];
+    for (int i = 0; i < U; ++i)
+      if (p + i < p1) add(m[i], s[i], v[i]);
+  }
+  if constexpr (PG > 1) {
+    __shared__ float red[6][256];
+    red[0][tid] = mx;
+    red[1][tid] = den;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[2 + e][tid] = y[e];
+    __syncthreads();
+    if (pg) return;
+    float nm = mx;
+#pragma unroll
+    for (int i = 1; i < PG; ++i) nm = fmaxf(nm, red[0][tid + 32 * i]);
+    rescale(nm);
+#pragma unroll
+    for (int i = 1; i < PG; ++i) {
+      const int t = tid + 32 * i;
+      add(red[0][t], red[1][t], f32x4_t{red[2][t], red[3][t], red[4][t], red[5][t]});
     }
   }
+  if (!in) return;
   const float inv = den == 0.f ? 0.f : 1.f / den;
   *(uint2*)(P.o + ((int64_t)z * P.Lq + qi) * P.ldo + h * D + c) =
       make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
@@ -1167,11 +1193,8 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
   a.x[0] = (const bf16_t*)q; a.ld[0] = ldq; a.out[0] = qm; a.L[0] = s.Lq; a.heads[0] = s.heads; a.blocks[0] = nqb;
   a.x[1] = (const bf16_t*)k; a.ld[1] = ldk; a.out[1] = km; a.L[1] = s.Lk; a.heads[1] = s.kv_heads; a.blocks[1] = nkb;
   a.klen = s.klen;
-  const int64_t total = rows + (int64_t)s.batch * s.kv_heads * nkb;
-  if (total > 0x7fffffff) return hipErrorInvalidValue;
   a.queries = (int)rows;
-  a.total = (int)total;
-  hipLaunchKernelGGL(block_mean_kernel, dim3(a.total), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(block_mean_kernel, dim3((uint32_t)(rows + (int64_t)s.batch * s.kv_heads * nkb)), dim3(256), 0, st, a);
   if (nkb <= SELECT_BLOCKS) {
     // More waves a work-group where there is at most one per CU: 4608 tokens, 24 heads (72)
     // 12.0 us with 16 waves, 14.0 with 8; 32760 tokens, 40 heads (640) 58.9 and 54.0.
@@ -1199,11 +1222,16 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
 
 // Work-groups that share one list, so that the launch fills the chip's 256 CUs, of
 // at least MIN_PART entries each.  (By the shape alone: the workspace's size does
-// not depend on the device.)
-constexpr int MIN_PART = 4;
+// not depend on the device.)  One token, 8 heads, 256 entries: 32 parts 16.6 us, 16
+// 17.3, 10 20.5; 24 heads, 52 entries: 10 parts 13.3, 4 15.5, 2 20.5; 128 queries, 8
+// heads, 24 entries: 12 parts 14.3, 6 14.8, 3 18.5.  Twice as many work-groups as CUs lose:
+// one token, 40 heads, 80 entries 20.5 -> 25.3 us; 32760 tokens' last 1280, 24 heads, 24 entries 35.5 -> 43.0.
+// Few queries' four waves share a list anyhow: up to FEW_WHOLE entries the joining
+// launch costs more than it saves (40 heads, 16 entries: 11.7 us whole, 13.4 in four).
+constexpr int MIN_PART = 4, FEW_QUERIES = 32, FEW_WHOLE = 16;
 int sparse_parts(const dit_sparse_shape& s) {
   const int64_t items = (int64_t)s.batch * s.heads * blocks_of(s.Lq, QBLK);
-  if (items == 0) return 1;
+  if (items == 0 || (s.Lq <= FEW_QUERIES && s.topk <= FEW_WHOLE)) return 1;
   const int64_t p = 256 / items;
   return (int)std::max<int64_t>(1, std::min<int64_t>(p, s.topk / MIN_PART));
 }
@@ -1215,7 +1243,9 @@ size_t attention_sparse_ws_bytes(const dit_sparse_shape& s) {
   return (size_t)s.batch * s.heads * blocks_of(s.Lq, QBLK) * parts * piece_floats(sparse_rows(s)) * sizeof(float);
 }
 
-constexpr int LONG_LIST = 16;  // entries from which the pipelined kernel is the faster one
+// Entries from which the pipelined kernel is the faster one: 32760 tokens, 40 heads,
+// bounded, in us, pipelined and plain: 8 entries 486 and 475, 12 638 and 635, 16 781 and 793, 32 1369 and 1417.
+constexpr int LONG_LIST = 16;
 
 hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                    const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, bool bounded,
@@ -1234,16 +1264,22 @@ hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int
   P.ws = (float*)ws;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   const int64_t groups = (int64_t)P.items * P.parts;
-  const bool two = s.Lq > 32 && groups <= n_cu;
+  // One work-group per CU leaves it the whole LDS: for few queries four waves with
+  // lists of their own (40 heads, 80 entries: 20.5 us, 23.8 with the waves in step; 300 lists of 50
+  // entries on two work-groups per CU 111, on one 117), else eight waves (1280 queries, 24
+  // heads, 24 entries: 35.5 us, 41.1 with four).
+  const bool one = groups <= n_cu, few = one && s.Lq <= FEW_QUERIES, two = one && !few;
   void (*fn)(SparseArgs);
-  if (s.Lq <= 16) fn = bounded ? attn_few_kernel<true, 1> : attn_few_kernel<false, 1>;
-  else if (s.Lq <= 32) fn = bounded ? attn_few_kernel<true, 2> : attn_few_kernel<false, 2>;
+  if (few && s.Lq <= 16) fn = bounded ? attn_few_kernel<true, 1> : attn_few_kernel<false, 1>;
+  else if (few) fn = bounded ? attn_few_kernel<true, 2> : attn_few_kernel<false, 2>;
   else if (two) fn = bounded ? attn_sparse_kernel<true, 2> : attn_sparse_kernel<false, 2>;
   else if (bounded && s.topk >= LONG_LIST) fn = attn_sparse_long_kernel;
   else fn = bounded ? attn_sparse_kernel<true, 1> : attn_sparse_kernel<false, 1>;
   hipLaunchKernelGGL(fn, dim3((uint32_t)groups), dim3(two ? 512 : 256), 0, st, P);
-  if (P.parts > 1)
-    hipLaunchKernelGGL(sparse_combine_kernel, dim3(P.items, (P.rows + 7) / 8), dim3(256), 0, st, P);
+  if (P.parts > 8)
+    hipLaunchKernelGGL(sparse_combine_kernel<8>, dim3(P.items, std::min(s.Lq, QBLK)), dim3(256), 0, st, P);
+  else if (P.parts > 1)
+    hipLaunchKernelGGL(sparse_combine_kernel<1>, dim3(P.items, (std::min(s.Lq, QBLK) + 7) / 8), dim3(256), 0, st, P);
   return hipGetLastError();
 }
 

@@ -35,6 +35,10 @@ dit_status launched(hipError_t e) {
 // Strides and alignment of the scale bytes of rows of K values.
 bool scale_ok(const void* p, int64_t ld, int32_t K) { return aligned(p, 4) && ld % 4 == 0 && ld >= DIT_FP8_SCALE_LD(K); }
 
+// A launch has fewer than 2^32 threads: work-groups of 512 and of 256.
+constexpr int64_t kMaxGroups512 = ((int64_t)1 << 23) - 1, kMaxGroups256 = ((int64_t)1 << 24) - 1;
+int64_t blocks_of(int64_t n, int64_t b) { return (n + b - 1) / b; }
+
 constexpr int64_t kMaxStride = (int64_t)1 << 22;  // a tile's rows lie below 2^31 bytes from its first one
 
 dit_status check_shape(const dit_sparse_shape* s) {
@@ -42,10 +46,9 @@ dit_status check_shape(const dit_sparse_shape* s) {
   if (s->batch < 0 || s->Lq < 0 || s->Lk < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads)
     return component_fail(DIT_ESHAPE, "bad attention shape");
   if (s->topk < 1) return component_fail(DIT_ESHAPE, "topk must be at least 1");
-  // (the products below stay inside 64 bits)
-  const int64_t nqb = ((int64_t)s->Lq + DIT_SPARSE_QB - 1) / DIT_SPARSE_QB, heads = (int64_t)s->batch * s->heads;
-  if (heads > 0x7fffffff || heads * nqb > 0x7fffffff) return component_fail(DIT_ESHAPE, "too many lists");
-  if (s->heads > (1 << 20)) return component_fail(DIT_ESHAPE, "too many heads");
+  const int64_t heads = (int64_t)s->batch * s->heads;  // (times 2^24 query blocks at most: inside 64 bits)
+  if (s->heads > (1 << 20) || heads > 0x7fffffff || heads * blocks_of(s->Lq, DIT_SPARSE_QB) > (1 << 22))
+    return component_fail(DIT_ESHAPE, "too many lists");
   return DIT_OK;
 }
 
@@ -75,6 +78,8 @@ dit_status dit_quant_fp8(const void* x, int32_t x_dtype, int64_t ldx, void* q, i
   if (M < 0 || K < 0 || K % 16) return component_fail(DIT_ESHAPE, "K must be a multiple of 16");
   if (ldx < K || ldx % (x_dtype == DIT_DTYPE_BF16 ? 8 : 4) || ldq < K || ldq % 16 || !scale_ok(scale, lds, K))
     return component_fail(DIT_ESHAPE, "bad row stride");
+  if (K > (1 << 30) || blocks_of((int64_t)M * blocks_of(K, 1024), 4) > kMaxGroups256)
+    return component_fail(DIT_ESHAPE, "too many values");
   return launched(dit::launch_quant_fp8(x, x_dtype == DIT_DTYPE_BF16, ldx, q, ldq, scale, lds, M, K,
                                         (hipStream_t)hip_stream));
 }
@@ -107,6 +112,7 @@ dit_status dit_gemm_fp8(const dit_gemm_fp8_desc* d, void* hip_stream) {
     return component_fail(DIT_ESHAPE, "bad output stride");
   if (fp8 && (d->N % 128 || (gelu && d->gelu_from % 128) || gap || d->ldc % 16 || !scale_ok(d->c_scale, d->ld_cs, d->N)))
     return component_fail(DIT_ESHAPE, "bad shape of the 8-bit output");
+  if (blocks_of(d->M, 64) * blocks_of(d->N, 128) > kMaxGroups512) return component_fail(DIT_ESHAPE, "too many outputs");
   dit::GemmFp8Args g{};
   g.A = d->A; g.lda = d->lda; g.W = d->W; g.ldw = d->ldw;
   g.As = d->a_scale; g.ldas = d->ld_as; g.Ws = d->w_scale; g.ldws = d->ld_ws;
@@ -130,8 +136,10 @@ dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int6
   TRY(check_rows(q, ldq, (int64_t)s->heads * 128, (int64_t)1 << 40));
   TRY(check_rows(k, ldk, (int64_t)s->kv_heads * 128, (int64_t)1 << 40));
   if (first < 0 || first > s->topk) return component_fail(DIT_EINVAL, "first must lie in [0, topk]");
-  if (s->Lk > 16384 * DIT_SPARSE_KB || s->batch > 65535 || s->heads > 65535 || (int64_t)s->batch * s->heads > 65535)
-    return component_fail(DIT_ESHAPE, "too many key blocks, sequences or heads");
+  const int64_t heads = (int64_t)s->batch * s->heads, nkb = blocks_of(s->Lk, DIT_SPARSE_KB);
+  if (nkb > 16384 || heads > 65535 ||
+      heads * blocks_of(s->Lq, DIT_SPARSE_QB) + (int64_t)s->batch * s->kv_heads * nkb > kMaxGroups256)
+    return component_fail(DIT_ESHAPE, "too many blocks or heads");
   return launched(dit::launch_select_blocks(*s, q, ldq, k, ldk, first, idx, ws, (hipStream_t)hip_stream, compute_units()));
 }
 

@@ -111,6 +111,29 @@ def test_sparse_calls_refuse_their_own():
     assert lib.dit_attention_sparse_ws_bytes(None) == 0
 
 
+def test_launches_past_their_limits_are_refused():
+    """Sizes whose grids would pass 2^32 threads, or whose indexes 32 bits; no rows or columns still do nothing."""
+    lib = binding.load()
+    top = 2 ** 31 - 1
+    for kw in ({"M": top}, {"M": top, "N": 8}, {"M": 64, "N": top - 7, "ldc": 1 << 40}, {"M": 1 << 20, "N": 1 << 17, "ldc": 1 << 20}):
+        d = gemm_desc(**kw)
+        assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_ESHAPE, kw
+    d = gemm_desc(M=top, N=0)
+    assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_OK
+    for M, K in ((1 << 26, 16), (1, top - 15), (1 << 16, 1 << 21), (top, 1 << 30)):
+        assert lib.dit_quant_fp8(FAKE, 1, 1 << 40, FAKE, 1 << 40, FAKE, 1 << 40, M, K, None) == binding.DIT_ESHAPE, (M, K)
+    assert lib.dit_quant_fp8(FAKE, 1, 1 << 40, FAKE, 1 << 40, FAKE, 1 << 40, top, 0, None) == binding.DIT_OK
+    for shape in (dict(Lq=top, heads=1, batch=1), dict(Lq=top, heads=1 << 20, batch=2047), dict(Lq=1, heads=2, batch=1 << 22),
+                  dict(Lq=1, heads=(1 << 20) + 1, batch=1)):
+        s = binding.sparse_shape(**dict(dict(Lk=64, topk=1, kv_heads=1), **shape))
+        ld = 128 * shape["heads"]
+        assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, ld, FAKE, 128, 0, FAKE, FAKE, None) == binding.DIT_ESHAPE
+        assert lib.dit_attention_sparse_bf16(C.byref(s), FAKE, ld, FAKE, 128, FAKE, 128, FAKE, ld, FAKE, 0, FAKE,
+                                             None) == binding.DIT_ESHAPE
+    s = binding.sparse_shape(Lq=1, Lk=16384 * 64, heads=8, kv_heads=8, batch=128, topk=1)
+    assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, 1024, FAKE, 1024, 0, FAKE, FAKE, None) == binding.DIT_ESHAPE
+
+
 def test_select_workspace_holds_means_and_keys():
     means = 2 * 4 * 16 * 128 + 2 * 2 * 16 * 128      # in groups of 16 blocks
     assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * means
