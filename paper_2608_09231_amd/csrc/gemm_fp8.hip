@@ -104,6 +104,13 @@ __device__ __forceinline__ void copy16_oob(const void* base, lds_void_t* dst, ui
 #endif
 }
 
+// 4 bytes from each lane's p to LDS at dst + 4 lane.
+__device__ __forceinline__ void copy4(const uint8_t* p, lds_void_t* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, dst, 4, 0, 0);
+#endif
+}
+
 // The 128 x 128-deep step of one 16 x 16 block.  A lane holds row lr's 16-byte
 // chunks lq and lq + 4 of the block of 128 (the sum over k does not mind their
 // order, and these are the chunks that a swizzled LDS row serves without bank
@@ -318,22 +325,29 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
 // slices in flight count: the waves meet before every step kt; slice kt + 1 has
 // landed, and slice kt, whose fragments are all in registers, gives its place to
 // slice kt + ST.  The fragments of kt + 1 are read under the MFMAs of kt.
-template <int BM, int KIND, bool WIDE>
-__global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
+// KG = 2: two groups of four waves with rings of their own take the halves of K; their
+// sums meet in LDS.
+template <int BM, int KIND, bool WIDE, int KG = 1>
+__global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
   constexpr int ST = BM == 128 ? 2 : 3;
-  constexpr int NW = BM == 256 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
+  constexpr int NW = BM == 256 ? 8 : 4, WM = BM / (NW / 2);  // waves (of a group), rows of a wave
   constexpr int TM = WM / 16, TN = 4, NF = TM + TN;
   constexpr int SLICE = (BM + 128) * 128;
   constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW, INS = A_INS + W_INS;
-  constexpr int EPI = BM * 128 * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[ST * SLICE > EPI ? ST * SLICE : EPI];
+  constexpr int TILE = BM * 128 * 4, RING = ST * SLICE;
+  __shared__ __attribute__((aligned(1024))) char lds[KG * (RING > TILE ? RING : TILE)];
   int tm, tn;
   tile_at(P, xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n), tm, tn);
   const int m0 = tm * BM, n0 = tn * 128;
   const int nk = (P.K + 127) >> 7;
 
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 8);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW;
+  char* smem = lds + grp * RING;
+  // slices k0 .. k1 - 1 are the group's; whole dwords of scales
+  const int half = 4 * ((nk + 7) >> 3);
+  const int k0 = KG == 1 || grp == 0 ? 0 : half, k1 = KG == 1 || grp ? nk : min(half, nk);
   const int wm = wave >> 1, wn = wave & 1;
   const int lr = lane & 15, lq = lane >> 4;
 
@@ -376,11 +390,11 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp8_tile_kernel
   };
   f32x4_t acc[TM][TN] = {};
 
-  load_scales(0);
+  load_scales(k0 >> 2);
 #pragma unroll
   for (int s = 0; s < ST; ++s)
 #pragma unroll
-    for (int j = 0; j < INS; ++j) issue1(s * SLICE, s, j);
+    for (int j = 0; j < INS; ++j) issue1(s * SLICE, k0 + s, j);
   wait_vmcnt<(ST - 1) * INS>();  // scales and slice 0 have landed
   barrier_no_fence();
   i32x8_t f0[NF], f1[NF];
@@ -422,189 +436,207 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp8_tile_kernel
     u = un;
   };
   using std::integral_constant;
-  int kt = 0;
-  for (; kt + 4 <= nk; kt += 4) {
+  int kt = k0;
+  for (; kt + 4 <= k1; kt += 4) {
     step(kt, f0, f1, integral_constant<int, 0>{});
     step(kt + 1, f1, f0, integral_constant<int, 1>{});
     step(kt + 2, f0, f1, integral_constant<int, 2>{});
     step(kt + 3, f1, f0, integral_constant<int, 3>{});
   }
-  if (kt < nk) step(kt, f0, f1, integral_constant<int, 0>{});
-  if (kt + 1 < nk) step(kt + 1, f1, f0, integral_constant<int, 1>{});
-  if (kt + 2 < nk) step(kt + 2, f0, f1, integral_constant<int, 2>{});
+  if (kt < k1) step(kt, f0, f1, integral_constant<int, 0>{});
+  if (kt + 1 < k1) step(kt + 1, f1, f0, integral_constant<int, 1>{});
+  if (kt + 2 < k1) step(kt + 2, f0, f1, integral_constant<int, 2>{});
+  if constexpr (KG == 2)
+    for (int i = max(k1 - k0, 0); i < min(half, nk); ++i) barrier_no_fence();  // the first group's steps
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
-  // The tile in LDS as slabs of BM / NW rows x 128, one per wave, columns XOR 16
-  // ((row >> 2) & 3): then each wave has whole 128-column rows.
-  float* tile = (float*)smem;
+  // The tile in LDS as slabs of ROWS rows x 128, one per wave, columns XOR 16
+  // ((row >> 2) & MASK): then each wave has whole 128-column rows.
+  constexpr int ROWS = BM / (NW * KG), MASK = ROWS == 8 ? 1 : 3;
+  float* tile = (float*)lds + grp * (BM * 128);
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        tile[(wm * WM + 16 * i + 4 * lq + r) * 128 + ((64 * wn + 16 * j + lr) ^ (lq << 4))] = acc[i][j][r];
+        tile[(wm * WM + 16 * i + 4 * lq + r) * 128 + ((64 * wn + 16 * j + lr) ^ ((lq & MASK) << 4))] = acc[i][j][r];
   __syncthreads();
-  constexpr int ROWS = BM / NW;
-  EpiLds<KIND> epi(P, m0 + ROWS * wave, n0, lane & 31, lane >> 5, tile + ROWS * wave * 128);
+  const int slab = grp * NW + wave;
+  float* mine = (float*)lds + ROWS * slab * 128;
+  if constexpr (KG == 2) {
+#pragma unroll
+    for (int i = 0; i < ROWS / 2; ++i) {
+      f32x4_t* x = (f32x4_t*)mine + 64 * i + lane;
+      *x += x[BM * 32];
+    }
+  }
+  EpiLds<KIND> epi(P, m0 + ROWS * slab, n0, lane & 31, lane >> 5, mine);
   epi.prep();
   uint2 old[8][2];
   if (epi.gated) epi.load_old(0, old);
-  epi.template slab_rows<3, 4, ROWS>(0, old);
+  epi.template slab_rows<MASK, 4, ROWS>(0, old);
 }
 
-// Few rows or few tiles: 16 RB x NT outputs per work-group, operands straight
-// from global memory into the fragments, K shared by its eight waves (NT = 128:
-// by four, the other four take the second 64 columns).
+// Few rows or few tiles: 16 RB x NT outputs per work-group, eight waves of 16 RB x 32
+// that share K (NT = 32: eight ways, 64: four, 128: two).  Each wave copies its own
+// rows' slices to a ring of its own in LDS, so that no wave waits for another until
+// their sums meet at the end; the copies read whole 128-byte lines, eight lanes each
+// (fragments loaded from global memory to registers, 16 rows an instruction, keep a CU's address unit
+// busy four times as long: one row, N = 64, K = 5120 12.9 us).
 template <int NT, int RB, int KIND, bool WIDE>
 __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
-  constexpr int NH = NT / 64, KS = 8 / NH, LD = 68;
-  __shared__ __attribute__((aligned(16))) float part[8][16 * RB][LD];
+  constexpr int NH = NT / 32, KS = 8 / NH, NF = 2 + RB, ST = RB == 1 ? 3 : 2;
+  constexpr int INS = 2 * NF, SLICE = INS * 1024 + 256, LD = 36;  // W's two fragments, A's, scales
+  constexpr int RING = 8 * ST * SLICE, PART = 8 * 16 * RB * LD * 4;
+  static_assert(PART <= RING, "the waves' sums take the rings' place");
+  __shared__ __attribute__((aligned(1024))) char smem[RING];
   const int lt = xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n);
   const int m0 = lt % P.tiles_m * (16 * RB), n0 = lt / P.tiles_m * NT;  // neighbours share the weights
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lq = lane >> 4;
   const int ks = wave % KS, nh = wave / KS;
-  const uint8_t *ap[RB], *wp[4], *sap[RB], *swp[4];
+  const int nw = min(n0 + 32 * nh, P.N - 1);  // (a wave past the last column repeats it)
+  const uint8_t* Wb = P.W + (int64_t)nw * P.ldw;
+  const uint8_t* Ab = P.A + (int64_t)m0 * P.lda;
+  // copy j: rows 8 j .. + 7 of W, then of A
+  uint32_t off[INS];
+  int ch[INS];
 #pragma unroll
-  for (int i = 0; i < RB; ++i) {
-    const int64_t r = min(m0 + 16 * i + lr, P.M - 1);
-    ap[i] = P.A + r * P.lda;
-    sap[i] = P.As + r * P.ldas;
+  for (int j = 0; j < INS; ++j) {
+    const int row = 8 * (j < 4 ? j : j - 4) + (lane >> 3);
+    ch[j] = 16 * ((lane & 7) ^ ((row >> 1) & 7));
+    off[j] = (uint32_t)min(row, (j < 4 ? P.N - 1 - nw : P.M - 1 - m0)) * (uint32_t)(j < 4 ? P.ldw : P.lda) + ch[j];
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t r = min(n0 + 64 * nh + 16 * j + lr, P.N - 1);
-    wp[j] = P.W + r * P.ldw;
-    swp[j] = P.Ws + r * P.ldws;
-  }
+  // scales of four slices of row lane: 32 of W, 16 RB of A
+  const uint8_t* sp = lane < 32 ? P.Ws + (int64_t)min(nw + lane, P.N - 1) * P.ldws
+                                : P.As + (int64_t)min(m0 + (lane - 32) % (16 * RB), P.M - 1) * P.ldas;
   const int steps = (P.K + 127) >> 7, per = (steps + KS - 1) / KS;
   const int s0 = ks * per, s1 = min(steps, s0 + per);
-  f32x4_t acc[RB][4] = {};
-  auto load16 = [&](const uint8_t* p, int k) {
-    const i32x4_t v = *(const i32x4_t*)(p + min(k, P.K - 16));
-    return k < P.K ? v : i32x4_t{0, 0, 0, 0};
+  char* ring = smem + wave * (ST * SLICE);
+  // slice s of K (past the wave's last one: zeros) and its scales
+  auto issue = [&](int s, int u) {
+    const int left = s < s1 ? P.K - 128 * s : 0;
+    copy4(sp + 4 * (min(s, steps - 1) >> 2), (lds_void_t*)(ring + u * SLICE + INS * 1024));
+#pragma unroll
+    for (int j = 0; j < INS; ++j)
+      copy16_oob(j < 4 ? Wb : Ab, (lds_void_t*)(ring + u * SLICE + j * 1024), ch[j] < left ? off[j] : OOB, (uint32_t)s * 128);
   };
-  auto load = [&](const uint8_t* p, int s) { return frag8(load16(p, 128 * s + 16 * lq), load16(p, 128 * s + 64 + 16 * lq)); };
-  constexpr int U = 2;  // steps whose loads are in flight together
-  for (int s = s0; s < s1; s += U) {
-    i32x8_t a[U][RB], w[U][4];
-    int sa[U][RB], sw[U][4];
+  int loff[2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u >= s1) break;
+  for (int h = 0; h < 2; ++h) loff[h] = lr * 128 + (((4 * h + lq) ^ ((lr >> 1) & 7)) << 4);
+  f32x4_t acc[RB][2] = {};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { w[u][j] = load(wp[j], s + u); sw[u][j] = swp[j][s + u]; }
+  for (int u = 0; u < ST; ++u) issue(s0 + u, u);
+  for (int s = s0; s < s1; s += ST) {
 #pragma unroll
-      for (int i = 0; i < RB; ++i) { a[u][i] = load(ap[i], s + u); sa[u][i] = sap[i][s + u]; }
-    }
+    for (int u = 0; u < ST; ++u) {  // (a slice past s1 adds zeros)
+      wait_vmcnt<(ST - 1) * (INS + 1)>();  // this slice and its scales have landed
+      asm volatile("" ::: "memory");
+      i32x8_t f[NF];
+      int b[NF];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u >= s1) break;
+      for (int i = 0; i < NF; ++i) {
+        f[i] = lds_frag(ring + u * SLICE + i * 2048 + loff[0], ring + u * SLICE + i * 2048 + loff[1]);
+        const int x = *(const int*)(ring + u * SLICE + INS * 1024 + 4 * (16 * i + lr));
+        b[i] = (x >> (8 * ((s + u) & 3))) & (s + u < s1 ? 255 : 0);
+      }
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): read, its place is free
+      asm volatile("" ::: "memory");
+      issue(s + u + ST, u);
       if constexpr (WIDE) {
-        bf16x8_t aw[RB][4];
+        bf16x8_t w[2][4];
+        widen(f[0], b[0], w[0]);
+        widen(f[1], b[1], w[1]);
 #pragma unroll
-        for (int i = 0; i < RB; ++i) widen(a[u][i], sa[u][i], aw[i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bf16x8_t wv[4];
-          widen(w[u][j], sw[u][j], wv);
+        for (int i = 0; i < RB; ++i) {
+          bf16x8_t a[4];
+          widen(f[2 + i], b[2 + i], a);
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < RB; ++i)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[i][t], wv[t], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < 2; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], w[j][t], acc[i][j], 0, 0, 0);
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < RB; ++i)
 #pragma unroll
-          for (int i = 0; i < RB; ++i) acc[i][j] = mfma_scaled(a[u][i], w[u][j], acc[i][j], sa[u][i], sw[u][j]);
+          for (int j = 0; j < 2; ++j) acc[i][j] = mfma_scaled(f[2 + i], f[j], acc[i][j], b[2 + i], b[j]);
       }
     }
   }
+  __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
+  __syncthreads();
+  float(*part)[16 * RB][LD] = (float(*)[16 * RB][LD])smem;
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) part[wave][16 * i + 4 * lq + r][16 * j + lr] = acc[i][j][r];
   __syncthreads();
 
-  // 16 threads per row: columns 4 c .. + 3 of each half, added in wave order
-  const int row = tid >> 4, c = tid & 15, m = m0 + row;
-  if (row >= 16 * RB) return;  // whole waves
-  float v[NH][4];
+  // NT / 4 threads per row, 4 columns each, the waves' sums added in their order
+  constexpr int TPR = NT / 4, PASS = 512 / TPR;
+  const int c = tid % TPR, n = n0 + 4 * c;
 #pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    const int n = n0 + 64 * h + 4 * c;
+  for (int r0 = 0; r0 < 16 * RB; r0 += PASS) {
+    const int row = r0 + tid / TPR, m = m0 + row;
+    if (row >= 16 * RB) return;  // whole waves
     f32x4_t t = {};
 #pragma unroll
-    for (int w = 0; w < KS; ++w) t += *(const f32x4_t*)&part[KS * h + w][row][4 * c];
+    for (int w = 0; w < KS; ++w) t += *(const f32x4_t*)&part[KS * (c / 8) + w][row][4 * (c % 8)];
+    float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[h][e] = t[e] + (P.bias && n < P.N ? bf16_to_f32(P.bias[n + e]) : 0.f);
-  }
-  if constexpr (NT == 128) {
-    if (n0 < P.rms_cols) {  // one 128-wide head per tile
-      float ss = 0.f;
+    for (int e = 0; e < 4; ++e) v[e] = t[e] + (P.bias && n < P.N ? bf16_to_f32(P.bias[n + e]) : 0.f);
+    if constexpr (NT == 128) {
+      if (n0 < P.rms_cols) {  // one 128-wide head per tile
+        float ss = v[0] * v[0] + v[1] * v[1] + v[2] * v[2] + v[3] * v[3];
 #pragma unroll
-      for (int h = 0; h < NH; ++h)
+        for (int o = 1; o < 32; o <<= 1) ss += __shfl_xor(ss, o, 64);
+        const float f = rsqrtf(ss * (1.f / 128.f) + DIT_RMS_EPS);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ss += v[h][e] * v[h][e];
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) ss += __shfl_xor(ss, o, 64);
-      const float sc = rsqrtf(ss * (1.f / 128.f) + DIT_RMS_EPS);
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[h][e] *= sc;
+        for (int e = 0; e < 4; ++e) v[e] *= f;
+      }
     }
-  }
-  uint32_t top = 0;
-#pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    const int n = n0 + 64 * h + 4 * c;
+    uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (n >= P.gelu_from) v[h][e] = gelu_tanh_f(v[h][e]);
-      if (P.flags & DIT_EPI_SILU) v[h][e] = silu_f(v[h][e]);
-      top = max(top, __float_as_uint(v[h][e]) & 0x7fffffffu);
+      if (n >= P.gelu_from) v[e] = gelu_tanh_f(v[e]);
+      if (P.flags & DIT_EPI_SILU) v[e] = silu_f(v[e]);
+      top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
     }
-  }
-  uint32_t byte = 127;
-  float inv = 1.f;
-  if constexpr (KIND == EPI_K_FP8) {
-    top = max_over<16>(top);
-    byte = e8m0_of(top);
-    inv = e8m0_inverse(byte);
-  }
-  if (m >= P.M) return;
-#pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    const int n = n0 + 64 * h + 4 * c;
-    if (n >= P.N) continue;
+    uint32_t byte = 127;
+    float inv = 1.f;
     if constexpr (KIND == EPI_K_FP8) {
-      *(uint32_t*)((uint8_t*)P.C + (int64_t)m * P.ldc + n) =
-          pack_fp8x4(v[h][0] * inv, v[h][1] * inv, v[h][2] * inv, v[h][3] * inv);
-      if (n % 128 == 0) P.Cs[(int64_t)m * P.ldcs + (n >> 7)] = (uint8_t)byte;
+      top = max_over<16>(top);
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+      byte = e8m0_of(top);
+      inv = e8m0_inverse(byte);
+    }
+    if (m >= P.M || n >= P.N) continue;
+    if constexpr (KIND == EPI_K_FP8) {
+      *(uint32_t*)((uint8_t*)P.C + (int64_t)m * P.ldc + n) = pack_fp8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+      if (c == 0) P.Cs[(int64_t)m * P.ldcs + (n >> 7)] = (uint8_t)byte;
       continue;
     }
     const int64_t at = (int64_t)m * P.ldc + n + (n >= P.gap_at ? P.gap : 0);
     if constexpr (WIDE) {
-      *(float4*)((float*)P.C + at) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+      *(float4*)((float*)P.C + at) = make_float4(v[0], v[1], v[2], v[3]);
       continue;
     }
     uint2* o = (uint2*)((bf16_t*)P.C + at);
     if (P.flags & DIT_EPI_GATED_RES) {
       const uint2 x = *o;
       const float4 g = *(const float4*)(P.gate + n);
-      v[h][0] = __uint_as_float(x.x << 16) + g.x * v[h][0];
-      v[h][1] = __uint_as_float(x.x & 0xffff0000u) + g.y * v[h][1];
-      v[h][2] = __uint_as_float(x.y << 16) + g.z * v[h][2];
-      v[h][3] = __uint_as_float(x.y & 0xffff0000u) + g.w * v[h][3];
+      v[0] = __uint_as_float(x.x << 16) + g.x * v[0];
+      v[1] = __uint_as_float(x.x & 0xffff0000u) + g.y * v[1];
+      v[2] = __uint_as_float(x.y << 16) + g.z * v[2];
+      v[3] = __uint_as_float(x.y & 0xffff0000u) + g.w * v[3];
     }
-    *o = make_uint2(pack_bf16x2(v[h][0], v[h][1]), pack_bf16x2(v[h][2], v[h][3]));
+    *o = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
   }
 }
 
@@ -615,7 +647,6 @@ hipError_t launch_quant_fp8(const void* x, bool bf16, int64_t ldx, void* q, int6
   if (M == 0 || K == 0) return hipSuccess;
   const int per_row = (K + 1023) / 1024;
   const int64_t groups = ((int64_t)M * per_row + 3) / 4;
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
   if (bf16)
     hipLaunchKernelGGL(quant_fp8_kernel<bf16_t>, dim3((uint32_t)groups), dim3(256), 0, s, (const bf16_t*)x, ldx,
                        (uint8_t*)q, ldq, (uint8_t*)scale, lds, M, K, per_row);
@@ -644,33 +675,49 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu) {
   auto go = [&](void (*fn)(Fp8Prob), int bm, int bn, int threads) {
     p.tiles_m = (g.M + bm - 1) / bm;
     p.tiles_n = (g.N + bn - 1) / bn;
-    const int64_t n = (int64_t)p.tiles_m * p.tiles_n;
-    if (n > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(fn, dim3((uint32_t)n), dim3(threads), 0, s, p);
+    hipLaunchKernelGGL(fn, dim3((uint32_t)p.tiles_m * p.tiles_n), dim3(threads), 0, s, p);
     return hipGetLastError();
   };
-  const int nt = groups ? 128 : 64;
-  if (tiles(32, nt) <= n_cu) {
-    const bool one = g.M <= 16;
-    if (fp8) return one ? go(gemm_fp8_small_kernel<128, 1, EPI_K_FP8, false>, 16, 128, 512)
-                        : go(gemm_fp8_small_kernel<128, 2, EPI_K_FP8, false>, 32, 128, 512);
-    if (f32) {
-      if (groups) return one ? go(gemm_fp8_small_kernel<128, 1, EPI_K_ANY, true>, 16, 128, 512)
-                             : go(gemm_fp8_small_kernel<128, 2, EPI_K_ANY, true>, 32, 128, 512);
-      return one ? go(gemm_fp8_small_kernel<64, 1, EPI_K_ANY, true>, 16, 64, 512)
-                 : go(gemm_fp8_small_kernel<64, 2, EPI_K_ANY, true>, 32, 64, 512);
-    }
-    if (groups) return one ? go(gemm_fp8_small_kernel<128, 1, EPI_K_ANY, false>, 16, 128, 512)
-                           : go(gemm_fp8_small_kernel<128, 2, EPI_K_ANY, false>, 32, 128, 512);
-    return one ? go(gemm_fp8_small_kernel<64, 1, EPI_K_ANY, false>, 16, 64, 512)
-               : go(gemm_fp8_small_kernel<64, 2, EPI_K_ANY, false>, 32, 64, 512);
-  }
-  if (f32) return go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true>, 64, 128, 256);
   const bool plain = !(g.flags & DIT_EPI_SILU);
   const bool store = plain && !gated && !fp8 && (g.gelu_from >= g.N || g.gelu_from % 128 == 0) &&
                      (g.gap == 0 || g.gap_at % 128 == 0);
   const bool only_gate = plain && gated && g.rms_cols == 0 && g.gelu_from >= g.N && g.gap == 0;
-  // Rounds of the chip times a tile's time: 4 us and, per slice of 128 of K,
+  // Few rows or few tiles: the narrowest tiles that fit the CUs once, to spread the
+  // way of W over them.  In us, these tiles (their width) and 64 x 128 ones: 1 x 5120 x 5120 9 (32) and 17, 8 x
+  // 5120 x 13824 13.8 (32) and 37, 64 x 5120 x 5120 12 (64) and 18, 32 x 16384 x 5120 16 (64) and 19, 1 x 28672 x
+  // 5120 29 (128) and 30.  128 columns of 32 rows only for f32, 128 x 8192 x 5120 21 and 26; bf16
+  // 19.5 and 18.6, 32 x 28672 x 5120 39 and 33.  Two rounds of them lose: 512 x 2560 x 5120 35 and 19.
+  const bool one = g.M <= 16;
+  const int rows = one ? 16 : 32, widest = one || f32 ? 128 : 64;
+  int nt = groups ? 128 : 32;
+  while (nt < widest && tiles(rows, nt) > n_cu) nt *= 2;
+  if (nt <= widest && tiles(rows, nt) <= n_cu) {
+    if (fp8) return go(gemm_fp8_small_kernel<128, 1, EPI_K_FP8, false>, rows, 128, 512);
+    if (f32 && one)
+      return go(nt == 128 ? gemm_fp8_small_kernel<128, 1, EPI_K_ANY, true> : nt == 64 ? gemm_fp8_small_kernel<64, 1, EPI_K_ANY, true>
+                : gemm_fp8_small_kernel<32, 1, EPI_K_ANY, true>, rows, nt, 512);
+    if (f32)
+      return go(nt == 128 ? gemm_fp8_small_kernel<128, 2, EPI_K_ANY, true> : nt == 64 ? gemm_fp8_small_kernel<64, 2, EPI_K_ANY, true>
+                : gemm_fp8_small_kernel<32, 2, EPI_K_ANY, true>, rows, nt, 512);
+    if (one)
+      return go(nt == 128 ? gemm_fp8_small_kernel<128, 1, EPI_K_ANY, false> : nt == 64 ? gemm_fp8_small_kernel<64, 1, EPI_K_ANY, false>
+                : gemm_fp8_small_kernel<32, 1, EPI_K_ANY, false>, rows, nt, 512);
+    return go(nt == 64 ? gemm_fp8_small_kernel<64, 2, EPI_K_ANY, false> : gemm_fp8_small_kernel<32, 2, EPI_K_ANY, false>,
+              rows, nt, 512);
+  }
+  if (f32) {
+    // One work-group per CU: two groups of waves, one's widening beside the other's
+    // products, where either has some slices.  256 x 5120 x 5120 31.5 -> 26.6 us,
+    // 1333 x 1000 x 2320 18.6 -> 17.7 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
+    // (256 x 5120 x 5120 18.6 and 18.4 us, 1333 x 1000 x 2320 12.8 and 13.5).
+    const bool split = tiles(64, 128) <= n_cu && g.K > 1024;
+    return split ? go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true, 2>, 64, 128, 512)
+                 : go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true>, 64, 128, 256);
+  }
+  // Rounds of the chip times a tile's time, which is 4 us and some per slice of 128 of K
+  // (fitted to each kernel alone over the sizes below).  In us, 64 x 128, 128 x 128, 256 x 128 and 256 x 256 tiles:
+  //   512 x 10240 x 5120  45 44 36 56    1024 x 10240 x 5120 75 81 76 55    512 x 5120 x 5120  29 39 37 56
+  //   2048 x 4096 x 4096  50 40 36 51    4096 x 4096 x 1024  39 32 32 23    1333 x 1000 x 2320 13 25 27 37
   struct { int bm, bn, per_cu; double slice_us; } const cfg[] = {
       {64, 128, 2, 0.62}, {128, 128, 2, 1.0}, {256, 128, 1, 0.95}, {256, 256, 1, 1.5}};
   int best = 0;

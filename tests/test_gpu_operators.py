@@ -195,6 +195,26 @@ def test_gemm_sizes_of_one_round(M, N, K, out):
     check_gemm(M, N, K, out=out, pad=8 if M % 8 else 0, bias=M % 8 == 0)
 
 
+# narrow tiles of 64 and 128 columns; f32 outputs whose K is shared by two groups of waves, the second with one to
+# as many slices as the first
+@pytest.mark.parametrize("out", ["bf16", "f32", "gated"])
+@pytest.mark.parametrize("M,N,K", [(5, 9000, 400), (16, 20008, 272), (100, 3000, 656), (300, 2056, 1936), (900, 2000, 1040),
+                                   (897, 1992, 1552), (900, 2040, 2064), (850, 2048, 2048)])
+def test_gemm_sizes_of_few_tiles(M, N, K, out):
+    check_gemm(M, N, K, out=out, pad=8 if M % 8 else 0, bias=M % 8 == 0)
+
+
+def test_gemm_f32_of_shared_k_norm_gelu_and_gap():
+    check_gemm(900, 2048, 1168, out="f32", rms_cols=256, gelu_from=384, gap_at=384, gap=128, seed=1)
+    check_gemm(900, 2048, 1296, out="f32", rms_cols=128, gelu_from=204, gap_at=140, gap=12, pad=4, seed=2)
+    check_gemm(900, 2048, 1168, out="f32", act="silu", seed=3)
+    a, w = operand(rng(1), 900, 1168), operand(rng(2), 2048, 1168)
+    a[1][700, 9] = 255
+    _, _, got, y, tol = run_gemm(900, 2048, 1168, out="f32", operands=(a, w))
+    rest = np.arange(900) != 700
+    assert np.isnan(got[700]).all() and (np.abs(got - y)[rest] <= tol[rest]).all()
+
+
 @pytest.mark.parametrize("act", ["none", "gelu", "rms"])
 @pytest.mark.parametrize("M,N,K", [(1913, 4352, 656), (500, 10240, 400)])
 def test_gemm_fp8_output_of_one_round(M, N, K, act):
