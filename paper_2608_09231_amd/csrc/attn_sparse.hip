@@ -272,11 +272,14 @@ __device__ __forceinline__ void topk_row(const uint64_t (&key)[R], int32_t* __re
 // Scores and choice in one for at most 64 R key blocks: 16 query blocks of a head, their
 // means in registers, their keys in LDS.  NW waves take 16 key blocks in turn (f64
 // 16x16x4 MFMAs), then 16 / NW rows each.
+//
+// 32760 tokens, 40 heads: 54 us, in which a CU's f64 MFMAs alone take 20, the means
+// from L2 (640 work-groups of 16 query blocks against 512 key blocks) about as long and the
+// search the rest, one after the other within a work-group.
 template <int R, int NW>
-__global__ __launch_bounds__(64 * NW, R == 16 && NW == 8 ? 2 : 4) void block_select_kernel(const double* __restrict__ qm, const double* __restrict__ km,
-                                                              int32_t* __restrict__ idx, int nqb, int nkb, int heads,
-                                                              int kv_heads, int Lk, int first, int topk,
-                                                              const int32_t* klen) {
+__global__ __launch_bounds__(64 * NW, R == 16 && NW == 8 ? 2 : 4) void block_select_kernel(
+    const double* __restrict__ qm, const double* __restrict__ km, int32_t* __restrict__ idx, int nqb, int nkb, int heads,
+    int kv_heads, int Lk, int first, int topk, const int32_t* klen) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ uint64_t keys[16][64 * R + 2];
   const int hz = blockIdx.y, z = hz / heads, h = hz - z * heads;
@@ -444,7 +447,8 @@ struct ListCursor {
   const int32_t* p;
   int n, base, v, nkb;
   uint64_t left;
-  __device__ __forceinline__ ListCursor(const int32_t* p_, int n_, int nkb_) : p(p_), n(n_), base(-64), v(0), nkb(nkb_), left(0) {}
+  __device__ __forceinline__ ListCursor(const int32_t* p_, int n_, int nkb_)
+      : p(p_), n(n_), base(-64), v(0), nkb(nkb_), left(0) {}
   __device__ __forceinline__ int next() {  // -1: none left
     while (left == 0) {
       base += 64;
@@ -472,7 +476,8 @@ __device__ __forceinline__ bf16x8_t vt_frag(const char* p) {
 #endif
 }
 
-// A wave's 32 queries (block rows wrow ..), 16 per group, d blocks of 16: normalised to o, or as a part of the list.
+// A wave's 32 queries (block rows wrow ..), 16 per group, d blocks of 16: normalised
+// to o, or as a part of the list.
 __device__ __forceinline__ void store_rows(const SparseArgs& P, const f32x4_t (&acc)[8][2], const float (&l)[2],
                                            const float (&m)[2], int unit, int z, int h, int qb, int wrow, int lr, int lq) {
 #pragma unroll
@@ -508,6 +513,11 @@ __device__ __forceinline__ void store_rows(const SparseArgs& P, const f32x4_t (&
 // TP = 1: two work-groups per CU, one's softmax beside the other's products.  TP =
 // 2: one per CU, for launches that leave no second one; the groups take tiles in
 // turn, and their outputs meet in LDS.
+//
+// The waves of a work-group meet at every tile, so its LDS reads, MFMAs and softmax,
+// each about 1 us of a CU for two tiles, overlap little: 192 lists of 9 blocks 18.6 us
+// (0.38 PFLOP/s); 10240 lists of 52, two work-groups per CU, 2.3 ms (0.97).  V's rows in an
+// order without bank conflicts (a third of the LDS cycles) change nothing.
 template <bool BOUNDED, int TP>
 __global__ __launch_bounds__(256 * TP, 2) void attn_sparse_kernel(SparseArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -702,7 +712,8 @@ __global__ __launch_bounds__(256 * TP, 2) void attn_sparse_kernel(SparseArgs P) 
 // At most 16 NG queries a sequence (single tokens, say): what bounds it is the way
 // of K and V from memory.  Each of four waves takes all queries and its own share
 // of the list, 32 keys at a time in its own two buffers of LDS: no wave waits for
-// another until their four parts meet at the end.
+// another until their four parts meet at the end.  One token, 40 heads, 64 blocks (84
+// MB): 17 us and 2.4 to join the pieces, 4.3 TB/s; 200 blocks 5.6 TB/s.
 template <bool BOUNDED, int NG>
 __global__ __launch_bounds__(256, 1) void attn_few_kernel(SparseArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -731,7 +742,7 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(SparseArgs P) {
   // first key of the next 32; -1: none
   int kb = list.next(), half = 0;
 #pragma unroll
-  for (int g = 0; g < NG; ++g)  // the queries arrive with the list: waited for later, they would wait for the copies, too
+  for (int g = 0; g < NG; ++g)  // (queries waited for later would wait for the copies, too)
 #pragma unroll
     for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(qf[g][s]));
   auto next = [&]() {
@@ -901,6 +912,11 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(SparseArgs P) {
 // t - 1 on MFMA with the softmax of tile t, which depends on neither, between
 // them in 32 fenced slots of two MFMAs, one fragment read AHEAD slots before its use
 // and a share of the softmax.  Its copies are V of tile t and K of tile t + 3.
+//
+// 32760 tokens, 40 heads, lists of 52 (2.2 TFLOP): 2.03 - 2.1 ms, 1.07 PFLOP/s (a large bf16
+// product: 1.35).  Power and the way from memory bound it: 1.6 ms on zeros, 1.9 ms where all lists are the
+// same.  A running maximum between the slots costs more than the overlap gives: such
+// lists take attn_sparse_kernel.
 __global__ __launch_bounds__(256, 2) void attn_sparse_long_kernel(SparseArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int TILE = KT * D * 2, VBASE = 3 * TILE;
@@ -1174,7 +1190,8 @@ constexpr int SELECT_BLOCKS = 1024;
 // Means of the query blocks and of the key blocks (f64), then, past SELECT_BLOCKS, one key per pair.
 size_t select_blocks_ws_bytes(const dit_sparse_shape& s) {
   const size_t nqb = blocks_of(s.Lq, QBLK), nkb = blocks_of(s.Lk, KBLK), b = s.batch;
-  return 8 * (b * s.heads * mean_doubles((int)nqb) + b * s.kv_heads * mean_doubles((int)nkb) + (nkb > SELECT_BLOCKS ? b * s.heads * nqb * nkb : 0));
+  return 8 * (b * s.heads * mean_doubles((int)nqb) + b * s.kv_heads * mean_doubles((int)nkb) +
+              (nkb > SELECT_BLOCKS ? b * s.heads * nqb * nkb : 0));
 }
 
 hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
@@ -1225,7 +1242,7 @@ hipError_t launch_select_blocks(const dit_sparse_shape& s, const void* q, int64_
 // not depend on the device.)  One token, 8 heads, 256 entries: 32 parts 16.6 us, 16
 // 17.3, 10 20.5; 24 heads, 52 entries: 10 parts 13.3, 4 15.5, 2 20.5; 128 queries, 8
 // heads, 24 entries: 12 parts 14.3, 6 14.8, 3 18.5.  Twice as many work-groups as CUs lose:
-// one token, 40 heads, 80 entries 20.5 -> 25.3 us; 32760 tokens' last 1280, 24 heads, 24 entries 35.5 -> 43.0.
+// one token, 40 heads, 64 entries 20.5 -> 25.3 us; 32760 tokens' last 1280, 24 heads, 24 entries 35.5 -> 43.0.
 // Few queries' four waves share a list anyhow: up to FEW_WHOLE entries the joining
 // launch costs more than it saves (40 heads, 16 entries: 11.7 us whole, 13.4 in four).
 constexpr int MIN_PART = 4, FEW_QUERIES = 32, FEW_WHOLE = 16;
@@ -1265,7 +1282,7 @@ hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   const int64_t groups = (int64_t)P.items * P.parts;
   // One work-group per CU leaves it the whole LDS: for few queries four waves with
-  // lists of their own (40 heads, 80 entries: 20.5 us, 23.8 with the waves in step; 300 lists of 50
+  // lists of their own (40 heads, 64 entries: 20.5 us, 23.8 with the waves in step; 300 lists of 50
   // entries on two work-groups per CU 111, on one 117), else eight waves (1280 queries, 24
   // heads, 24 entries: 35.5 us, 41.1 with four).
   const bool one = groups <= n_cu, few = one && s.Lq <= FEW_QUERIES, two = one && !few;

@@ -46,7 +46,8 @@ using EpiLds = EpiLdsT<KIND, Fp8Prob>;
 // ---------------------------------------------------------------- quantise
 
 // Eight lanes per block of 128, 16 values each; a wave takes eight blocks of a
-// row.  One pass: bound by the copy rate.
+// row.  One pass, bound by memory: 32760 x 5120 bf16 (504 MB) 86 us, 5.9 TB/s (a
+// copy of 1 GiB: 5.2).
 template <typename T>
 __global__ __launch_bounds__(256) void quant_fp8_kernel(const T* __restrict__ x, int64_t ldx, uint8_t* __restrict__ q,
                                                         int64_t ldq, uint8_t* __restrict__ scale, int64_t lds, int M,
@@ -126,7 +127,8 @@ __device__ __forceinline__ f32x4_t mfma_scaled(const i32x8_t& a, const i32x8_t& 
 
 // The same of a 32 x 32 block and 64 of K: lane (lr, lh) holds 32 of row lr.
 template <int B>
-__device__ __forceinline__ f32x16_t mfma_scaled32(const i32x8_t& a, const i32x8_t& w, const f32x16_t& c, int sa, int sw) {
+__device__ __forceinline__ f32x16_t mfma_scaled32(const i32x8_t& a, const i32x8_t& w, const f32x16_t& c, int sa,
+                                                  int sw) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, w, c, 0, 0, B, sa, B, sw);
 #else
@@ -185,6 +187,11 @@ __device__ __forceinline__ void tile_at(const Fp8Prob& P, int lt, int& tm, int& 
 // units take A slice kt + 2 (in substep 1) and W slice kt + 3 (in the next
 // substep 0).  Slices past the last one are copied as zeros (no memory
 // traffic), which keeps every iteration and wait alike.
+//
+// 32760 x 13824 x 5120: bf16 out 1.87 ms (2.48 PFLOP/s), GELU and 8-bit rows out
+// 2.02 ms (2.30).  Power bounds it: the same launch on operands of zeros runs at
+// 3.65 PFLOP/s; on normal data the clock falls to 1.9 - 2.15 GHz.  Slices of 64
+// and 128 x 128 tiles of four waves were slower.
 template <int KIND>
 __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
   constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4;
@@ -325,8 +332,13 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
 // slices in flight count: the waves meet before every step kt; slice kt + 1 has
 // landed, and slice kt, whose fragments are all in registers, gives its place to
 // slice kt + ST.  The fragments of kt + 1 are read under the MFMAs of kt.
-// KG = 2: two groups of four waves with rings of their own take the halves of K; their
-// sums meet in LDS.
+// 512 x 10240 x 5120 with the norm: 37 us (1.45 PFLOP/s) on 160 tiles of 256 x 128,
+// which leave a third of the CUs without one.  Three work-groups of 64 x 128 per CU
+// with two slices each lose: 1333 x 1000 x 2320 13 -> 17 us.
+//
+// KG = 2: two groups of four waves with rings of their own take the halves of K;
+// their sums meet in LDS.  1333 x 1000 x 2320, f32: 17 us (0.36 PFLOP/s), a chain of
+// ten slices on 168 CUs.
 template <int BM, int KIND, bool WIDE, int KG = 1>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
   constexpr int ST = BM == 128 ? 2 : 3;
@@ -481,9 +493,10 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
 // Few rows or few tiles: 16 RB x NT outputs per work-group, eight waves of 16 RB x 32
 // that share K (NT = 32: eight ways, 64: four, 128: two).  Each wave copies its own
 // rows' slices to a ring of its own in LDS, so that no wave waits for another until
-// their sums meet at the end; the copies read whole 128-byte lines, eight lanes each
-// (fragments loaded from global memory to registers, 16 rows an instruction, keep a CU's address unit
-// busy four times as long: one row, N = 64, K = 5120 12.9 us).
+// their sums meet at the end; the copies read whole 128-byte lines, eight lanes
+// each (fragments loaded to registers, 16 rows an instruction, take a CU longer
+// than the memory does: 8 x 5120 x 13824 20.7 us).  Bound by the way of W from
+// memory: 8 x 5120 x 13824 13.8 us, 5.1 TB/s; 1 x 13824 x 5120 13.6 us, 5.2 TB/s.
 template <int NT, int RB, int KIND, bool WIDE>
 __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
   constexpr int NH = NT / 32, KS = 8 / NH, NF = 2 + RB, ST = RB == 1 ? 3 : 2;
@@ -694,14 +707,17 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu) {
   if (nt <= widest && tiles(rows, nt) <= n_cu) {
     if (fp8) return go(gemm_fp8_small_kernel<128, 1, EPI_K_FP8, false>, rows, 128, 512);
     if (f32 && one)
-      return go(nt == 128 ? gemm_fp8_small_kernel<128, 1, EPI_K_ANY, true> : nt == 64 ? gemm_fp8_small_kernel<64, 1, EPI_K_ANY, true>
-                : gemm_fp8_small_kernel<32, 1, EPI_K_ANY, true>, rows, nt, 512);
+      return go(nt == 128  ? gemm_fp8_small_kernel<128, 1, EPI_K_ANY, true>
+                : nt == 64 ? gemm_fp8_small_kernel<64, 1, EPI_K_ANY, true>
+                           : gemm_fp8_small_kernel<32, 1, EPI_K_ANY, true>, rows, nt, 512);
     if (f32)
-      return go(nt == 128 ? gemm_fp8_small_kernel<128, 2, EPI_K_ANY, true> : nt == 64 ? gemm_fp8_small_kernel<64, 2, EPI_K_ANY, true>
-                : gemm_fp8_small_kernel<32, 2, EPI_K_ANY, true>, rows, nt, 512);
+      return go(nt == 128  ? gemm_fp8_small_kernel<128, 2, EPI_K_ANY, true>
+                : nt == 64 ? gemm_fp8_small_kernel<64, 2, EPI_K_ANY, true>
+                           : gemm_fp8_small_kernel<32, 2, EPI_K_ANY, true>, rows, nt, 512);
     if (one)
-      return go(nt == 128 ? gemm_fp8_small_kernel<128, 1, EPI_K_ANY, false> : nt == 64 ? gemm_fp8_small_kernel<64, 1, EPI_K_ANY, false>
-                : gemm_fp8_small_kernel<32, 1, EPI_K_ANY, false>, rows, nt, 512);
+      return go(nt == 128  ? gemm_fp8_small_kernel<128, 1, EPI_K_ANY, false>
+                : nt == 64 ? gemm_fp8_small_kernel<64, 1, EPI_K_ANY, false>
+                           : gemm_fp8_small_kernel<32, 1, EPI_K_ANY, false>, rows, nt, 512);
     return go(nt == 64 ? gemm_fp8_small_kernel<64, 2, EPI_K_ANY, false> : gemm_fp8_small_kernel<32, 2, EPI_K_ANY, false>,
               rows, nt, 512);
   }

@@ -115,7 +115,8 @@ def test_launches_past_their_limits_are_refused():
     """Sizes whose grids would pass 2^32 threads, or whose indexes 32 bits; no rows or columns still do nothing."""
     lib = binding.load()
     top = 2 ** 31 - 1
-    for kw in ({"M": top}, {"M": top, "N": 8}, {"M": 64, "N": top - 7, "ldc": 1 << 40}, {"M": 1 << 20, "N": 1 << 17, "ldc": 1 << 20}):
+    for kw in ({"M": top}, {"M": top, "N": 8}, {"M": 64, "N": top - 7, "ldc": 1 << 40},
+               {"M": 1 << 20, "N": 1 << 17, "ldc": 1 << 20}):
         d = gemm_desc(**kw)
         assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_ESHAPE, kw
     d = gemm_desc(M=top, N=0)
