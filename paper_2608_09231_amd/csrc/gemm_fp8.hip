@@ -409,12 +409,16 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
     for (int j = 0; j < INS; ++j) issue1(s * SLICE, k0 + s, j);
   wait_vmcnt<(ST - 1) * INS>();  // scales and slice 0 have landed
   barrier_no_fence();
-  i32x8_t f0[NF], f1[NF];
+  i32x8_t f0[NF], other[WIDE ? 1 : NF];
+  auto& f1 = [&]() -> auto& {
+    if constexpr (WIDE) return f0;
+    else return other;
+  }();
 #pragma unroll
   for (int f = 0; f < NF; ++f) f0[f] = rd(0, f);
   spread_scales();
   int u = 0;  // place of slice kt
-  auto step = [&](int kt, const i32x8_t(&f)[NF], i32x8_t(&fn)[NF], auto b_) {
+  auto step = [&](int kt, i32x8_t(&f)[NF], i32x8_t(&fn)[NF], auto b_) {
     constexpr int B = decltype(b_)::value;
     const int un = u == (ST - 1) * SLICE ? 0 : u + SLICE;
     // this wave's reads of slice kt and its copies of slice kt + 1 are done (those
@@ -423,26 +427,44 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
     barrier_no_fence();
     if constexpr (B == 0) load_scales((kt >> 2) + 1);
     __builtin_amdgcn_sched_barrier(0);
-    [[maybe_unused]] bf16x8_t aw[WIDE ? TM : 1][4], wv[4];
-    if constexpr (WIDE)
+    if constexpr (WIDE) {
+      // A widened, then W's fragments one ahead of their MFMAs; a fragment's registers take
+      // that of the next slice as soon as it is widened (f and fn are the same)
+      bf16x8_t aw[TM][4], wv[2][4];
 #pragma unroll
       for (int i = 0; i < TM; ++i) widen(f[i], sc[i] >> (8 * B), aw[i]);
+      widen(f[TM], sc[TM] >> (8 * B), wv[0]);
 #pragma unroll
-    for (int q = 0; q < TM * TN; ++q) {
-      const int i = q % TM, j = q / TM;
-      if constexpr (WIDE) {
-        if (i == 0) widen(f[TM + j], sc[TM + j] >> (8 * B), wv);
+      for (int j = 0; j < TN; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        fn[TM + j] = rd(un, TM + j);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+          if (j == TN - 2) fn[i] = rd(un, i);
+#pragma unroll
+        for (int c = j * INS / TN; c < (j + 1) * INS / TN; ++c) issue1(u, kt + ST, c);
+        if (j + 1 < TN) widen(f[TM + j + 1], sc[TM + j + 1] >> (8 * B), wv[(j + 1) & 1]);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[i][t], wv[t], acc[i][j], 0, 0, 0);
-      } else {
-        acc[i][j] = mfma_scaled<B>(f[i], f[TM + j], acc[i][j], sc[i], sc[TM + j]);
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[i][t], wv[j & 1][t], acc[i][j], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      // in the order of their use: A 0, W 0, the other A, the other W
-      if (q < NF) fn[q == 0 ? 0 : q == 1 ? TM : q <= TM ? q - 1 : q] = rd(un, q == 0 ? 0 : q == 1 ? TM : q <= TM ? q - 1 : q);
-      if (q >= TM * TN - INS) issue1(u, kt + ST, q - (TM * TN - INS));
-      __builtin_amdgcn_sched_barrier(0);
+    } else {
+#pragma unroll
+      for (int q = 0; q < TM * TN; ++q) {
+        const int i = q % TM, j = q / TM;
+        acc[i][j] = mfma_scaled<B>(f[i], f[TM + j], acc[i][j], sc[i], sc[TM + j]);
+        __builtin_amdgcn_sched_barrier(0);
+        // in the order of their use: A 0, W 0, the other A, the other W
+        if (q < NF) {
+          const int x = q == 0 ? 0 : q == 1 ? TM : q <= TM ? q - 1 : q;
+          fn[x] = rd(un, x);
+        }
+        if (q >= TM * TN - INS) issue1(u, kt + ST, q - (TM * TN - INS));
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     if constexpr (B == 3) spread_scales();
     u = un;
@@ -721,28 +743,31 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu) {
     return go(nt == 64 ? gemm_fp8_small_kernel<64, 2, EPI_K_ANY, false> : gemm_fp8_small_kernel<32, 2, EPI_K_ANY, false>,
               rows, nt, 512);
   }
-  if (f32) {
-    // One work-group per CU: two groups of waves, one's widening beside the other's
-    // products, where either has some slices.  256 x 5120 x 5120 31.5 -> 26.6 us,
-    // 1333 x 1000 x 2320 18.6 -> 17.7 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
-    // (256 x 5120 x 5120 18.6 and 18.4 us, 1333 x 1000 x 2320 12.8 and 13.5).
-    const bool split = tiles(64, 128) <= n_cu && g.K > 1024;
-    return split ? go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true, 2>, 64, 128, 512)
-                 : go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true>, 64, 128, 256);
-  }
   // Rounds of the chip times a tile's time, which is 4 us and some per slice of 128 of K
   // (fitted to each kernel alone over the sizes below).  In us, 64 x 128, 128 x 128, 256 x 128 and 256 x 256 tiles:
   //   512 x 10240 x 5120  45 44 36 56    1024 x 10240 x 5120 75 81 76 55    512 x 5120 x 5120  29 39 37 56
   //   2048 x 4096 x 4096  50 40 36 51    4096 x 4096 x 1024  39 32 32 23    1333 x 1000 x 2320 13 25 27 37
-  struct { int bm, bn, per_cu; double slice_us; } const cfg[] = {
-      {64, 128, 2, 0.62}, {128, 128, 2, 1.0}, {256, 128, 1, 0.95}, {256, 256, 1, 1.5}};
-  int best = 0;
-  double best_us = 1e30;
-  for (int c = 0; c < 4; ++c) {
-    const int64_t slots = (int64_t)n_cu * cfg[c].per_cu;
-    const double us = (double)((tiles(cfg[c].bm, cfg[c].bn) + slots - 1) / slots) * ((g.K + 127) / 128 * cfg[c].slice_us + 4);
-    if (us < best_us) { best_us = us; best = c; }
+  // and f32 outputs on 64 x 128 and 128 x 128 tiles:
+  //   4096 x 4096 x 4096 147 122   32760 x 5120 x 2048 794 668   512 x 10240 x 5120 66 68   32760 x 64 x 5120 54 64
+  struct Tile { int bm, bn, per_cu; double slice_us; };
+  auto cost = [&](const Tile& c) {
+    const int64_t slots = (int64_t)n_cu * c.per_cu;
+    return (double)((tiles(c.bm, c.bn) + slots - 1) / slots) * ((g.K + 127) / 128 * c.slice_us + 4);
+  };
+  if (f32) {
+    // One work-group per CU: two groups of waves, one's widening beside the other's
+    // products, where either has some slices.  256 x 5120 x 5120 31.5 -> 24.6 us,
+    // 1333 x 1000 x 2320 18.6 -> 17.2 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
+    // (256 x 5120 x 5120 18.6 and 18.4 us, 1333 x 1000 x 2320 12.8 and 13.5).
+    if (tiles(64, 128) <= n_cu && g.K > 1024) return go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true, 2>, 64, 128, 512);
+    if (cost({64, 128, 2, 1.02}) <= cost({128, 128, 2, 1.78}))
+      return go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true>, 64, 128, 256);
+    return go(gemm_fp8_tile_kernel<128, EPI_K_ANY, true>, 128, 128, 256);
   }
+  const Tile cfg[] = {{64, 128, 2, 0.62}, {128, 128, 2, 1.0}, {256, 128, 1, 0.95}, {256, 256, 1, 1.5}};
+  int best = 0;
+  for (int c = 1; c < 4; ++c)
+    if (cost(cfg[c]) < cost(cfg[best])) best = c;
   if (best == 3)
     return go(fp8 ? gemm_fp8_ring_kernel<EPI_K_FP8> : store ? gemm_fp8_ring_kernel<EPI_K_STORE>
               : only_gate ? gemm_fp8_ring_kernel<EPI_K_GATED> : gemm_fp8_ring_kernel<EPI_K_ANY>, 256, 256, 512);

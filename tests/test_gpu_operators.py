@@ -204,6 +204,19 @@ def test_gemm_sizes_of_few_tiles(M, N, K, out):
     check_gemm(M, N, K, out=out, pad=8 if M % 8 else 0, bias=M % 8 == 0)
 
 
+def test_gemm_f32_of_wide_tiles_norm_gelu_and_gap():
+    """Tiles of 128 x 128: 512 and more of them."""
+    for M, N, K in ((4096, 2048, 400), (4090, 2304, 656), (8192, 1408, 144)):
+        check_gemm(M, N, K, out="f32", rms_cols=256, gelu_from=384, gap_at=384, gap=128, seed=1)
+    check_gemm(4090, 2048, 656, out="f32", rms_cols=128, gelu_from=204, gap_at=140, gap=12, pad=4, seed=2)
+    check_gemm(4090, 2040, 784, out="f32", act="silu", seed=3)
+    a, w = operand(rng(1), 4096, 1168), operand(rng(2), 2048, 1168)
+    a[1][700, 9] = 255
+    _, _, got, y, tol = run_gemm(4096, 2048, 1168, out="f32", operands=(a, w))
+    rest = np.arange(4096) != 700
+    assert np.isnan(got[700]).all() and (np.abs(got - y)[rest] <= tol[rest]).all()
+
+
 def test_gemm_f32_of_shared_k_norm_gelu_and_gap():
     check_gemm(900, 2048, 1168, out="f32", rms_cols=256, gelu_from=384, gap_at=384, gap=128, seed=1)
     check_gemm(900, 2048, 1296, out="f32", rms_cols=128, gelu_from=204, gap_at=140, gap=12, pad=4, seed=2)
