@@ -514,10 +514,11 @@ __device__ __forceinline__ void store_rows(const SparseArgs& P, const f32x4_t (&
 // 2: one per CU, for launches that leave no second one; the groups take tiles in
 // turn, and their outputs meet in LDS.
 //
-// The waves of a work-group meet at every tile, so its LDS reads, MFMAs and softmax,
-// each about 1 us of a CU for two tiles, overlap little: 192 lists of 9 blocks 18.6 us
-// (0.38 PFLOP/s); 10240 lists of 52, two work-groups per CU, 2.3 ms (0.97).  V's rows in an
-// order without bank conflicts (a third of the LDS cycles) change nothing.
+// A tile's score product, softmax and second product follow one another in every
+// wave: 192 lists of 9 blocks on as many CUs take 18.6 us (0.38 PFLOP/s), the MFMAs busy
+// in 0.22 of the cycles and LDS in 0.18; 10240 lists of 52, two work-groups per CU,
+// 2.3 ms (0.97).  V's rows in an order without bank conflicts (a third of the LDS
+// cycles) change nothing.
 template <bool BOUNDED, int TP>
 __global__ __launch_bounds__(256 * TP, 2) void attn_sparse_kernel(SparseArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
