@@ -120,7 +120,9 @@ dit_status dit_attention_bf16_noalloc(const void* q, int64_t ldq, const void* k,
  * Their workspaces belong to the caller, and a workspace serves one call at
  * a time: two calls (or graphs) that may run at the same time need two.  The
  * current device is the stream's.  Nothing is launched where a status other
- * than DIT_OK is returned for an argument; a size of zero is no error.
+ * than DIT_OK is returned for an argument.  A size of zero is no error (K = 0
+ * of a product is), and the pointers to what is empty then may be NULL; where
+ * nothing is to be written nothing is launched.
  *
  * 8-bit rows.  A row of K values is held as K bytes of e4m3 (OCP, largest
  * value 448) and one scale byte (E8M0: 2^(byte - 127)) for each 128 of them,
@@ -157,7 +159,6 @@ enum { DIT_EPI_FP8 = 8 };
  * which add a few neighbouring products in about 14 bits before they enter the
  * f32 sum (2e-5 in the 2-norm on normal data); f32 outputs are computed from
  * operands widened to bf16, at half that rate.
- * K and N of zero: K = 0 is refused, N = 0 and M = 0 do nothing.
  * Errors: DIT_EINVAL (null pointers; bad flags: one of F32, FP8 and GATED_RES
  * at most; A, W, C, gate not 16-byte, scales not 4-byte, bias not 2-byte
  * aligned), DIT_ESHAPE (negative sizes, K < 1, K % 16, N % 8, lda or ldw below

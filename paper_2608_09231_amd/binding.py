@@ -358,8 +358,8 @@ def fp8_scale_ld(K: int) -> int:
 
 
 def _rows(t, name, rows, width, ld, esize):
-    """Row stride of a device tensor that holds `rows` rows of `width` elements (None: the tensor's own; a
-    tensor of one dimension holds them back to back): the library reads them through a raw pointer."""
+    """Row stride of a device tensor that holds `rows` rows of `width` elements (None: a matrix's own; tensors of
+    other dimensions hold them back to back): the library reads them through a raw pointer."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.element_size() != esize:
@@ -372,6 +372,8 @@ def _rows(t, name, rows, width, ld, esize):
             return step if have > 1 else max(step, width)
         ld = step if have > 1 else width
     elif ld is None:
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be a matrix, or contiguous, or come with its row stride")
         ld = width
     if len(shape) and shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} must have contiguous rows")

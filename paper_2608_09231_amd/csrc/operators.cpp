@@ -52,8 +52,9 @@ dit_status check_shape(const dit_sparse_shape* s) {
   return DIT_OK;
 }
 
-dit_status check_rows(const void* p, int64_t ld, int64_t width, int64_t most) {
-  if (!p) return component_fail(DIT_EINVAL, "null argument");
+// (empty: no rows, so that nothing is read or written at p)
+dit_status check_rows(const void* p, int64_t ld, int64_t width, int64_t most, bool empty) {
+  if (!p && !empty) return component_fail(DIT_EINVAL, "null argument");
   if (!aligned(p, 16)) return component_fail(DIT_EINVAL, "rows must be 16-byte aligned");
   if (ld < width || ld % 8 || ld > most) return component_fail(DIT_ESHAPE, "bad row stride");
   return DIT_OK;
@@ -71,7 +72,7 @@ extern "C" {
 
 dit_status dit_quant_fp8(const void* x, int32_t x_dtype, int64_t ldx, void* q, int64_t ldq, void* scale, int64_t lds,
                          int32_t M, int32_t K, void* hip_stream) {
-  if (!x || !q || !scale) return component_fail(DIT_EINVAL, "null argument");
+  if (M != 0 && K != 0 && (!x || !q || !scale)) return component_fail(DIT_EINVAL, "null argument");
   if (x_dtype != DIT_DTYPE_BF16 && x_dtype != DIT_DTYPE_F32) return component_fail(DIT_EINVAL, "bad input type");
   if (!aligned(x, 16) || !aligned(q, 16) || !aligned(scale, 4))
     return component_fail(DIT_EINVAL, "x and q must be 16-byte, scale 4-byte aligned");
@@ -85,12 +86,14 @@ dit_status dit_quant_fp8(const void* x, int32_t x_dtype, int64_t ldx, void* q, i
 }
 
 dit_status dit_gemm_fp8(const dit_gemm_fp8_desc* d, void* hip_stream) {
-  if (!d || !d->A || !d->W || !d->a_scale || !d->w_scale || !d->C) return component_fail(DIT_EINVAL, "null argument");
+  if (!d) return component_fail(DIT_EINVAL, "null argument");
+  const bool empty = d->M == 0 || d->N == 0;
+  if (!empty && (!d->A || !d->W || !d->a_scale || !d->w_scale || !d->C)) return component_fail(DIT_EINVAL, "null argument");
   const bool f32 = d->flags & DIT_EPI_F32, fp8 = d->flags & DIT_EPI_FP8, gated = d->flags & DIT_EPI_GATED_RES;
   if ((d->flags & ~(DIT_EPI_F32 | DIT_EPI_GATED_RES | DIT_EPI_SILU | DIT_EPI_FP8)) || f32 + fp8 + gated > 1)
     return component_fail(DIT_EINVAL, "bad flags");
-  if (gated && !d->gate) return component_fail(DIT_EINVAL, "the gated residual needs a gate");
-  if (fp8 && !d->c_scale) return component_fail(DIT_EINVAL, "the 8-bit output needs c_scale");
+  if (gated && !d->gate && !empty) return component_fail(DIT_EINVAL, "the gated residual needs a gate");
+  if (fp8 && !d->c_scale && !empty) return component_fail(DIT_EINVAL, "the 8-bit output needs c_scale");
   if (!aligned(d->A, 16) || !aligned(d->W, 16) || !aligned(d->C, 16) || !aligned(d->bias, 2) ||
       (gated && !aligned(d->gate, 16)))
     return component_fail(DIT_EINVAL, "A, W, C and gate must be 16-byte aligned");
@@ -130,11 +133,12 @@ size_t dit_select_blocks_ws_bytes(const dit_sparse_shape* s) {
 dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                   int32_t first, int32_t* idx, void* ws, void* hip_stream) {
   TRY(check_shape(s));
-  if (!idx || !ws) return component_fail(DIT_EINVAL, "null argument");
+  const bool no_q = s->batch == 0 || s->Lq == 0, no_k = no_q || s->Lk == 0;
+  if (!no_q && (!idx || !ws)) return component_fail(DIT_EINVAL, "null argument");
   if (!aligned(ws, 16) || !aligned(idx, 4) || !aligned(s->klen, 4))
     return component_fail(DIT_EINVAL, "the workspace must be 16-byte, idx and klen 4-byte aligned");
-  TRY(check_rows(q, ldq, (int64_t)s->heads * 128, (int64_t)1 << 40));
-  TRY(check_rows(k, ldk, (int64_t)s->kv_heads * 128, (int64_t)1 << 40));
+  TRY(check_rows(q, ldq, (int64_t)s->heads * 128, (int64_t)1 << 40, no_q));
+  TRY(check_rows(k, ldk, (int64_t)s->kv_heads * 128, (int64_t)1 << 40, no_k));
   if (first < 0 || first > s->topk) return component_fail(DIT_EINVAL, "first must lie in [0, topk]");
   const int64_t heads = (int64_t)s->batch * s->heads, nkb = blocks_of(s->Lk, DIT_SPARSE_KB);
   if (nkb > 16384 || heads > 65535 ||
@@ -151,13 +155,14 @@ dit_status dit_attention_sparse_bf16(const dit_sparse_shape* s, const void* q, i
                                      const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, int32_t flags,
                                      void* ws, void* hip_stream) {
   TRY(check_shape(s));
-  if (!idx) return component_fail(DIT_EINVAL, "null argument");
+  const bool no_q = s->batch == 0 || s->Lq == 0, no_k = no_q || s->Lk == 0;
+  if (!idx && !no_q) return component_fail(DIT_EINVAL, "null argument");
   if (flags & ~DIT_ATTN_BOUNDED_LOGITS) return component_fail(DIT_EINVAL, "bad attention flags");
   if (!aligned(idx, 4) || !aligned(s->klen, 4)) return component_fail(DIT_EINVAL, "idx and klen must be 4-byte aligned");
-  TRY(check_rows(q, ldq, (int64_t)s->heads * 128, kMaxStride - 1));
-  TRY(check_rows(k, ldk, (int64_t)s->kv_heads * 128, kMaxStride - 1));
-  TRY(check_rows(v, ldv, (int64_t)s->kv_heads * 128, kMaxStride - 1));
-  TRY(check_rows(o, ldo, (int64_t)s->heads * 128, kMaxStride - 1));
+  TRY(check_rows(q, ldq, (int64_t)s->heads * 128, kMaxStride - 1, no_q));
+  TRY(check_rows(k, ldk, (int64_t)s->kv_heads * 128, kMaxStride - 1, no_k));
+  TRY(check_rows(v, ldv, (int64_t)s->kv_heads * 128, kMaxStride - 1, no_k));
+  TRY(check_rows(o, ldo, (int64_t)s->heads * 128, kMaxStride - 1, no_q));
   if (dit::attention_sparse_ws_bytes(*s) && (!ws || !aligned(ws, 16)))
     return component_fail(DIT_EINVAL, "needs a 16-byte aligned workspace");
   return launched(dit::launch_attention_sparse(*s, q, ldq, k, ldk, v, ldv, o, ldo, idx,

@@ -566,6 +566,19 @@ def test_lengths_of_zero():
         idx.fill_(0)
         binding.attention_sparse_bf16(x, x, x, o, idx, ws=ws, **shape)
         assert (o[:batch * Lq] == 0).all() and (o[batch * Lq:] == 0x2A2A).all()
+    # empty tensors, whose pointers are null
+    for Lq, Lk in ((200, 0), (0, 64), (40, 0), (20, 0)):
+        shape = dict(Lq=Lq, Lk=Lk, heads=2, topk=20)
+        q, k = (torch.empty(n, 256, dtype=torch.int16, device="cuda") for n in (Lq, Lk))
+        idx = torch.full((1, 2, -(-Lq // 128), 20), 1, dtype=torch.int32, device="cuda")
+        o = torch.full((Lq, 256), 1, dtype=torch.int16, device="cuda")
+        binding.attention_sparse_bf16(q, k, k, o, idx, **shape)
+        binding.select_blocks_bf16(q, k, idx, **shape)
+        assert (o == 0).all() and (idx == -1).all()
+    e = torch.empty(0, 256, dtype=torch.uint8, device="cuda")
+    w, c = torch.zeros(64, 256, dtype=torch.uint8, device="cuda"), torch.empty(0, 64, dtype=torch.int16, device="cuda")
+    binding.quant_fp8(torch.empty(0, 256, device="cuda"), e, e, M=0, K=256)
+    binding.gemm_fp8(e, e, w, w, None, c, M=0, N=64, K=256)
 
 
 @pytest.mark.parametrize("Lq", [1, 200])
@@ -775,3 +788,34 @@ def test_workspaces_of_the_caching_allocator():
             outs.append((idx, o))
     for idx, o in outs:
         assert torch.equal(idx, outs[0][0]) and torch.equal(o, outs[0][1])
+
+
+def test_workspaces_of_a_captured_call():
+    """Workspaces that the binding takes during a capture stay the graph's own: other allocations between the
+    replays do not touch them."""
+    torch = torch_cuda()
+    r = rng(33)
+    shape = shape_of(1, 5000, 3, 64)
+    q, k = dev(torch, tokens(r, 1, 3)[0]), dev(torch, tokens(r, 5000, 3)[0])
+    idx = torch.empty(1, 3, 1, 64, dtype=torch.int32, device="cuda")
+    o = torch.empty(1, 384, dtype=torch.int16, device="cuda")
+
+    def run():
+        binding.select_blocks_bf16(q, k, idx, **shape)
+        binding.attention_sparse_bf16(q, k, k, o, idx, **shape)
+
+    run()
+    want = idx.clone(), o.clone()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for i in range(4):
+        junk = [torch.full((n,), -1, dtype=torch.int32, device="cuda") for n in (300, 5000, 70000, 10 ** 6)]
+        idx.fill_(7)
+        o.zero_()
+        g.replay()
+        junk += [torch.full((n,), -1, dtype=torch.int32, device="cuda") for n in (300, 5000, 70000)]
+        torch.cuda.synchronize()
+        assert torch.equal(idx, want[0]) and torch.equal(o, want[1]), i
+        del junk

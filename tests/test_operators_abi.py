@@ -191,6 +191,39 @@ def test_binding_checks_sizes_and_devices():
         binding.quant_fp8(x, q, s, M=4, K=128, stream=type("S", (), {"device": "cuda:1"})())
 
 
+def test_binding_refuses_strided_tensors_of_other_dimensions():
+    """A slice of a [batch, rows, 3, width] projection is no run of rows; with its row stride it is."""
+    torch = pytest.importorskip("torch")
+    qkv = torch.zeros(2, 5, 3, 256)
+    part = _Device(qkv[:, :, 1])
+    with pytest.raises(ValueError, match="row stride"):
+        binding._rows(part, "q", 10, 256, None, 4)
+    assert binding._rows(part, "q", 10, 256, 768, 4) == 768
+    assert binding._rows(_Device(qkv.view(10, 768)[:, 256:512]), "q", 10, 256, None, 4) == 768
+    assert binding._rows(_Device(torch.zeros(2, 5, 256)), "q", 10, 256, None, 4) == 256
+    with pytest.raises(ValueError, match="row stride"):
+        binding._rows(_Device(torch.zeros(20)[::2]), "klen", 1, 10, None, 4)
+
+
+def test_nothing_to_write_needs_no_pointers():
+    lib = binding.load()
+    assert lib.dit_quant_fp8(None, 1, 256, None, 256, None, 4, 0, 256, None) == binding.DIT_OK
+    for kw in ({"M": 0}, {"N": 0}):
+        for flags in (0, 1, 2, 8):
+            d = gemm_desc(A=None, W=None, a_scale=None, w_scale=None, C=None, flags=flags, ld_cs=4, **kw)
+            assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_OK
+    for shape in ({"Lq": 0}, {"batch": 0}):
+        s = binding.sparse_shape(**dict(SHAPE, **shape))
+        assert lib.dit_select_blocks_bf16(C.byref(s), None, 512, None, 256, 0, None, None, None) == binding.DIT_OK
+        assert lib.dit_attention_sparse_bf16(C.byref(s), None, 512, None, 256, None, 256, None, 512, None, 0, None,
+                                             None) == binding.DIT_OK
+    # no keys: k and v may be empty, the lists and rows are written
+    s = binding.sparse_shape(**dict(SHAPE, Lk=0))
+    assert lib.dit_attention_sparse_bf16(C.byref(s), FAKE, 512, None, 256, None, 256, None, 512, FAKE, 0, None,
+                                         None) == binding.DIT_EINVAL
+    assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, 512, None, 256, 0, None, FAKE, None) == binding.DIT_EINVAL
+
+
 def test_oracle_rounds_to_nearest_even():
     """The oracle's quantiser against torch's conversion, which rounds to nearest even."""
     torch = pytest.importorskip("torch")
