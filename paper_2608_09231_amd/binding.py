@@ -357,13 +357,25 @@ def fp8_scale_ld(K: int) -> int:
     return (K + 511) // 512 * 4
 
 
+_ESIZE = {}  # bytes of an element by type; those whose values the library would misread: 0
+
+
+def _esize(t):
+    size = _ESIZE.get(t.dtype)
+    if size is None:
+        size = 0 if str(t.dtype) in ("torch.float16", "torch.bool", "torch.float8_e5m2", "torch.float8_e4m3fnuz",
+                                     "torch.float8_e5m2fnuz") else t.element_size()
+        _ESIZE[t.dtype] = size
+    return size
+
+
 def _rows(t, name, rows, width, ld, esize):
     """Row stride of a device tensor that holds `rows` rows of `width` elements (None: a matrix's own; tensors of
     other dimensions hold them back to back): the library reads them through a raw pointer."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.element_size() != esize:
-        raise ValueError(f"{name} must have elements of {esize} bytes")
+    if _esize(t) != esize:
+        raise ValueError(f"{name} must have elements of {esize} bytes and not be {t.dtype}")
     shape = t.shape
     if ld is None and len(shape) == 2:
         have, wide = shape

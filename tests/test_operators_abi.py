@@ -205,6 +205,14 @@ def test_binding_refuses_strided_tensors_of_other_dimensions():
         binding._rows(_Device(torch.zeros(20)[::2]), "klen", 1, 10, None, 4)
 
 
+@pytest.mark.parametrize("dtype", ["float16", "float8_e5m2", "float8_e4m3fnuz", "bool"])
+def test_binding_refuses_types_that_would_be_misread(dtype):
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(4, 128, dtype=getattr(torch, dtype))
+    with pytest.raises(ValueError, match="not be torch"):
+        binding._rows(_Device(x), "x", 4, 128, None, x.element_size())
+
+
 def test_nothing_to_write_needs_no_pointers():
     lib = binding.load()
     assert lib.dit_quant_fp8(None, 1, 256, None, 256, None, 4, 0, 256, None) == binding.DIT_OK
