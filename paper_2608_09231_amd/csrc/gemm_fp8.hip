@@ -337,7 +337,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
 // with two slices each lose: 1333 x 1000 x 2320 13 -> 17 us.
 //
 // KG = 2: two groups of four waves with rings of their own take the halves of K;
-// their sums meet in LDS.  1333 x 1000 x 2320, f32: 17 us (0.36 PFLOP/s), a chain of
+// their sums meet in LDS.  1333 x 1000 x 2320, f32: 16 us (0.38 PFLOP/s), a chain of
 // ten slices on 168 CUs.
 template <int BM, int KIND, bool WIDE, int KG = 1>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
@@ -357,9 +357,9 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
   const int grp = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 8);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW;
   char* smem = lds + grp * RING;
-  // slices k0 .. k1 - 1 are the group's; whole dwords of scales
-  const int half = 4 * ((nk + 7) >> 3);
-  const int k0 = KG == 1 || grp == 0 ? 0 : half, k1 = KG == 1 || grp ? nk : min(half, nk);
+  // slices k0 .. k1 - 1 are the group's
+  const int half = (nk + 1) >> 1;
+  const int k0 = KG == 1 || grp == 0 ? 0 : half, k1 = KG == 1 || grp ? nk : half;
   const int wm = wave >> 1, wn = wave & 1;
   const int lr = lane & 15, lq = lane >> 4;
 
@@ -382,13 +382,22 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
   // permutation hands them to the lanes that multiply (A's fragments, then W's)
   const uint8_t* sap = P.As + (int64_t)min(m0 + WM * wm + (lane & (WM - 1)), P.M - 1) * P.ldas;
   const uint8_t* swp = P.Ws + (int64_t)min(n0 + 64 * wn + lane, P.N - 1) * P.ldws;
-  int sna, snw, sc[NF];
-  auto load_scales = [&](int g) {
-    const int at = 4 * min(g, (nk - 1) >> 2);
+  int sna, snw, sna1 = 0, snw1 = 0, sc[NF];
+  auto load_scales = [&](int g) {  // of slices k0 + 4 g .. + 3; KG = 2: from two dwords
+    const int at = 4 * min((k0 >> 2) + g, (nk - 1) >> 2);
     sna = *(const int*)(sap + at);
     snw = *(const int*)(swp + at);
+    if constexpr (KG == 2) {
+      const int next = 4 * min((k0 >> 2) + g + 1, (nk - 1) >> 2);
+      sna1 = *(const int*)(sap + next);
+      snw1 = *(const int*)(swp + next);
+    }
   };
   auto spread_scales = [&]() {
+    if constexpr (KG == 2) {
+      sna = __builtin_amdgcn_alignbyte(sna1, sna, k0 & 3);
+      snw = __builtin_amdgcn_alignbyte(snw1, snw, k0 & 3);
+    }
 #pragma unroll
     for (int f = 0; f < NF; ++f)
       sc[f] = __builtin_amdgcn_ds_bpermute(4 * lr + 64 * (f < TM ? f : f - TM), f < TM ? sna : snw);
@@ -402,7 +411,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
   };
   f32x4_t acc[TM][TN] = {};
 
-  load_scales(k0 >> 2);
+  load_scales(0);
 #pragma unroll
   for (int s = 0; s < ST; ++s)
 #pragma unroll
@@ -425,7 +434,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
     // of the next ST - 2 may stay in flight); then everyone's are
     wait_vmcnt_lgkm0<(ST - 2) * INS>();
     barrier_no_fence();
-    if constexpr (B == 0) load_scales((kt >> 2) + 1);
+    if constexpr (B == 0) load_scales(((kt - k0) >> 2) + 1);
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (WIDE) {
       // A widened, then W's fragments one ahead of their MFMAs; a fragment's registers take
@@ -481,7 +490,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
   if (kt + 1 < k1) step(kt + 1, f1, f0, integral_constant<int, 1>{});
   if (kt + 2 < k1) step(kt + 2, f0, f1, integral_constant<int, 2>{});
   if constexpr (KG == 2)
-    for (int i = max(k1 - k0, 0); i < min(half, nk); ++i) barrier_no_fence();  // the first group's steps
+    for (int i = k1 - k0; i < half; ++i) barrier_no_fence();  // the first group may have one more step
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
   // The tile in LDS as slabs of ROWS rows x 128, one per wave, columns XOR 16
@@ -757,7 +766,7 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu) {
   if (f32) {
     // One work-group per CU: two groups of waves, one's widening beside the other's
     // products, where either has some slices.  256 x 5120 x 5120 31.5 -> 24.6 us,
-    // 1333 x 1000 x 2320 18.6 -> 17.2 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
+    // 1333 x 1000 x 2320 18.6 -> 16 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
     // (256 x 5120 x 5120 18.6 and 18.4 us, 1333 x 1000 x 2320 12.8 and 13.5).
     if (tiles(64, 128) <= n_cu && g.K > 1024) return go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true, 2>, 64, 128, 512);
     if (cost({64, 128, 2, 1.02}) <= cost({128, 128, 2, 1.78}))
