@@ -69,6 +69,7 @@ SHAPE = dict(Lq=300, Lk=1000, heads=4, kv_heads=2, topk=5, batch=2)
     (binding.DIT_ESHAPE, {"batch": -1}, {}), (binding.DIT_ESHAPE, {"Lq": -1}, {}), (binding.DIT_ESHAPE, {"Lk": -1}, {}),
     (binding.DIT_ESHAPE, {"heads": 0}, {}), (binding.DIT_ESHAPE, {"kv_heads": 3}, {}),
     (binding.DIT_ESHAPE, {"kv_heads": 0}, {}), (binding.DIT_ESHAPE, {"topk": 0}, {}),
+    (binding.DIT_ESHAPE, {"topk": 2 ** 30 + 1}, {}),
     (binding.DIT_ESHAPE, {"batch": 2 ** 30, "heads": 2 ** 20}, {}),
     (binding.DIT_EINVAL, {}, {"q": None}), (binding.DIT_EINVAL, {}, {"k": None}), (binding.DIT_EINVAL, {}, {"idx": None}),
     (binding.DIT_EINVAL, {}, {"q": FAKE + 8}), (binding.DIT_EINVAL, {}, {"idx": FAKE + 2}),
