@@ -158,7 +158,9 @@ enum { DIT_EPI_FP8 = 8 };
  * Accumulation is f32.  bf16 and e4m3 outputs come from the 8-bit matrix cores,
  * which add a few neighbouring products in about 14 bits before they enter the
  * f32 sum (2e-5 in the 2-norm on normal data); f32 outputs are computed from
- * operands widened to bf16, at half that rate.
+ * operands widened to bf16, at half that rate.  Every scale byte is good for
+ * every output; f32 outputs of rows with bytes above 236, or whose sums pass 2^108,
+ * take up to ten times as long.
  * Errors: DIT_EINVAL (null pointers; bad flags: one of F32, FP8 and GATED_RES
  * at most; A, W, C, gate not 16-byte, scales not 4-byte, bias not 2-byte
  * aligned), DIT_ESHAPE (negative sizes, K < 1, K % 16, N % 8, lda or ldw below

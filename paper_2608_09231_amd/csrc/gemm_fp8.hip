@@ -13,7 +13,9 @@
 // and kept between far k; normal data come out 1.8e-5 off in the 2-norm, at
 // any K).  A bf16 or e4m3 output rounds by 2^-9 or 2^-4, a hundred times that.
 // An f32 output would carry it, so for those the operands are widened to bf16
-// with their scale in registers (exact) and multiplied by bf16 MFMAs (WIDE).
+// with their scale in registers and multiplied by bf16 MFMAs (WIDE).  That is exact
+// for scale bytes up to 236; a wave that meets a larger one, or whose sums overflow,
+// forms them anew (wide_sums).
 #include <algorithm>
 #include <type_traits>
 
@@ -147,12 +149,10 @@ __device__ __forceinline__ i32x8_t lds_frag(const char* lo, const char* hi) {
   return frag8(*(const i32x4_t*)lo, *(const i32x4_t*)hi);
 }
 
-// The fragment widened to bf16, times its row's scale: four 32-deep operands.
-// (The conversion reads the scale's exponent bits only: byte << 23 is 2^(byte - 127)
-// at either end of the range, too.)
-__device__ __forceinline__ void widen(const i32x8_t& f, int scale, bf16x8_t (&w)[4]) {
+// The fragment widened to bf16, times 2^(byte - 127): four 32-deep operands.
+__device__ __forceinline__ void widen(const i32x8_t& f, int byte, bf16x8_t (&w)[4]) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  const float s = __uint_as_float((uint32_t)(scale & 255) << 23);
+  const float s = __uint_as_float((uint32_t)(byte & 255) << 23);
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     uint32_t u[4];
@@ -163,6 +163,77 @@ __device__ __forceinline__ void widen(const i32x8_t& f, int scale, bf16x8_t (&w)
     }
     w[t] = __builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3]));
   }
+#endif
+}
+
+// Other than zero, e4m3 values are 2^-9 .. 448, and bf16 numbers are normal from 2^-126
+// to below 2^128.  Widened with a scale 2^UP times their own, values of bytes 0 .. 236 are
+// normal bf16 numbers, the 2^-126 that a block of zeros has included; the sums then
+// are 2^(2 UP) times too large.  (Without UP the least values of bytes below 3 lose bits.)
+constexpr int UP = 10, LAST_BYTE = 236;
+// Whether one of the lowest `valid` bytes lies above LAST_BYTE.  (A byte of ~x that is less
+// than n borrows into its top bit, which is clear; one of x that is not leaves it.)
+__device__ __forceinline__ uint32_t any_too_large(uint32_t x, int valid) {
+  const uint32_t last = valid >= 4 ? ~0u : (1u << (8 * max(valid, 0))) - 1u;
+  return (~x - 0x01010101u * (255 - LAST_BYTE)) & x & 0x80808080u & last;
+}
+
+// Sums over slices k0 .. k1 - 1 of 16 TM x 16 TN outputs from row m0 and column n0 on, for
+// any scale bytes: each block of K is summed without its scales (e4m3 is exact in bf16),
+// and the sum takes both at once.  Straight from memory, for waves that need it: 4096^3
+// takes 1.26 ms where all do, and 0.12 where none does.
+template <int TM, int TN>
+__device__ __forceinline__ void wide_sums(const Fp8Prob& P, int m0, int n0, int k0, int k1, f32x4_t (&acc)[TM][TN]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+  auto frag = [&](const uint8_t* row, int k) {  // the lane's chunks of the block from k on
+    const i32x4_t none = {0, 0, 0, 0};
+    const int a = k + 16 * lq, b = a + 64;
+    return frag8(a < P.K ? *(const i32x4_t*)(row + a) : none, b < P.K ? *(const i32x4_t*)(row + b) : none);
+  };
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int m = min(m0 + 16 * i + lr, P.M - 1), n = min(n0 + 16 * j + lr, P.N - 1);
+      f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int k = k0; k < k1; ++k) {
+        bf16x8_t a[4], w[4];
+        widen(frag(P.A + m * P.lda, 128 * k), 127, a);
+        widen(frag(P.W + n * P.ldw, 128 * k), 127, w);
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], w[t], x, 0, 0, 0);
+        const int sw = P.Ws[n * P.ldws + k];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int sa = P.As[min(m0 + 16 * i + 4 * lq + r, P.M - 1) * P.ldas + k];
+          sum[r] += sa == 255 || sw == 255 ? __uint_as_float(0x7fc00000u) : ldexpf(x[r], sa + sw - 254);
+        }
+      }
+      acc[i][j] = sum;
+    }
+#endif
+}
+
+// The end of a wave's sums of operands widened with 2^UP.  too_large: a lane met a byte above LAST_BYTE.
+template <int TM, int TN>
+__device__ __forceinline__ void finish_wide(const Fp8Prob& P, int m0, int n0, int k0, int k1, bool too_large,
+                                            f32x4_t (&acc)[TM][TN]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  f32x4_t zero = {};  // NaN where a sum is not finite, which the true one may still be
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        acc[i][j][r] *= 1.f / (1 << 2 * UP);
+        zero[r] = __builtin_fmaf(acc[i][j][r], 0.f, zero[r]);
+      }
+  const bool overflow = (zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.f;
+  if (__builtin_amdgcn_ballot_w64(too_large || overflow)) wide_sums<TM, TN>(P, m0, n0, k0, k1, acc);
 #endif
 }
 
@@ -393,10 +464,16 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
       snw1 = *(const int*)(swp + next);
     }
   };
-  auto spread_scales = [&]() {
+  uint32_t too_large = 0;
+  auto spread_scales = [&](int slices) {  // that are left
     if constexpr (KG == 2) {
       sna = __builtin_amdgcn_alignbyte(sna1, sna, k0 & 3);
       snw = __builtin_amdgcn_alignbyte(snw1, snw, k0 & 3);
+    }
+    if constexpr (WIDE) {  // (a byte past 255 carries into the next slice's, but is too large)
+      too_large |= any_too_large(sna, slices) | any_too_large(snw, slices);
+      sna += 0x01010101 * UP;
+      snw += 0x01010101 * UP;
     }
 #pragma unroll
     for (int f = 0; f < NF; ++f)
@@ -425,7 +502,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
   }();
 #pragma unroll
   for (int f = 0; f < NF; ++f) f0[f] = rd(0, f);
-  spread_scales();
+  spread_scales(k1 - k0);
   int u = 0;  // place of slice kt
   auto step = [&](int kt, i32x8_t(&f)[NF], i32x8_t(&fn)[NF], auto b_) {
     constexpr int B = decltype(b_)::value;
@@ -475,7 +552,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if constexpr (B == 3) spread_scales();
+    if constexpr (B == 3) spread_scales(k1 - kt - 1);
     u = un;
   };
   using std::integral_constant;
@@ -491,6 +568,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_k
   if (kt + 2 < k1) step(kt + 2, f0, f1, integral_constant<int, 2>{});
   if constexpr (KG == 2)
     for (int i = k1 - k0; i < half; ++i) barrier_no_fence();  // the first group may have one more step
+  if constexpr (WIDE) finish_wide<TM, TN>(P, m0 + wm * WM, n0 + 64 * wn, k0, k1, too_large != 0, acc);
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
   // The tile in LDS as slabs of ROWS rows x 128, one per wave, columns XOR 16
@@ -571,6 +649,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) loff[h] = lr * 128 + (((4 * h + lq) ^ ((lr >> 1) & 7)) << 4);
   f32x4_t acc[RB][2] = {};
+  int largest = 0;
 #pragma unroll
   for (int u = 0; u < ST; ++u) issue(s0 + u, u);
   for (int s = s0; s < s1; s += ST) {
@@ -591,12 +670,14 @@ __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
       issue(s + u + ST, u);
       if constexpr (WIDE) {
         bf16x8_t w[2][4];
-        widen(f[0], b[0], w[0]);
-        widen(f[1], b[1], w[1]);
+#pragma unroll
+        for (int i = 0; i < NF; ++i) largest = max(largest, b[i]);
+        widen(f[0], b[0] + UP, w[0]);
+        widen(f[1], b[1] + UP, w[1]);
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
           bf16x8_t a[4];
-          widen(f[2 + i], b[2 + i], a);
+          widen(f[2 + i], b[2 + i] + UP, a);
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -611,6 +692,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_small_kernel(Fp8Prob P) {
       }
     }
   }
+  if constexpr (WIDE) finish_wide<RB, 2>(P, m0, nw, s0, s1, largest > LAST_BYTE, acc);
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
   float(*part)[16 * RB][LD] = (float(*)[16 * RB][LD])smem;

@@ -301,6 +301,45 @@ def test_gemm_scales_across_the_range():
             check_gemm(M, N, K, out=out, operands=(a, w), bias=False)
 
 
+ENDS = [0, 254, 1, 247, 2, 246, 9, 10, 253, 120]     # least and largest scale bytes, and those beside bf16's range
+
+
+# one size for each kernel; f32: narrow tiles of one and two blocks of rows, K shared by two groups, tiles of 64 and 128 rows
+@pytest.mark.parametrize("out", ["bf16", "f32", "gated", "fp8"])
+@pytest.mark.parametrize("M,N,K", [(5, 128, 1168), (5, 9088, 1168), (9, 20096, 528), (40, 256, 1168),
+                                   (40, 4992, 528), (300, 2048, 1168), (900, 2048, 1296), (900, 2048, 1024),
+                                   (500, 10240, 528), (1920, 4352, 528), (4096, 2048, 1168), (4100, 4352, 1168)])
+def test_gemm_scales_at_the_ends(M, N, K, out):
+    """Blocks whose scale bytes are an end of the range in one operand and the opposite one in the other, so that
+    every product is an ordinary number though neither operand is one in bf16 or f32.  Every e4m3 value occurs, some
+    rows hold subnormals only, and some hold zeros where others hold the largest values."""
+    r = rng(M, N, K, 19)
+    nb = -(-K // 128)
+    ends = np.resize(ENDS, nb)
+
+    def rows(n, scale):
+        q = r.integers(0, 127, (n, K)) | 128 * r.integers(0, 2, (n, K))
+        q[1::4] &= 0x87                                # subnormals and zeros
+        s = np.broadcast_to(scale, (n, nb)).copy()
+        for b in range(nb):
+            q[3::8, 128 * b:128 * (b + 1)] &= 0x80 if b % 3 == 0 else 0xFF
+            s[3::8, b] = r.integers(0, 255) if b % 3 == 0 else s[3::8, b]
+        return q.astype(np.uint8), s.astype(np.uint8)
+
+    check_gemm(M, N, K, out=out, operands=(rows(M, ends), rows(N, 254 - ends)), bias=False)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 128, 400), (40, 256, 400), (900, 2048, 1296), (900, 2048, 400), (4096, 2048, 400)])
+def test_gemm_f32_sums_near_the_largest_number(M, N, K):
+    """Sums of up to 2^125, of blocks whose scale bytes lie on both sides of 236."""
+    r = rng(M, N, 20)
+    a, w = operand(r, M, K, spread=0), operand(r, N, K, spread=0)
+    nb = -(-K // 128)
+    a[1][:] = 127 + 100 + r.integers(0, 12, (M, 1)) + np.array([0, 0, 0, 1])[np.arange(nb) % 4]
+    w[1][:] = 127 + r.integers(-27, -23, (N, 1)) + 16 * (np.arange(N) % 3 == 0)[:, None]
+    check_gemm(M, N, K, out="f32", operands=(a, w), bias=False)
+
+
 @pytest.mark.parametrize("out", ["bf16", "f32", "fp8"])
 @pytest.mark.parametrize("M,N", [(4, 128), (300, 2048), (4100, 4352)])
 def test_gemm_nan_rows_stay_in_their_rows(M, N, out):
@@ -326,6 +365,21 @@ def test_gemm_scale_of_255_is_nan(M, N, out):
     r = rng(M, N, 4)
     a, w = operand(r, M, K), operand(r, N, K)
     a[1][2, 1] = w[1][5, 3] = 255
+    _, _, got, y, tol = run_gemm(M, N, K, out=out, operands=(a, w), bias=False)
+    assert np.isnan(got[2]).all() and np.isnan(got[:, 5]).all()
+    rest = np.ones(y.shape, bool)
+    rest[2], rest[:, 5] = False, False
+    assert (np.abs(got - y)[rest] <= tol[rest]).all()
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(4, 128, 400), (40, 256, 400), (900, 2048, 1296), (900, 2048, 400), (4096, 2048, 400)])
+def test_gemm_scale_of_255_is_nan_on_zeros(M, N, K, out):
+    r = rng(M, N, 6)
+    a, w = operand(r, M, K), operand(r, N, K)
+    a[0][2, 128:256], w[0][5, 384:] = 0, 0
+    a[1][2, 1] = w[1][5, 3] = 255
+    a[0][3], a[1][3] = 0, 0                             # a row of zeros
     _, _, got, y, tol = run_gemm(M, N, K, out=out, operands=(a, w), bias=False)
     assert np.isnan(got[2]).all() and np.isnan(got[:, 5]).all()
     rest = np.ones(y.shape, bool)
