@@ -212,7 +212,7 @@ typedef struct dit_sparse_shape {
  *   q [batch Lq, heads 128] (row stride ldq), k [batch Lk, kv_heads 128] (ldk)
  *   ws  device, dit_select_blocks_ws_bytes(s), 16-byte aligned
  * Errors: DIT_EINVAL (null pointers, alignment of 16 bytes, first outside [0,
- * topk]), DIT_ESHAPE (negative sizes; heads no multiple of kv_heads; topk < 1 or above 2^30;
+ * topk]), DIT_ESHAPE (negative sizes; heads no multiple of kv_heads; topk < 1; topk or Lk above 2^30;
  * strides below the row or no multiple of 8; more than 2^22 lists; more than
  * 16384 key blocks a sequence, 65535 batch * heads, or 2^24 - 1 lists and key
  * blocks of all key heads together), DIT_EHIP. */

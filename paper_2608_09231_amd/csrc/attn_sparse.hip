@@ -405,7 +405,7 @@ struct SparseArgs {
   bf16_t* o; int64_t ldo;
   const int32_t* idx;
   const int32_t* klen;
-  int Lq, Lk, heads, kv_heads, nqb, nkb, topk;
+  int Lq, Lk, heads, kv_heads, nqb, topk;
   int items, parts;   // the list of an item is shared by `parts` work-groups
   int rows;           // query rows of a piece in ws
   float* ws;
@@ -1274,7 +1274,6 @@ hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int
   P.idx = idx; P.klen = s.klen;
   P.Lq = s.Lq; P.Lk = s.Lk; P.heads = s.heads; P.kv_heads = s.kv_heads; P.topk = s.topk;
   P.nqb = blocks_of(s.Lq, QBLK);
-  P.nkb = blocks_of(s.Lk, KBLK);
   P.items = s.batch * s.heads * P.nqb;
   if (P.items == 0) return hipSuccess;
   P.parts = sparse_parts(s);

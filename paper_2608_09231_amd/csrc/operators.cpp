@@ -45,6 +45,8 @@ dit_status check_shape(const dit_sparse_shape* s) {
   if (!s) return component_fail(DIT_EINVAL, "null argument");
   if (s->batch < 0 || s->Lq < 0 || s->Lk < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads)
     return component_fail(DIT_ESHAPE, "bad attention shape");
+  // (rounded up to whole tiles, key positions stay inside 32 bits)
+  if (s->Lk > (1 << 30)) return component_fail(DIT_ESHAPE, "Lk must not pass 2^30");
   if (s->topk < 1 || s->topk > (1 << 30)) return component_fail(DIT_ESHAPE, "topk must lie in [1, 2^30]");
   const int64_t heads = (int64_t)s->batch * s->heads;  // (times 2^24 query blocks at most: inside 64 bits)
   if (s->heads > (1 << 20) || heads > 0x7fffffff || heads * blocks_of(s->Lq, DIT_SPARSE_QB) > (1 << 22))

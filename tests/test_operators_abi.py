@@ -136,6 +136,20 @@ def test_launches_past_their_limits_are_refused():
     assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, 1024, FAKE, 1024, 0, FAKE, FAKE, None) == binding.DIT_ESHAPE
 
 
+def test_sequences_past_their_limit_are_refused():
+    """Key counts whose rounding up to whole blocks would pass 32 bits."""
+    lib = binding.load()
+    for Lk in (2 ** 31 - 1, 2 ** 31 - 63, 2 ** 30 + 1):
+        for klen in (None, FAKE):
+            s = binding.SparseShapeC(2, 300, Lk, 4, 2, 5, klen)
+            assert lib.dit_attention_sparse_bf16(C.byref(s), FAKE, 512, FAKE, 256, FAKE, 256, FAKE, 512, FAKE, 0, FAKE,
+                                                 None) == binding.DIT_ESHAPE, Lk
+            assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, 512, FAKE, 256, 0, FAKE, FAKE, None) == binding.DIT_ESHAPE
+            assert lib.dit_attention_sparse_ws_bytes(C.byref(s)) == 0 and lib.dit_select_blocks_ws_bytes(C.byref(s)) == 0
+    s = binding.SparseShapeC(1, 300, 2 ** 30, 4, 2, 64, None)
+    assert lib.dit_attention_sparse_ws_bytes(C.byref(s)) > 0
+
+
 def test_select_workspace_holds_means_and_keys():
     means = 2 * 4 * 16 * 128 + 2 * 2 * 16 * 128      # in groups of 16 blocks
     assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * means
