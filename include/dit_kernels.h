@@ -214,8 +214,9 @@ typedef struct dit_sparse_shape {
  * Errors: DIT_EINVAL (null pointers, alignment of 16 bytes, first outside [0,
  * topk]), DIT_ESHAPE (negative sizes; heads no multiple of kv_heads; topk < 1; topk or Lk above 2^30;
  * strides below the row or no multiple of 8; more than 2^22 lists; more than
- * 16384 key blocks a sequence, 65535 batch * heads, or 2^24 - 1 lists and key
- * blocks of all key heads together), DIT_EHIP. */
+ * 16384 key blocks a sequence, 65535 batch * heads, 2^24 - 1 lists and key
+ * blocks of all key heads together, or 2^22 - 1 lists where a sequence has more than
+ * 4096 key blocks), DIT_EHIP. */
 size_t dit_select_blocks_ws_bytes(const dit_sparse_shape* s);
 dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                   int32_t first, int32_t* idx, void* ws, void* hip_stream);
@@ -227,7 +228,7 @@ dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int6
  * and in the product), sums and outputs are f32 until the one rounding of o.
  *   ws  device, dit_attention_sparse_ws_bytes(s) (may be 0: then NULL will do),
  *       16-byte aligned
- * Errors: as dit_select_blocks_bf16 (without `first` and the last three
+ * Errors: as dit_select_blocks_bf16 (without `first` and the last four
  * limits), strides of 2^22 or more, bad flags. */
 size_t dit_attention_sparse_ws_bytes(const dit_sparse_shape* s);
 dit_status dit_attention_sparse_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,

@@ -35,8 +35,9 @@ dit_status launched(hipError_t e) {
 // Strides and alignment of the scale bytes of rows of K values.
 bool scale_ok(const void* p, int64_t ld, int32_t K) { return aligned(p, 4) && ld % 4 == 0 && ld >= DIT_FP8_SCALE_LD(K); }
 
-// A launch has fewer than 2^32 threads: work-groups of 512 and of 256.
-constexpr int64_t kMaxGroups512 = ((int64_t)1 << 23) - 1, kMaxGroups256 = ((int64_t)1 << 24) - 1;
+// A launch has fewer than 2^32 threads: work-groups of 1024, 512 and 256.
+constexpr int64_t kMaxGroups1024 = ((int64_t)1 << 22) - 1, kMaxGroups512 = ((int64_t)1 << 23) - 1,
+                  kMaxGroups256 = ((int64_t)1 << 24) - 1;
 int64_t blocks_of(int64_t n, int64_t b) { return (n + b - 1) / b; }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 22;  // a tile's rows lie below 2^31 bytes from its first one
@@ -51,6 +52,18 @@ dit_status check_shape(const dit_sparse_shape* s) {
   const int64_t heads = (int64_t)s->batch * s->heads;  // (times 2^24 query blocks at most: inside 64 bits)
   if (s->heads > (1 << 20) || heads > 0x7fffffff || heads * blocks_of(s->Lq, DIT_SPARSE_QB) > (1 << 22))
     return component_fail(DIT_ESHAPE, "too many lists");
+  return DIT_OK;
+}
+
+// (past 4096 key blocks a list takes 1024 threads)
+dit_status check_select(const dit_sparse_shape* s) {
+  const dit_status st = check_shape(s);
+  if (st != DIT_OK) return st;
+  const int64_t heads = (int64_t)s->batch * s->heads, nkb = blocks_of(s->Lk, DIT_SPARSE_KB);
+  const int64_t lists = heads * blocks_of(s->Lq, DIT_SPARSE_QB);
+  if (nkb > 16384 || heads > 65535 || lists + (int64_t)s->batch * s->kv_heads * nkb > kMaxGroups256 ||
+      (nkb > 4096 && lists > kMaxGroups1024))
+    return component_fail(DIT_ESHAPE, "too many blocks or heads");
   return DIT_OK;
 }
 
@@ -134,7 +147,7 @@ size_t dit_select_blocks_ws_bytes(const dit_sparse_shape* s) {
 
 dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                   int32_t first, int32_t* idx, void* ws, void* hip_stream) {
-  TRY(check_shape(s));
+  TRY(check_select(s));
   const bool no_q = s->batch == 0 || s->Lq == 0, no_k = no_q || s->Lk == 0;
   if (!no_q && (!idx || !ws)) return component_fail(DIT_EINVAL, "null argument");
   if (!aligned(ws, 16) || !aligned(idx, 4) || !aligned(s->klen, 4))
@@ -142,10 +155,6 @@ dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int6
   TRY(check_rows(q, ldq, (int64_t)s->heads * 128, (int64_t)1 << 40, no_q));
   TRY(check_rows(k, ldk, (int64_t)s->kv_heads * 128, (int64_t)1 << 40, no_k));
   if (first < 0 || first > s->topk) return component_fail(DIT_EINVAL, "first must lie in [0, topk]");
-  const int64_t heads = (int64_t)s->batch * s->heads, nkb = blocks_of(s->Lk, DIT_SPARSE_KB);
-  if (nkb > 16384 || heads > 65535 ||
-      heads * blocks_of(s->Lq, DIT_SPARSE_QB) + (int64_t)s->batch * s->kv_heads * nkb > kMaxGroups256)
-    return component_fail(DIT_ESHAPE, "too many blocks or heads");
   return launched(dit::launch_select_blocks(*s, q, ldq, k, ldk, first, idx, ws, (hipStream_t)hip_stream, compute_units()));
 }
 

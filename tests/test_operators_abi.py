@@ -150,6 +150,16 @@ def test_sequences_past_their_limit_are_refused():
     assert lib.dit_attention_sparse_ws_bytes(C.byref(s)) > 0
 
 
+def test_selection_of_as_many_lists_as_threads_allow():
+    """Past 4096 key blocks a list takes 1024 threads: 2^22 lists are one too many."""
+    lib = binding.load()
+    for heads, Lq, Lk, bad in ((32768, 128 * 128, 64 * 4097, True), (1024, 128 * 4096, 64 * 4097, True),
+                               (32768, 128 * 128, 64 * 4096, False), (32768, 128 * 127, 64 * 4097, False)):
+        s = binding.SparseShapeC(1, Lq, Lk, heads, 1, 1, None)
+        st = lib.dit_select_blocks_bf16(C.byref(s), None, 128 * heads, None, 128, 0, FAKE, FAKE, None)
+        assert st == (binding.DIT_ESHAPE if bad else binding.DIT_EINVAL), (heads, Lq, Lk)
+
+
 def test_select_workspace_holds_means_and_keys():
     means = 2 * 4 * 16 * 128 + 2 * 2 * 16 * 128      # in groups of 16 blocks
     assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * means
