@@ -210,7 +210,7 @@ typedef struct dit_sparse_shape {
  * ascending order.  Blocks 0 .. first - 1 are taken whatever their product.
  * Where a sequence has fewer blocks than topk, the rest of the list is -1.
  *   q [batch Lq, heads 128] (row stride ldq), k [batch Lk, kv_heads 128] (ldk)
- *   ws  device, dit_select_blocks_ws_bytes(s), 16-byte aligned
+ *   ws  device, dit_select_blocks_ws_bytes(s) (0 for shapes that are refused), 16-byte aligned
  * Errors: DIT_EINVAL (null pointers, alignment of 16 bytes, first outside [0,
  * topk]), DIT_ESHAPE (negative sizes; heads no multiple of kv_heads; topk < 1; topk or Lk above 2^30;
  * strides below the row or no multiple of 8; more than 2^22 lists; more than

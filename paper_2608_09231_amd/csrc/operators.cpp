@@ -142,7 +142,7 @@ dit_status dit_gemm_fp8(const dit_gemm_fp8_desc* d, void* hip_stream) {
 }
 
 size_t dit_select_blocks_ws_bytes(const dit_sparse_shape* s) {
-  return check_shape(s) == DIT_OK ? dit::select_blocks_ws_bytes(*s) : 0;
+  return check_select(s) == DIT_OK ? dit::select_blocks_ws_bytes(*s) : 0;
 }
 
 dit_status dit_select_blocks_bf16(const dit_sparse_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,

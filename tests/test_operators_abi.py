@@ -160,6 +160,17 @@ def test_selection_of_as_many_lists_as_threads_allow():
         assert st == (binding.DIT_ESHAPE if bad else binding.DIT_EINVAL), (heads, Lq, Lk)
 
 
+def test_no_workspace_for_a_selection_that_is_refused():
+    """Else its caller would first ask for gigabytes."""
+    lib = binding.load()
+    for shape in (dict(Lq=128, Lk=2 ** 30, heads=1, batch=1), dict(Lq=128, Lk=64, heads=65536, batch=1),
+                  dict(Lq=1, Lk=16384 * 64, heads=8, batch=128)):
+        s = binding.sparse_shape(topk=1, **shape)
+        ld = 128 * shape["heads"]
+        assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, ld, FAKE, ld, 0, FAKE, FAKE, None) == binding.DIT_ESHAPE
+        assert lib.dit_select_blocks_ws_bytes(C.byref(s)) == 0
+
+
 def test_select_workspace_holds_means_and_keys():
     means = 2 * 4 * 16 * 128 + 2 * 2 * 16 * 128      # in groups of 16 blocks
     assert binding.select_blocks_ws_bytes(**SHAPE) == 8 * means
