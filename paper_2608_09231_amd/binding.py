@@ -371,25 +371,30 @@ def _esize(t):
 
 def _rows(t, name, rows, width, ld, esize):
     """Row stride of a device tensor that holds `rows` rows of `width` elements (None: a matrix's own; tensors of
-    other dimensions hold them back to back): the library reads them through a raw pointer."""
+    other dimensions hold them back to back): the library reads them through a raw pointer, and no further than the
+    tensor's own last element."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if _esize(t) != esize:
         raise ValueError(f"{name} must have elements of {esize} bytes and not be {t.dtype}")
-    shape = t.shape
+    shape, strides = t.shape, t.stride()
+    held = 0
     if ld is None and len(shape) == 2:
         have, wide = shape
-        step, unit = t.stride()
+        step, unit = strides
+        ld = step if have > 1 else max(step, width)
         if unit == 1 and have >= rows and wide >= width:
-            return step if have > 1 else max(step, width)
-        ld = step if have > 1 else width
-    elif ld is None:
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be a matrix, or contiguous, or come with its row stride")
-        ld = width
-    if len(shape) and shape[-1] > 1 and t.stride(-1) != 1:
+            return ld
+    else:
+        if ld is None:
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be a matrix, or contiguous, or come with its row stride")
+            ld = width
+        if 0 not in shape:
+            held = 1 + sum((n - 1) * step for n, step in zip(shape, strides))
+    if len(shape) and shape[-1] > 1 and strides[-1] != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if rows > 0 and (rows - 1) * ld + width > t.untyped_storage().nbytes() // esize - t.storage_offset():
+    if rows > 0 and (rows - 1) * ld + width > held:
         raise ValueError(f"{name} must hold {rows} rows of {width} elements with stride {ld}")
     return ld
 

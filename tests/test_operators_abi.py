@@ -241,6 +241,26 @@ def test_binding_refuses_strided_tensors_of_other_dimensions():
         binding._rows(_Device(torch.zeros(20)[::2]), "klen", 1, 10, None, 4)
 
 
+def test_binding_refuses_views_that_are_too_small():
+    """What a view shows is what a call may touch, however large its storage is."""
+    torch = pytest.importorskip("torch")
+    buf = torch.zeros(12, 768, dtype=torch.uint8)
+    for view, ld in ((buf[:10, :64], None), (buf[:3, :256], None), (buf[2:11, 256:512], None), (buf[:10, :64], 768),
+                     (buf[:3, :256], 768), (buf[:3].view(-1), None), (buf[:3].view(-1), 256), (buf[:2].view(2, 3, 256), None),
+                     (buf[:3, :256].view(3, 2, 128)[:, 0], None)):
+        with pytest.raises(ValueError, match="must hold 10 rows"):
+            binding._rows(_Device(view), "q", 10, 256, ld, 1)
+    for view, ld, want in ((buf[:10, :256], None, 768), (buf[1:12, 512:], None, 768), (buf[:10, :256], 768, 768),
+                           (buf[:4].view(-1)[:2560], None, 256), (buf[:4].view(12, 256)[:10], 256, 256),
+                           (buf[:5].view(5, 3, 256), None, 256)):
+        assert binding._rows(_Device(view), "q", 10, 256, ld, 1) == want
+    x = _Device(torch.zeros(64, 768, dtype=torch.bfloat16)[:, :128])
+    o = _Device(torch.zeros(64, 768, dtype=torch.bfloat16)[:, :64])
+    idx = _Device(torch.zeros(1, 1, 1, 1, dtype=torch.int32))
+    with pytest.raises(ValueError, match="o must hold 64 rows"):
+        binding.attention_sparse_bf16(x, x, x, o, idx, Lq=64, Lk=64, heads=1, topk=1)
+
+
 @pytest.mark.parametrize("dtype", ["float16", "float8_e5m2", "float8_e4m3fnuz", "bool"])
 def test_binding_refuses_types_that_would_be_misread(dtype):
     torch = pytest.importorskip("torch")
