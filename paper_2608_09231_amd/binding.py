@@ -357,32 +357,36 @@ def fp8_scale_ld(K: int) -> int:
     return (K + 511) // 512 * 4
 
 
-_ESIZE = {}  # bytes of an element by type; those whose values the library would misread: 0
+# what the library may read or write a type's elements as: 8-bit values and scales also as plain bytes, bf16 also as
+# its bits
+_E4M3, _E8M0, _BF16, _F32, _I32 = "e4m3 bytes", "E8M0 bytes", "bf16", "float32", "int32"
+_MEANINGS = {"torch.uint8": (_E4M3, _E8M0), "torch.int8": (_E4M3, _E8M0), "torch.float8_e4m3fn": (_E4M3,),
+             "torch.float8_e8m0fnu": (_E8M0,), "torch.bfloat16": (_BF16,), "torch.int16": (_BF16,),
+             "torch.uint16": (_BF16,), "torch.float32": (_F32,), "torch.int32": (_I32,)}
+_TYPES = {}  # by torch type: bytes of an element, meanings
 
 
-def _esize(t):
-    size = _ESIZE.get(t.dtype)
-    if size is None:
-        size = 0 if str(t.dtype) in ("torch.float16", "torch.bool", "torch.float8_e5m2", "torch.float8_e4m3fnuz",
-                                     "torch.float8_e5m2fnuz") else t.element_size()
-        _ESIZE[t.dtype] = size
-    return size
+def _type(t):
+    known = _TYPES[t.dtype] = (t.element_size(), _MEANINGS.get(str(t.dtype), ()))
+    return known
 
 
-def _rows(t, name, rows, width, ld, esize):
+def _rows(t, name, rows, width, ld, esize, meaning=None):
     """Row stride of a device tensor that holds `rows` rows of `width` elements (None: a matrix's own; tensors of
     other dimensions hold them back to back): the library reads them through a raw pointer, and no further than the
     tensor's own last element."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if _esize(t) != esize:
+    size, meanings = _TYPES.get(t.dtype) or _type(t)
+    if size != esize or not (meaning or meanings):
         raise ValueError(f"{name} must have elements of {esize} bytes and not be {t.dtype}")
-    shape, strides = t.shape, t.stride()
-    held = 0
+    if meaning and meaning not in meanings:
+        raise ValueError(f"{name} must be {meaning} and not {t.dtype}")
+    shape, strides, held = t.shape, t.stride(), 0
     if ld is None and len(shape) == 2:
-        have, wide = shape
-        step, unit = strides
-        ld = step if have > 1 else max(step, width)
+        (have, wide), (ld, unit) = shape, strides
+        if have <= 1:
+            ld = max(ld, width)
         if unit == 1 and have >= rows and wide >= width:
             return ld
     else:
@@ -444,14 +448,14 @@ class _Call:
 
 def quant_fp8(x, q, scale, *, M, K, ldx=None, ldq=None, lds=None, stream=None):
     """dit_quant_fp8: rows of x (torch.float32, else bf16 as torch.bfloat16 or int16) to e4m3 bytes q and
-    E8M0 scale bytes (uint8 or torch's 8-bit float types)."""
+    E8M0 scale bytes (uint8 or torch's type of the format)."""
     lib = load()
     f32 = x.element_size() == 4
     if f32 and not x.is_floating_point():
         raise ValueError("x must be float32 or bf16")
-    ldx = _rows(x, "x", M, K, ldx, 4 if f32 else 2)
-    ldq = _rows(q, "q", M, K, ldq, 1)
-    lds = _rows(scale, "scale", M, fp8_scale_ld(K), lds, 1)
+    ldx = _rows(x, "x", M, K, ldx, 4, _F32) if f32 else _rows(x, "x", M, K, ldx, 2, _BF16)
+    ldq = _rows(q, "q", M, K, ldq, 1, _E4M3)
+    lds = _rows(scale, "scale", M, fp8_scale_ld(K), lds, 1, _E8M0)
     with _Call(stream, x, q, scale) as call:
         _check(lib.dit_quant_fp8(x.data_ptr(), DTYPE_F32 if f32 else DTYPE_BF16, ldx, q.data_ptr(), ldq,
                                  scale.data_ptr(), lds, M, K, call.ptr))
@@ -460,20 +464,21 @@ def quant_fp8(x, q, scale, *, M, K, ldx=None, ldq=None, lds=None, stream=None):
 def gemm_fp8(A, a_scale, W, w_scale, bias, Cout, *, M, N, K, lda=None, ld_as=None, ldw=None, ld_ws=None, ldc=None,
              c_scale=None, ld_cs=None, flags=EPI_STORE, gate=None, rms_cols=0, gelu_from=None, gap_at=0, gap=0,
              stream=None):
-    """dit_gemm_fp8 on torch cuda tensors: 8-bit rows as uint8 or torch's 8-bit float types, bias and Cout as in
+    """dit_gemm_fp8 on torch cuda tensors: 8-bit rows as uint8 or torch's types of the formats, bias and Cout as in
     gemm_bf16 (Cout e4m3 with EPI_FP8, c_scale its scale bytes)."""
     lib = load()
-    lda, ldw = _rows(A, "A", M, K, lda, 1), _rows(W, "W", N, K, ldw, 1)
-    ld_as = _rows(a_scale, "a_scale", M, fp8_scale_ld(K), ld_as, 1)
-    ld_ws = _rows(w_scale, "w_scale", N, fp8_scale_ld(K), ld_ws, 1)
+    lda, ldw = _rows(A, "A", M, K, lda, 1, _E4M3), _rows(W, "W", N, K, ldw, 1, _E4M3)
+    ld_as = _rows(a_scale, "a_scale", M, fp8_scale_ld(K), ld_as, 1, _E8M0)
+    ld_ws = _rows(w_scale, "w_scale", N, fp8_scale_ld(K), ld_ws, 1, _E8M0)
     width = N + (gap if gap and gap_at < N else 0)
-    ldc = _rows(Cout, "Cout", M, width, ldc, 4 if flags & EPI_F32 else 1 if flags & EPI_FP8 else 2)
+    ldc = _rows(Cout, "Cout", M, width, ldc, *((4, _F32) if flags & EPI_F32 else (1, _E4M3) if flags & EPI_FP8
+                                               else (2, _BF16)))
     if bias is not None:
-        _rows(bias, "bias", 1, N, None, 2)
+        _rows(bias, "bias", 1, N, None, 2, _BF16)
     if gate is not None:
-        _rows(gate, "gate", 1, N, None, 4)
+        _rows(gate, "gate", 1, N, None, 4, _F32)
     if flags & EPI_FP8 and c_scale is not None:
-        ld_cs = _rows(c_scale, "c_scale", M, fp8_scale_ld(N), ld_cs, 1)
+        ld_cs = _rows(c_scale, "c_scale", M, fp8_scale_ld(N), ld_cs, 1, _E8M0)
     d = GemmFp8DescC(A.data_ptr(), lda, a_scale.data_ptr(), ld_as, W.data_ptr(), ldw, w_scale.data_ptr(), ld_ws,
                      bias.data_ptr() if bias is not None else None, Cout.data_ptr(), ldc,
                      c_scale.data_ptr() if c_scale is not None else None, ld_cs if ld_cs is not None else 0,
@@ -486,9 +491,7 @@ def gemm_fp8(A, a_scale, W, w_scale, bias, Cout, *, M, N, K, lda=None, ld_as=Non
 def sparse_shape(*, Lq, Lk, heads, topk, kv_heads=None, batch=1, klen=None) -> SparseShapeC:
     """dit_sparse_shape; klen: int32 cuda tensor [batch] or None."""
     if klen is not None:
-        _rows(klen, "klen", 1, batch, None, 4)
-        if klen.is_floating_point():
-            raise ValueError("klen must be int32")
+        _rows(klen, "klen", 1, batch, None, 4, _I32)
     return SparseShapeC(batch, Lq, Lk, heads, kv_heads if kv_heads is not None else heads, topk,
                         klen.data_ptr() if klen is not None else None)
 
@@ -514,7 +517,7 @@ def attention_sparse_ws_bytes(**shape) -> int:
 def _lists(idx, s):
     if not idx.is_cuda:
         raise ValueError("idx must be a device tensor")
-    if idx.element_size() != 4 or idx.is_floating_point():
+    if _I32 not in (_TYPES.get(idx.dtype) or _type(idx))[1]:
         raise ValueError("idx must be int32")
     if not idx.is_contiguous() or idx.numel() < s.batch * s.heads * -(-s.Lq // SPARSE_QB) * s.topk:
         raise ValueError("idx must be contiguous and hold every list")
@@ -525,8 +528,8 @@ def select_blocks_bf16(q, k, idx, *, first=0, ldq=None, ldk=None, ws=None, strea
     a workspace of torch's caching allocator."""
     lib = load()
     s = sparse_shape(**shape)
-    ldq = _rows(q, "q", s.batch * s.Lq, s.heads * 128, ldq, 2)
-    ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2)
+    ldq = _rows(q, "q", s.batch * s.Lq, s.heads * 128, ldq, 2, _BF16)
+    ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2, _BF16)
     _lists(idx, s)
     with _Call(stream, q, k, idx, shape.get("klen")) as call:
         w = call.workspace(ws, _ws_of("dit_select_blocks_ws_bytes", s) or 16, "ws")
@@ -539,10 +542,10 @@ def attention_sparse_bf16(q, k, v, o, idx, *, flags=0, ldq=None, ldk=None, ldv=N
     """dit_attention_sparse_bf16; idx as select_blocks_bf16 writes it, shape as in sparse_shape."""
     lib = load()
     s = sparse_shape(**shape)
-    ldq = _rows(q, "q", s.batch * s.Lq, s.heads * 128, ldq, 2)
-    ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2)
-    ldv = _rows(v, "v", s.batch * s.Lk, s.kv_heads * 128, ldv, 2)
-    ldo = _rows(o, "o", s.batch * s.Lq, s.heads * 128, ldo, 2)
+    ldq = _rows(q, "q", s.batch * s.Lq, s.heads * 128, ldq, 2, _BF16)
+    ldk = _rows(k, "k", s.batch * s.Lk, s.kv_heads * 128, ldk, 2, _BF16)
+    ldv = _rows(v, "v", s.batch * s.Lk, s.kv_heads * 128, ldv, 2, _BF16)
+    ldo = _rows(o, "o", s.batch * s.Lq, s.heads * 128, ldo, 2, _BF16)
     _lists(idx, s)
     with _Call(stream, q, k, v, o, idx, shape.get("klen")) as call:
         w = call.workspace(ws, _ws_of("dit_attention_sparse_ws_bytes", s), "ws")

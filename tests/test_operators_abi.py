@@ -269,6 +269,40 @@ def test_binding_refuses_types_that_would_be_misread(dtype):
         binding._rows(_Device(x), "x", 4, 128, None, x.element_size())
 
 
+def test_binding_refuses_types_of_another_meaning():
+    """Same size, other values: whole numbers for floats, scale bytes for e4m3 and the reverse."""
+    torch = pytest.importorskip("torch")
+
+    def t(dtype, *shape):
+        return _Device(torch.zeros(*shape, dtype=torch.uint8 if "float8" in dtype else getattr(torch, dtype)).view(
+            getattr(torch, dtype)))
+
+    good = dict(A="float8_e4m3fn", a_scale="float8_e8m0fnu", W="uint8", w_scale="int8", bias="bfloat16", Cout="float32",
+                gate=None)
+    sizes = dict(A=(16, 128), a_scale=(16, 4), W=(8, 128), w_scale=(8, 4), bias=(8,), Cout=(16, 8), gate=(8,))
+
+    def gemm(flags, **kw):
+        a = {n: d and t(d, *sizes[n]) for n, d in dict(good, **kw).items()}
+        gate = a.pop("gate")
+        binding.gemm_fp8(*a.values(), M=16, N=8, K=128, flags=flags, gate=gate)
+
+    for flags, kw in ((1, dict(Cout="int32")), (1, dict(Cout="uint32")), (1, dict(A="float8_e8m0fnu")),
+                      (1, dict(W="float8_e8m0fnu")), (1, dict(a_scale="float8_e4m3fn")), (1, dict(w_scale="float8_e4m3fn")),
+                      (2, dict(Cout="bfloat16", gate="int32")), (0, dict(Cout="float16")), (1, dict(bias="float16"))):
+        with pytest.raises(ValueError, match=next(iter(kw)) if len(kw) == 1 else "gate"):
+            gemm(flags, **kw)
+    x, q, s = t("bfloat16", 16, 128), t("uint8", 16, 128), t("uint8", 16, 4)
+    with pytest.raises(ValueError, match="^q must"):
+        binding.quant_fp8(x, t("float8_e8m0fnu", 16, 128), s, M=16, K=128)
+    with pytest.raises(ValueError, match="^scale must"):
+        binding.quant_fp8(x, q, t("float8_e4m3fn", 16, 4), M=16, K=128)
+    for dtype in ("uint32", "complex32", "float32"):
+        with pytest.raises(ValueError, match="idx must be int32"):
+            binding.select_blocks_bf16(x, x, t(dtype, 1), Lq=16, Lk=16, heads=1, topk=1)
+        with pytest.raises(ValueError, match="klen must be int32"):
+            binding.select_blocks_bf16(x, x, t("int32", 1), Lq=16, Lk=16, heads=1, topk=1, klen=t(dtype, 1))
+
+
 def test_nothing_to_write_needs_no_pointers():
     lib = binding.load()
     assert lib.dit_quant_fp8(None, 1, 256, None, 256, None, 4, 0, 256, None) == binding.DIT_OK
