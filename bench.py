@@ -137,21 +137,40 @@ def cpu_baseline(w, rows=2048, q_sample=256):
     }
 
 
-def kernel_traffic(kernel, workload, source):
-    """HBM-side bytes per launch of `kernel` from the committed rocprofv3
-    counter summary profiles/<kernel>_<workload>_hbm_traffic.md, or None when
-    it does not cover this workload or `source` changed since the counters
-    were taken."""
+def source_checksum(source):
+    """Checksum of the device code of csrc/`source`: the file and the headers
+    beside it that it includes, also through one another (not kernels.h,
+    which only declares the launchers)."""
     import hashlib
     import re
 
+    csrc = os.path.join(ROOT, "paper_2608_09231_amd", "csrc")
+    files, todo = {}, [source]
+    while todo:
+        name = todo.pop()
+        if name not in files:
+            with open(os.path.join(csrc, name), "rb") as f:
+                files[name] = f.read()
+            todo += [h.decode() for h in re.findall(rb'#include "([^"/]+)"', files[name]) if h != b"kernels.h"]
+    h = hashlib.sha256()
+    for name in [source] + sorted(files.keys() - {source}):
+        h.update(files[name])
+    return h.hexdigest()[:16]
+
+
+def kernel_traffic(kernel, workload, source):
+    """HBM-side bytes per launch of `kernel` from the committed rocprofv3
+    counter summary profiles/<kernel>_<workload>_hbm_traffic.md, or None when
+    it does not cover this workload or the code of `source` changed since the
+    counters were taken."""
+    import re
+
     path = os.path.join(ROOT, "profiles", f"{kernel}_{workload}_hbm_traffic.md")
-    src = os.path.join(ROOT, "paper_2608_09231_amd", "csrc", source)
     try:
         txt = open(path).read()
         m = re.search(r"```json\n(.*?)\n```", txt, flags=re.S)
         data = json.loads(m.group(1))
-        sha = hashlib.sha256(open(src, "rb").read()).hexdigest()[:16]
+        sha = source_checksum(source)
     except (OSError, AttributeError, ValueError):
         return None
     if data.get("source_sha256_16") != sha:
