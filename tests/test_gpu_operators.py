@@ -289,6 +289,15 @@ def test_gemm_norm_gelu_and_gap(M, N, K, out):
     check_gemm(M, N, K, out=out, act="silu", seed=3)
 
 
+# tiles of 256 x 128 and 128 x 128, f32 tiles of 64 rows whose K is not shared
+@pytest.mark.parametrize("M,N,K,out", [(500, 10240, 400, "bf16"), (1913, 4352, 656, "bf16"), (70, 13824, 656, "f32")])
+def test_gemm_norm_gelu_and_gap_of_one_round(M, N, K, out):
+    check_gemm(M, N, K, out=out, rms_cols=256, gelu_from=384, gap_at=384, gap=128, seed=1)
+    check_gemm(M, N, K, out=out, rms_cols=128, gelu_from=204, gap_at=140, gap=12, pad=8 - (N + 12) % 8, seed=2)
+    check_gemm(M, N, K, out=out, act="silu", seed=3)
+    check_gemm(M, N, K, out=out, rms_cols=N, seed=4)
+
+
 def test_gemm_scales_across_the_range():
     """Row scales over 2^-120 .. 2^120 whose products stay in range, and a smallest and a largest scale byte."""
     r = rng(9)
@@ -602,6 +611,51 @@ def test_rows_far_apart(Lq, heads, topk):
         del q, k, v, o, t
     torch.cuda.empty_cache()
     assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
+
+
+def guarded(torch, nbytes):
+    """A workspace of NaNs and the bytes behind it, which no call may change."""
+    buf = torch.full((nbytes + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    return buf[:nbytes], buf[nbytes:]
+
+
+@pytest.mark.parametrize("Lq,Lk,topk,klen", [(1, 63, 2, None), (300, 5000, 9, [5000, 4030]), (2049, 9000, 30, [1, 9000]),
+                                             (130, 40000, 600, None), (130, 70000, 64, [69999, 0])])
+def test_selection_in_a_workspace_of_its_size(Lq, Lk, topk, klen):
+    """Block counts that leave groups of 16 unfilled: what was never written is NaN."""
+    torch = torch_cuda()
+    r = rng(Lq, Lk, 61)
+    shape = shape_of(Lq, Lk, 4, topk, kv_heads=2, batch=len(klen or [0]), klen=klen)
+    qb, q = tokens(r, shape["batch"] * Lq, 4)
+    kb, k = tokens(r, shape["batch"] * Lk, 2)
+    on = on_device(torch, shape)
+    ws, rest = guarded(torch, binding.select_blocks_ws_bytes(**on))
+    idx = torch.empty(shape["batch"], 4, -(-Lq // 128), topk, dtype=torch.int32, device="cuda")
+    binding.select_blocks_bf16(dev(torch, qb), dev(torch, kb), idx, first=1, ws=ws, **on)
+    assert (rest == 0xFF).all()
+    np.testing.assert_array_equal(idx.cpu().numpy(), ref.select(q, k, first=1, **shape))
+
+
+@pytest.mark.parametrize("bounded", [False, True])
+@pytest.mark.parametrize("Lq,heads,topk", [(1, 2, 200), (1, 30, 40), (17, 3, 60), (33, 4, 30), (128, 9, 12), (300, 5, 100)])
+def test_attention_in_a_workspace_of_its_size(Lq, heads, topk, bounded):
+    torch = torch_cuda()
+    r = rng(Lq, heads, 62)
+    shape = shape_of(Lq, 4097, heads, topk, kv_heads=1)
+    qb, q = tokens(r, Lq, heads)
+    kb, k = tokens(r, 4097, 1)
+    vb, v = tokens(r, 4097, 1)
+    nqb = -(-Lq // 128)
+    idx = r.integers(-1, 65, (1, heads, nqb, topk)).astype(np.int32)
+    idx[0, 0, 0, topk // 4:] = -1                      # pieces of a list that hold no entry
+    n = binding.attention_sparse_ws_bytes(**shape)
+    assert n > 0
+    ws, rest = guarded(torch, n)
+    o = torch.empty(Lq, heads * 128, dtype=torch.int16, device="cuda")
+    binding.attention_sparse_bf16(dev(torch, qb), dev(torch, kb), dev(torch, vb), o, dev(torch, idx), ws=ws,
+                                  flags=binding.ATTN_BOUNDED_LOGITS if bounded else 0, **shape)
+    assert (rest == 0xFF).all()
+    check_attention(host_bf16(o), q, k, v, idx, shape)
 
 
 def test_lengths_of_zero():
