@@ -50,7 +50,8 @@ enum {
  * depend on other calls; only with no device memory left does it run whole
  * tiles instead (the same result up to the rounding of f32 sums).
  * Errors: DIT_EINVAL (null pointers, bad flags), DIT_ESHAPE (K % 8, lda or
- * ldw < K, ldc too small, gap < 0, rms_cols not a multiple of 128), DIT_EHIP. */
+ * ldw < K, ldc too small, gap < 0, an output row of more than 2^30 columns with
+ * its gap, rms_cols not a multiple of 128), DIT_EHIP. */
 typedef struct dit_gemm_desc {
   const void* A; int64_t lda;
   const void* W; int64_t ldw;
@@ -166,10 +167,10 @@ enum { DIT_EPI_FP8 = 8 };
  * aligned), DIT_ESHAPE (negative sizes, K < 1, K % 16, N % 8, lda or ldw below
  * K, above 2^22 or no multiple of 16, the scale strides, ldc below the written
  * row or no multiple of 8, rms_cols no multiple of 128 or above N, gelu_from < N
- * no multiple of 4, gap or gap_at no multiple of 4 or negative; with
- * DIT_EPI_FP8: N or gelu_from < N no multiple of 128, ldc no multiple of 16, a
- * gap; with rms_cols: N no multiple of 128; ceil(M / 64) * ceil(N / 128) of 2^23
- * or more), DIT_EHIP. */
+ * no multiple of 4, gap or gap_at no multiple of 4 or negative, an output row of
+ * more than 2^30 columns with its gap; with DIT_EPI_FP8: N or gelu_from < N no
+ * multiple of 128, ldc no multiple of 16, a gap; with rms_cols: N no multiple of
+ * 128; ceil(M / 64) * ceil(N / 128) of 2^23 or more), DIT_EHIP. */
 typedef struct dit_gemm_fp8_desc {
   const void* A; int64_t lda;
   const void* a_scale; int64_t ld_as;

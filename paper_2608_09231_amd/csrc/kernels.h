@@ -8,6 +8,10 @@
 
 namespace dit {
 
+// Widest output row of a product with a column gap: column indexes, those of a tile's
+// columns past the last one included, are 32 bits wide.
+constexpr int64_t kMaxGapWidth = (int64_t)1 << 30;
+
 struct GemmArgs {
   const void* A; int64_t lda;
   const void* W; int64_t ldw;

@@ -126,8 +126,9 @@ dit_status dit_gemm_fp8(const dit_gemm_fp8_desc* d, void* hip_stream) {
   if (gelu && (d->gelu_from < 0 || d->gelu_from % 4)) return component_fail(DIT_ESHAPE, "gelu_from must be a multiple of 4");
   if (d->rms_cols < 0 || d->rms_cols % 128 || d->rms_cols > d->N || (d->rms_cols && d->N % 128))
     return component_fail(DIT_ESHAPE, "rms_cols and N must be multiples of 128");
-  if (d->ldc < (int64_t)d->N + (gap && d->gap_at < d->N ? d->gap : 0) || d->ldc % 8)
-    return component_fail(DIT_ESHAPE, "bad output stride");
+  const int64_t width = (int64_t)d->N + (gap && d->gap_at < d->N ? d->gap : 0);
+  if (gap && width > dit::kMaxGapWidth) return component_fail(DIT_ESHAPE, "output row too wide");
+  if (d->ldc < width || d->ldc % 8) return component_fail(DIT_ESHAPE, "bad output stride");
   if (fp8 && (d->N % 128 || (gelu && d->gelu_from % 128) || gap || d->ldc % 16 || !scale_ok(d->c_scale, d->ld_cs, d->N)))
     return component_fail(DIT_ESHAPE, "bad shape of the 8-bit output");
   if (blocks_of(d->M, 64) * blocks_of(d->N, 128) > kMaxGroups512) return component_fail(DIT_ESHAPE, "too many outputs");

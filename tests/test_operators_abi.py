@@ -136,6 +136,20 @@ def test_launches_past_their_limits_are_refused():
     assert lib.dit_select_blocks_bf16(C.byref(s), FAKE, 1024, FAKE, 1024, 0, FAKE, FAKE, None) == binding.DIT_ESHAPE
 
 
+def test_output_columns_past_their_limit_are_refused():
+    """A column index is 32 bits wide, its gap included."""
+    lib = binding.load()
+    for N, gap_at, gap in ((512, 0, 2 ** 31 - 8), (512, 508, 2 ** 30 - 508), (2 ** 20, 2 ** 19, 2 ** 30)):
+        d = gemm_desc(M=1, N=N, ldc=1 << 40, gap_at=gap_at, gap=gap, gelu_from=N)
+        assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_ESHAPE, (N, gap)
+        b = binding.GemmDescC(A=FAKE, lda=256, W=FAKE, ldw=256, bias=None, C=FAKE, ldc=1 << 40, M=1, N=N, K=256, flags=0,
+                              gate=None, rms_cols=0, gelu_from=N, gap_at=gap_at, gap=gap)
+        assert lib.dit_gemm_bf16(C.byref(b), None) == binding.DIT_ESHAPE, (N, gap)
+    # a gap that no column reaches is none
+    d = gemm_desc(M=0, gap_at=512, gap=2 ** 31 - 8)
+    assert lib.dit_gemm_fp8(C.byref(d), None) == binding.DIT_OK
+
+
 def test_sequences_past_their_limit_are_refused():
     """Key counts whose rounding up to whole blocks would pass 32 bits."""
     lib = binding.load()
