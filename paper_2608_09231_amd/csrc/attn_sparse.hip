@@ -39,7 +39,7 @@ __device__ __forceinline__ int keys_of(const int32_t* klen, int z, int Lk) {
 // heads first, so that those in flight together read whole rows; where 8 divides
 // the heads, a head's blocks then share an XCD, whose L2 puts the lines of their
 // 16-byte pieces together (the rows pass it by).  Bound by the copy rate: 32760
-// tokens, 40 heads (674 MB) 127 us, 5.3 TB/s; rows through L2 139 us, blocks first 154 us.
+// tokens, 40 heads (674 MB) 129 us, 5.2 TB/s; rows through L2 139 us, blocks first 154 us.
 __host__ __device__ __forceinline__ int64_t mean_doubles(int blocks) { return (int64_t)((blocks + 15) / 16) * 16 * D; }
 struct MeanArgs {
   const bf16_t* x[2]; int64_t ld[2];
@@ -273,7 +273,7 @@ __device__ __forceinline__ void topk_row(const uint64_t (&key)[R], int32_t* __re
 // means in registers, their keys in LDS.  NW waves take 16 key blocks in turn (f64
 // 16x16x4 MFMAs), then 16 / NW rows each.
 //
-// 32760 tokens, 40 heads: 54 us, in which a CU's f64 MFMAs alone take 20, the means
+// 32760 tokens, 40 heads: 57 us, in which a CU's f64 MFMAs alone take 20, the means
 // from L2 (640 work-groups of 16 query blocks against 512 key blocks) about as long and the
 // search the rest, one after the other within a work-group.
 template <int R, int NW>
@@ -510,12 +510,16 @@ __device__ __forceinline__ void store_rows(const SparseArgs& P, const f32x4_t (&
 // probabilities from one to the other in registers).  V^T fragments are read from
 // the row-major tile by transposing LDS reads, so no transposed copy of V is made.
 //
+// Probabilities are rounded to bf16, the type that the second product takes beside V, by at
+// most 2^-8 of each and of either sign, as the output is in its turn.  The sum takes the
+// rounded values, so that the weights add up to one.
+//
 // TP = 1: two work-groups per CU, one's softmax beside the other's products.  TP =
 // 2: one per CU, for launches that leave no second one; the groups take tiles in
 // turn, and their outputs meet in LDS.
 //
 // A tile's score product, softmax and second product follow one another in every
-// wave: 192 lists of 9 blocks on as many CUs take 18.6 us (0.38 PFLOP/s), the MFMAs busy
+// wave: 192 lists of 9 blocks on as many CUs take 19 - 21 us (0.35 PFLOP/s), the MFMAs busy
 // in 0.22 of the cycles and LDS in 0.18; 10240 lists of 52, two work-groups per CU,
 // 2.3 ms (0.97).  V's rows in an order without bank conflicts (a third of the LDS
 // cycles) change nothing.
@@ -714,7 +718,7 @@ __global__ __launch_bounds__(256 * TP, 2) void attn_sparse_kernel(SparseArgs P) 
 // of K and V from memory.  Each of four waves takes all queries and its own share
 // of the list, 32 keys at a time in its own two buffers of LDS: no wave waits for
 // another until their four parts meet at the end.  One token, 40 heads, 64 blocks (84
-// MB): 17 us and 2.4 to join the pieces, 4.3 TB/s; 200 blocks 5.6 TB/s.
+// MB): 17 us and 2.5 - 4 to join the pieces, 4.3 TB/s; 200 blocks 5.6 TB/s.
 template <bool BOUNDED, int NG>
 __global__ __launch_bounds__(256, 1) void attn_few_kernel(SparseArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)

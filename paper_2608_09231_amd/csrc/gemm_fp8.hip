@@ -408,7 +408,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_ring_kernel(Fp8Prob P) {
 // with two slices each lose: 1333 x 1000 x 2320 13 -> 17 us.
 //
 // KG = 2: two groups of four waves with rings of their own take the halves of K;
-// their sums meet in LDS.  1333 x 1000 x 2320, f32: 16 us (0.38 PFLOP/s), a chain of
+// their sums meet in LDS.  1333 x 1000 x 2320, f32: 17 us (0.37 PFLOP/s), a chain of
 // ten slices on 168 CUs.
 template <int BM, int KIND, bool WIDE, int KG = 1>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256 * KG, 2) void gemm_fp8_tile_kernel(Fp8Prob P) {
@@ -848,7 +848,7 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t s, int n_cu) {
   if (f32) {
     // One work-group per CU: two groups of waves, one's widening beside the other's
     // products, where either has some slices.  256 x 5120 x 5120 31.5 -> 24.6 us,
-    // 1333 x 1000 x 2320 18.6 -> 16 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
+    // 1333 x 1000 x 2320 18.6 -> 16.8 (512 x 4096 x 528: 10.1 and 10.3).  It gives bf16 outputs nothing
     // (256 x 5120 x 5120 18.6 and 18.4 us, 1333 x 1000 x 2320 12.8 and 13.5).
     if (tiles(64, 128) <= n_cu && g.K > 1024) return go(gemm_fp8_tile_kernel<64, EPI_K_ANY, true, 2>, 64, 128, 512);
     if (cost({64, 128, 2, 1.02}) <= cost({128, 128, 2, 1.78}))
