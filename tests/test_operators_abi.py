@@ -283,6 +283,7 @@ def test_binding_refuses_types_that_would_be_misread(dtype):
         binding._rows(_Device(x), "x", 4, 128, None, x.element_size())
 
 
+@pytest.mark.filterwarnings("ignore:ComplexHalf")
 def test_binding_refuses_types_of_another_meaning():
     """Same size, other values: whole numbers for floats, scale bytes for e4m3 and the reverse."""
     torch = pytest.importorskip("torch")
