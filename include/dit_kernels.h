@@ -236,6 +236,168 @@ dit_status dit_attention_sparse_bf16(const dit_sparse_shape* s, const void* q, i
                                      const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx,
                                      int32_t flags, void* ws, void* hip_stream);
 
+/* ---- a prompt encoder's operators: 4-bit products, rotary positions, packed
+ * attention ----
+ *
+ * These calls only enqueue their work, as those above; the same holds of their
+ * workspaces, of sizes of zero and of the current device.
+ *
+ * 4-bit rows.  A row of K values (K % 32 == 0) is held as K / 2 bytes of e2m1
+ * (OCP: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; two a byte, the first in
+ * the low half) and one scale byte (E8M0: 2^(byte - 127)) for each 32 of them:
+ * x = e2m1 * scale.  Scale bytes of row m start at scale + m * lds; lds is a
+ * multiple of 4 and at least DIT_FP4_SCALE_LD(K), scale is 4-byte aligned (bytes
+ * past the last block's are read with their neighbours, and not used). */
+#define DIT_FP4_SCALE_LD(K) ((((int64_t)(K) + 127) / 128) * 4)
+
+/* q, scale = 4-bit rows of x: per block of 32 the least scale with max |x| <= 6 *
+ * scale, e2m1(x / scale) rounded to nearest even.  A block of zeros gets scale byte
+ * 0; one that holds a NaN or an infinity gets scale byte 255 (NaN).
+ *   x      device, x_dtype DIT_DTYPE_BF16 or DIT_DTYPE_F32 [M, K], row stride ldx
+ *   q      device [M, K / 2] bytes, row stride ldq bytes
+ * Errors: DIT_EINVAL (null pointers, bad type, x or q not 16-byte or scale not
+ * 4-byte aligned), DIT_ESHAPE (negative sizes, K % 32, a stride below the row
+ * or, in bytes, no multiple of 16, lds, K above 2^30, M * ceil(K / 1024) above 2^26 - 4), DIT_EHIP. */
+dit_status dit_quant_fp4(const void* x, int32_t x_dtype, int64_t ldx, void* q, int64_t ldq, void* scale,
+                         int64_t lds, int32_t M, int32_t K, void* hip_stream);
+
+/* y = the values of 4-bit rows, bf16 or f32 [M, K], row stride ldy: exact but for
+ * bf16 or f32 overflow (infinities).  Arguments and errors as dit_quant_fp4's (y for x). */
+dit_status dit_dequant_fp4(const void* q, int64_t ldq, const void* scale, int64_t lds, void* y, int32_t y_dtype,
+                           int64_t ldy, int32_t M, int32_t K, void* hip_stream);
+
+/* Epilogue flag of dit_gemm_fp4 beside those of dit_gemm_bf16: C and c_scale =
+ * the 4-bit rows of acc + bias (after norm, GELU, SiLU). */
+enum { DIT_EPI_FP4 = 16 };
+
+/* C = epilogue(A . W^T + bias) on 4-bit rows, with the epilogues of
+ * dit_gemm_bf16 (same meaning of bias, gate, rms_cols, gelu_from, gap_at, gap).
+ *   A, a_scale  4-bit rows [M, K], row strides lda, ld_as bytes
+ *   W, w_scale  4-bit rows [N, K], row strides ldw, ld_ws bytes
+ *   C           bf16, f32 (DIT_EPI_F32) or 4-bit (DIT_EPI_FP4), row stride ldc:
+ *               elements, bytes with DIT_EPI_FP4
+ *   c_scale     DIT_EPI_FP4 only: scale bytes of C, row stride ld_cs
+ * Accumulation is f32 (products of 4-bit values are exact, and so is their sum
+ * in a block).  Products and sums past f32's range are infinities, products below 2^-149 zeros.
+ * Errors: DIT_EINVAL (null pointers; bad flags: one of F32, FP4 and GATED_RES
+ * at most; A, W, C, gate not 16-byte, scales not 4-byte, bias not 2-byte
+ * aligned), DIT_ESHAPE (negative sizes, K < 1, K % 32, N % 8, lda or ldw below
+ * K / 2, above 2^22 or no multiple of 16, the scale strides (above 2^22, too), ldc below the written
+ * row or no multiple of 8, rms_cols no multiple of 128 or above N, gelu_from < N
+ * no multiple of 4, gap or gap_at no multiple of 4 or negative, an output row of
+ * more than 2^30 columns with its gap; with DIT_EPI_FP4: N no multiple of 32,
+ * gelu_from < N no multiple of 128, ldc no multiple of 16, a gap; with rms_cols: N no multiple of
+ * 128; ceil(M / 64) * ceil(N / 128) of 2^23 or more), DIT_EHIP. */
+typedef struct dit_gemm_fp4_desc {
+  const void* A; int64_t lda;
+  const void* a_scale; int64_t ld_as;
+  const void* W; int64_t ldw;
+  const void* w_scale; int64_t ld_ws;
+  const void* bias;
+  void* C; int64_t ldc;
+  void* c_scale; int64_t ld_cs;
+  const float* gate;
+  int32_t M, N, K;
+  int32_t flags;
+  int32_t rms_cols;
+  int32_t gelu_from;
+  int32_t gap_at, gap;
+} dit_gemm_fp4_desc;
+
+dit_status dit_gemm_fp4(const dit_gemm_fp4_desc* d, void* hip_stream);
+
+/* Rotary positions: the pairs of a head's first `rot` values are turned by an
+ * angle that grows with the token's position. */
+enum {
+  DIT_ROTARY_HALF = 0,        /* pair i: values i and i + rot / 2 */
+  DIT_ROTARY_INTERLEAVED = 1  /* pair i: values 2 i and 2 i + 1   */
+};
+enum {
+  DIT_ROTARY_PLAIN = 0,    /* f_i = base^(-i / pairs)                                          */
+  DIT_ROTARY_LINEAR = 1,   /* f_i / factor: positions squeezed into the trained range           */
+  DIT_ROTARY_BASE = 2,     /* base' = base * factor^(pairs / (pairs - 1)): the slowest pair      */
+                           /* turns `factor` times slower, the fastest as before                */
+  DIT_ROTARY_PARTS = 3     /* by turns t_i = context f_i / 2 pi over the trained context: f_i    */
+                           /* / factor below 1 turn, f_i above 32, in proportion to t_i between */
+};
+/* freq[0 .. pairs - 1] = radians per position (host, double), *scale = the factor
+ * on cosine and sine: 0.1 ln(factor) + 1 with DIT_ROTARY_PARTS, else 1.  A host
+ * function; its result is the program's to keep and copy to the device.
+ * Errors: DIT_EINVAL (null pointers, bad method, base or factor not positive and finite, PARTS with context not
+ * positive and finite), DIT_ESHAPE (pairs < 0, BASE with pairs of 1). */
+dit_status dit_rotary_freqs(int32_t pairs, double base, int32_t method, double factor, double context, double* freq,
+                            double* scale);
+
+/* y = x with every pair (a, b) of a head's first rot values replaced by
+ * scale * (a cos t - b sin t, b cos t + a sin t); the head's other values are copied.
+ * Pair i's angle is t = pos[axis][row] * freq[i], axis the one whose pairs i falls in:
+ * the first pairs[0] pairs belong to axis 0, the next pairs[1] to axis 1, and so on.
+ * Angles are formed and reduced in double, so that far positions lose nothing.
+ * Negative positions turn back.
+ *   x, y   device, dtype DIT_DTYPE_BF16 or DIT_DTYPE_F32 [rows, heads * head_dim],
+ *          row strides ldx, ldy; y == x (with ldy == ldx) rotates in place; other
+ *          overlaps of the rows' ranges are not allowed (the ranges of two column
+ *          ranges of one matrix do not overlap where the columns do not)
+ *   pos    device int32, axis a's rows at pos + a * ldpos
+ *   freq   device double [rot / 2]
+ * Errors: DIT_EINVAL (null pointers; bad type or layout; x, y not 16-byte, freq not
+ * 8-byte, pos not 4-byte aligned; scale not finite; x and y overlap), DIT_ESHAPE
+ * (negative sizes; rows of 2^24 or more; head_dim < 8, no multiple of 8 or above 512; rot odd, negative or above head_dim; axes outside
+ * 1 .. DIT_ROTARY_AXES; pairs negative or not rot / 2 together; heads * head_dim above 2^30; strides below
+ * the row or, in bytes, no multiple of 16; ldpos below rows with several axes), DIT_EHIP. */
+enum { DIT_ROTARY_AXES = 4 };
+typedef struct dit_rotary_desc {
+  const void* x; int64_t ldx;
+  void* y; int64_t ldy;
+  const int32_t* pos; int64_t ldpos;
+  const double* freq;
+  int32_t dtype;
+  int32_t rows, heads, head_dim, rot;
+  int32_t layout;
+  int32_t axes;
+  int32_t pairs[DIT_ROTARY_AXES];
+  float scale;
+} dit_rotary_desc;
+
+dit_status dit_rotary(const dit_rotary_desc* d, void* hip_stream);
+
+/* Attention flag of dit_attention_packed_bf16 beside DIT_ATTN_BOUNDED_LOGITS. */
+enum {
+  /* Query i of a sequence's n sees its first m - n + 1 + i keys of m: the last
+   * query sees every key, and with fewer keys than queries the first see none. */
+  DIT_ATTN_CAUSAL = 2
+};
+
+/* Packed sequences: sequence z's queries are rows qoff[z] .. qoff[z + 1] - 1 of q and
+ * o, its keys rows koff[z] .. koff[z + 1] - 1 of k and v, or the first klen[z] of
+ * these (a cache whose slots are filled so far).  Query head h reads key head h /
+ * (heads / kv_heads).  The offsets are read on the device and clamped there: to [0, Tq] and [0,
+ * Tk], and not to fall from one to the next; klen to the slot. */
+typedef struct dit_packed_shape {
+  int32_t batch;            /* sequences */
+  int32_t Tq, Tk;           /* rows of q and o, rows of k and v */
+  int32_t heads, kv_heads;
+  const int32_t* qoff;      /* device [batch + 1] */
+  const int32_t* koff;      /* device [batch + 1] */
+  const int32_t* klen;      /* device [batch], or NULL: every row of the slot */
+} dit_packed_shape;
+
+/* o = softmax(q k^T / sqrt(128)) v within each sequence, head_dim 128, bf16; f32
+ * softmax and sums, probabilities rounded to bf16 (both in the sum and in the product).
+ * A query without a key gets zeros; rows of o outside every sequence are left as
+ * they are.  What k and v hold for keys that a query does not see (infinities, NaN) does not reach it.
+ * Sequences of a batch may be of any lengths, single queries against long caches among them.
+ *   flags  0, DIT_ATTN_BOUNDED_LOGITS, DIT_ATTN_CAUSAL or both
+ *   ws     device, dit_attention_packed_ws_bytes(s) (0: then NULL will do; the offsets are not read for it), 16-byte aligned
+ * Errors: DIT_EINVAL (null pointers, alignment of 16 bytes, of 4 for the offsets; bad flags),
+ * DIT_ESHAPE (negative sizes; heads no multiple of kv_heads; Tq * heads / kv_heads or Tk above
+ * 2^30; strides below the row, no multiple of 8, or of 2^22 or more; batch * kv_heads and Tq * heads / 16 of
+ * 2^22 together), DIT_EHIP. */
+size_t dit_attention_packed_ws_bytes(const dit_packed_shape* s);
+dit_status dit_attention_packed_bf16(const dit_packed_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                     const void* v, int64_t ldv, void* o, int64_t ldo, int32_t flags, void* ws,
+                                     void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,7 +22,7 @@ STATUS_NAMES = {0: "DIT_OK", -1: "DIT_EINVAL", -2: "DIT_ENOMEM", -3: "DIT_EHIP",
                 -5: "DIT_EBUDGET", -6: "DIT_ENONFINITE"}
 DTYPE_F32, DTYPE_BF16 = 0, 1
 INDICATOR_MODULATED, INDICATOR_PATCH = 0, 1
-EPI_STORE, EPI_F32, EPI_GATED_RES, EPI_SILU, EPI_FP8 = 0, 1, 2, 4, 8
+EPI_STORE, EPI_F32, EPI_GATED_RES, EPI_SILU, EPI_FP8, EPI_FP4 = 0, 1, 2, 4, 8, 16
 ABI_VERSION = 4
 POLICIES = {"gate": 0, "static": 1, "threshold": 2}
 SOLVERS = {"euler": 0, "unipc": 1}
@@ -35,7 +35,9 @@ EXPORTS = ["dit_cache_create", "dit_cache_sample", "dit_cache_sample_ex", "dit_c
            "dit_cache_last_error", "dit_cache_set_profiling", "dit_cache_get_stats",
            "dit_cache_reset_stats", "dit_gemm_bf16", "dit_attention_bf16", "dit_attention_bf16_noalloc",
            "dit_quant_fp8", "dit_gemm_fp8", "dit_select_blocks_ws_bytes", "dit_select_blocks_bf16",
-           "dit_attention_sparse_ws_bytes", "dit_attention_sparse_bf16"]
+           "dit_attention_sparse_ws_bytes", "dit_attention_sparse_bf16",
+           "dit_quant_fp4", "dit_dequant_fp4", "dit_gemm_fp4", "dit_rotary_freqs", "dit_rotary",
+           "dit_attention_packed_ws_bytes", "dit_attention_packed_bf16"]
 
 
 class ModelConfigC(C.Structure):
@@ -85,6 +87,22 @@ class SparseShapeC(C.Structure):
                 ("kv_heads", C.c_int32), ("topk", C.c_int32), ("klen", C.c_void_p)]
 
 
+class GemmFp4DescC(C.Structure):
+    _fields_ = list(GemmFp8DescC._fields_)
+
+
+class RotaryDescC(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ldx", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
+                ("pos", C.c_void_p), ("ldpos", C.c_int64), ("freq", C.c_void_p)] \
+        + [(n, C.c_int32) for n in ("dtype", "rows", "heads", "head_dim", "rot", "layout", "axes")] \
+        + [("pairs", C.c_int32 * 4), ("scale", C.c_float)]
+
+
+class PackedShapeC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "Tq", "Tk", "heads", "kv_heads")] \
+        + [(n, C.c_void_p) for n in ("qoff", "koff", "klen")]
+
+
 class DitError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -129,6 +147,14 @@ def load(path: str = LIB_PATH):
     lib.dit_select_blocks_ws_bytes.argtypes = lib.dit_attention_sparse_ws_bytes.argtypes = [shape]
     lib.dit_select_blocks_bf16.argtypes = [shape, vp, i64, vp, i64, i32, vp, vp, vp]
     lib.dit_attention_sparse_bf16.argtypes = [shape, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, vp]
+    lib.dit_quant_fp4.argtypes = [vp, i32, i64, vp, i64, vp, i64, i32, i32, vp]
+    lib.dit_dequant_fp4.argtypes = [vp, i64, vp, i64, vp, i32, i64, i32, i32, vp]
+    lib.dit_gemm_fp4.argtypes = [C.POINTER(GemmFp4DescC), vp]
+    lib.dit_rotary_freqs.argtypes = [i32, C.c_double, i32, C.c_double, C.c_double, vp, vp]
+    lib.dit_rotary.argtypes = [C.POINTER(RotaryDescC), vp]
+    packed = C.POINTER(PackedShapeC)
+    lib.dit_attention_packed_ws_bytes.argtypes = [packed]
+    lib.dit_attention_packed_bf16.argtypes = [packed, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp]
     for n in EXPORTS:
         f = getattr(lib, n)
         if n not in ("dit_cache_destroy", "dit_cache_last_error"):
@@ -552,6 +578,152 @@ def attention_sparse_bf16(q, k, v, o, idx, *, flags=0, ldq=None, ldk=None, ldv=N
         _check(lib.dit_attention_sparse_bf16(C.byref(s), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                              o.data_ptr(), ldo, idx.data_ptr(), flags,
                                              w.data_ptr() if w is not None else None, call.ptr))
+
+
+# ---- a prompt encoder's operators: 4-bit rows and products, rotary positions, packed attention; these calls only
+# enqueue their work, too
+
+ATTN_CAUSAL = 2
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+ROTARY_AXES = 4
+_E2M1, _F64 = "pairs of e2m1", "float64"
+_MEANINGS["torch.float64"] = (_F64,)
+_MEANINGS["torch.float4_e2m1fn_x2"] = (_E2M1,)
+for _t in ("torch.uint8", "torch.int8"):
+    _MEANINGS[_t] += (_E2M1,)
+
+
+def fp4_scale_ld(K: int) -> int:
+    """DIT_FP4_SCALE_LD: least row stride of the scale bytes of 4-bit rows of K values."""
+    return (K + 127) // 128 * 4
+
+
+def _values(x, name, M, K, ld):
+    """Row stride and type of a matrix that is float32, or bf16 as torch.bfloat16 or int16."""
+    f32 = x.element_size() == 4
+    if f32 and not x.is_floating_point():
+        raise ValueError(f"{name} must be float32 or bf16")
+    return (_rows(x, name, M, K, ld, 4, _F32), DTYPE_F32) if f32 else (_rows(x, name, M, K, ld, 2, _BF16), DTYPE_BF16)
+
+
+def quant_fp4(x, q, scale, *, M, K, ldx=None, ldq=None, lds=None, stream=None):
+    """dit_quant_fp4: rows of x (torch.float32, else bf16 as torch.bfloat16 or int16) to pairs of e2m1 q [M, K / 2]
+    (uint8 or torch's type of the format) and E8M0 scale bytes (uint8 or torch's type of the format)."""
+    lib = load()
+    ldx, dtype = _values(x, "x", M, K, ldx)
+    ldq = _rows(q, "q", M, K // 2, ldq, 1, _E2M1)
+    lds = _rows(scale, "scale", M, fp4_scale_ld(K), lds, 1, _E8M0)
+    with _Call(stream, x, q, scale) as call:
+        _check(lib.dit_quant_fp4(x.data_ptr(), dtype, ldx, q.data_ptr(), ldq, scale.data_ptr(), lds, M, K, call.ptr))
+
+
+def dequant_fp4(q, scale, y, *, M, K, ldq=None, lds=None, ldy=None, stream=None):
+    """dit_dequant_fp4: the values of 4-bit rows (as quant_fp4 writes them) as float32 or bf16."""
+    lib = load()
+    ldy, dtype = _values(y, "y", M, K, ldy)
+    ldq = _rows(q, "q", M, K // 2, ldq, 1, _E2M1)
+    lds = _rows(scale, "scale", M, fp4_scale_ld(K), lds, 1, _E8M0)
+    with _Call(stream, q, scale, y) as call:
+        _check(lib.dit_dequant_fp4(q.data_ptr(), ldq, scale.data_ptr(), lds, y.data_ptr(), dtype, ldy, M, K, call.ptr))
+
+
+def gemm_fp4(A, a_scale, W, w_scale, bias, Cout, *, M, N, K, lda=None, ld_as=None, ldw=None, ld_ws=None, ldc=None,
+             c_scale=None, ld_cs=None, flags=EPI_STORE, gate=None, rms_cols=0, gelu_from=None, gap_at=0, gap=0,
+             stream=None):
+    """dit_gemm_fp4 on torch cuda tensors: 4-bit rows as quant_fp4 writes them, bias and Cout as in gemm_bf16 (Cout
+    pairs of e2m1 [M, N / 2] with EPI_FP4, c_scale its scale bytes)."""
+    lib = load()
+    lda, ldw = _rows(A, "A", M, K // 2, lda, 1, _E2M1), _rows(W, "W", N, K // 2, ldw, 1, _E2M1)
+    ld_as = _rows(a_scale, "a_scale", M, fp4_scale_ld(K), ld_as, 1, _E8M0)
+    ld_ws = _rows(w_scale, "w_scale", N, fp4_scale_ld(K), ld_ws, 1, _E8M0)
+    if flags & EPI_FP4:
+        ldc = _rows(Cout, "Cout", M, N // 2, ldc, 1, _E2M1)
+        if c_scale is not None:
+            ld_cs = _rows(c_scale, "c_scale", M, fp4_scale_ld(N), ld_cs, 1, _E8M0)
+    else:
+        width = N + (gap if gap and gap_at < N else 0)
+        ldc = _rows(Cout, "Cout", M, width, ldc, *((4, _F32) if flags & EPI_F32 else (2, _BF16)))
+    if bias is not None:
+        _rows(bias, "bias", 1, N, None, 2, _BF16)
+    if gate is not None:
+        _rows(gate, "gate", 1, N, None, 4, _F32)
+    d = GemmFp4DescC(A.data_ptr(), lda, a_scale.data_ptr(), ld_as, W.data_ptr(), ldw, w_scale.data_ptr(), ld_ws,
+                     bias.data_ptr() if bias is not None else None, Cout.data_ptr(), ldc,
+                     c_scale.data_ptr() if c_scale is not None else None, ld_cs if ld_cs is not None else 0,
+                     gate.data_ptr() if gate is not None else None, M, N, K, flags, rms_cols,
+                     gelu_from if gelu_from is not None else 0x7FFFFFFF, gap_at, gap)
+    with _Call(stream, A, a_scale, W, w_scale, bias, Cout, c_scale, gate) as call:
+        _check(lib.dit_gemm_fp4(C.byref(d), call.ptr))
+
+
+def rotary_freqs(pairs, *, base=10000.0, method=ROTARY_PLAIN, factor=1.0, context=0.0):
+    """dit_rotary_freqs: (float64 array of radians per position, factor on cosine and sine); rotary takes the array
+    as a device tensor."""
+    lib = load()
+    freq, scale = np.empty(max(pairs, 0)), C.c_double()
+    _check(lib.dit_rotary_freqs(pairs, base, method, factor, context, freq.ctypes.data_as(C.c_void_p), C.byref(scale)))
+    return freq, scale.value
+
+
+def rotary(x, y, *, pos, freq, rows, heads, head_dim=128, pairs=None, layout=ROTARY_HALF, scale=1.0, ldx=None, ldy=None,
+           ldpos=None, stream=None):
+    """dit_rotary: rows of x to y (x itself: in place), both float32, or bf16 as torch.bfloat16 or int16.  pos: int32
+    [rows] or [axes, rows]; freq: float64 cuda tensor, one per pair; pairs: those of each axis (None: one axis)."""
+    lib = load()
+    n = freq.numel()
+    pairs = [n] if pairs is None else list(pairs)
+    if not 1 <= len(pairs) <= ROTARY_AXES or sum(pairs) != n:
+        raise ValueError(f"pairs must be those of 1 to {ROTARY_AXES} axes, {n} together")
+    (ldx, dtype), (ldy, out) = (_values(t, name, rows, heads * head_dim, ld) for t, name, ld in ((x, "x", ldx), (y, "y", ldy)))
+    if dtype != out:
+        raise ValueError("x and y must be of one type")
+    _rows(freq, "freq", 1, n, None, 8, _F64)
+    ldpos = _rows(pos, "pos", len(pairs), rows, ldpos, 4, _I32) if len(pairs) > 1 or pos.dim() == 2 \
+        else _rows(pos, "pos", 1, rows, rows, 4, _I32)
+    d = RotaryDescC(x.data_ptr(), ldx, y.data_ptr(), ldy, pos.data_ptr(), ldpos, freq.data_ptr(), dtype, rows, heads,
+                    head_dim, 2 * n, layout, len(pairs), (C.c_int32 * 4)(*pairs), scale)
+    with _Call(stream, x, y, pos, freq) as call:
+        _check(lib.dit_rotary(C.byref(d), call.ptr))
+
+
+def packed_shape(*, qoff, koff, Tq, Tk, heads, kv_heads=None, klen=None) -> PackedShapeC:
+    """dit_packed_shape; qoff, koff: int32 cuda tensors [batch + 1], klen: [batch] or None."""
+    batch = qoff.numel() - 1
+    if batch < 0 or koff.numel() != batch + 1 or (klen is not None and klen.numel() != batch):
+        raise ValueError("qoff and koff must hold batch + 1 offsets, klen batch lengths")
+    for t, name, n in ((qoff, "qoff", batch + 1), (koff, "koff", batch + 1), (klen, "klen", batch)):
+        if t is not None:
+            _rows(t, name, 1, n, None, 4, _I32)
+    return PackedShapeC(batch, Tq, Tk, heads, kv_heads if kv_heads is not None else heads, qoff.data_ptr(),
+                        koff.data_ptr(), klen.data_ptr() if klen is not None else None)
+
+
+@functools.lru_cache(256)
+def _packed_ws_bytes(*sizes):
+    """A workspace's size depends on the shape's numbers alone."""
+    return load().dit_attention_packed_ws_bytes(C.byref(PackedShapeC(*sizes, None, None, None)))
+
+
+def attention_packed_ws_bytes(*, batch, Tq, Tk, heads, kv_heads=None) -> int:
+    return _packed_ws_bytes(batch, Tq, Tk, heads, kv_heads if kv_heads is not None else heads)
+
+
+def attention_packed_bf16(q, k, v, o, *, qoff, koff, heads, kv_heads=None, klen=None, Tq=None, Tk=None, flags=0, ldq=None,
+                          ldk=None, ldv=None, ldo=None, ws=None, stream=None):
+    """dit_attention_packed_bf16; shape as in packed_shape (Tq, Tk None: the rows of q and of k); ws None: a
+    workspace of torch's caching allocator."""
+    lib = load()
+    s = packed_shape(qoff=qoff, koff=koff, Tq=q.shape[0] if Tq is None else Tq, Tk=k.shape[0] if Tk is None else Tk,
+                     heads=heads, kv_heads=kv_heads, klen=klen)
+    ldq = _rows(q, "q", s.Tq, s.heads * 128, ldq, 2, _BF16)
+    ldk = _rows(k, "k", s.Tk, s.kv_heads * 128, ldk, 2, _BF16)
+    ldv = _rows(v, "v", s.Tk, s.kv_heads * 128, ldv, 2, _BF16)
+    ldo = _rows(o, "o", s.Tq, s.heads * 128, ldo, 2, _BF16)
+    with _Call(stream, q, k, v, o, qoff, koff, klen) as call:
+        w = call.workspace(ws, _packed_ws_bytes(s.batch, s.Tq, s.Tk, s.heads, s.kv_heads), "ws")
+        _check(lib.dit_attention_packed_bf16(C.byref(s), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                             o.data_ptr(), ldo, flags, w.data_ptr() if w is not None else None, call.ptr))
 
 
 def gate_logit(gate_blob, features) -> float:

@@ -129,6 +129,29 @@ size_t attention_sparse_ws_bytes(const dit_sparse_shape& s);
 hipError_t launch_attention_sparse(const dit_sparse_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                    const void* v, int64_t ldv, void* o, int64_t ldo, const int32_t* idx, bool bounded,
                                    void* ws, hipStream_t st, int n_cu);
+// ---- a prompt encoder's operators (the same) ----
+struct GemmFp4Args {
+  const void* A; int64_t lda;
+  const void* W; int64_t ldw;
+  const void* As; int64_t ldas;
+  const void* Ws; int64_t ldws;
+  const void* bias;
+  void* C; int64_t ldc;
+  void* Cs; int64_t ldcs;
+  const float* gate;
+  int M, N, K;
+  int flags, rms_cols, gelu_from, gap_at, gap;
+};
+hipError_t launch_quant_fp4(const void* x, bool bf16, int64_t ldx, void* q, int64_t ldq, void* scale, int64_t lds, int M,
+                            int K, hipStream_t s);
+hipError_t launch_dequant_fp4(const void* q, int64_t ldq, const void* scale, int64_t lds, void* y, bool bf16, int64_t ldy,
+                              int M, int K, hipStream_t s);
+hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu);
+hipError_t launch_rotary(const dit_rotary_desc& d, hipStream_t s);
+size_t attention_packed_ws_bytes(const dit_packed_shape& s);
+hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, void* o, int64_t ldo, bool bounded, bool causal, void* ws,
+                                   hipStream_t st);
 // Status and message of a failed component call (dit_cache_last_error(NULL)).
 dit_status component_fail(dit_status st, const char* msg) noexcept;
 
