@@ -163,7 +163,7 @@ def prepare(case, seed):
         codes, e = _quantise(x.float())
         sc = torch.full((rows, _scale_ld(K)), 127, dtype=torch.uint8, device="cuda")
         sc[:, :e.shape[1]] = e
-        return _pack(codes), sc.view(E8)
+        return _pack(codes).to(torch.uint8), sc.view(E8)
 
     s = dict(case=c)
     if c["op"] == "rotary":
