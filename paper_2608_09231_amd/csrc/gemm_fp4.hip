@@ -147,6 +147,8 @@ __global__ __launch_bounds__(256) void dequant_fp4_kernel(const uint8_t* __restr
 
 // ---------------------------------------------------------------- products
 
+// The 128-deep step of one 16 x 16 block: lane (lr, lq) holds row lr's values 32 lq .. + 31
+// and, in byte B of sa or sw, their scale.
 template <int B = 0>
 __device__ __forceinline__ f32x4_t mfma_fp4(const i32x4_t& a, const i32x4_t& w, const f32x4_t& c, int sa, int sw) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -157,6 +159,69 @@ __device__ __forceinline__ f32x4_t mfma_fp4(const i32x4_t& a, const i32x4_t& w, 
   return c;
 #endif
 }
+
+// The same of a 32 x 32 block and 64 of K: lane (lr, lh) holds row lr's values 32 lh .. + 31.
+template <int B>
+__device__ __forceinline__ f32x16_t mfma_fp4_32(const i32x4_t& a, const i32x4_t& w, const f32x16_t& c, int sa, int sw) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const i32x8_t x = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+  const i32x8_t y = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, B, sa, B, sw);
+#else
+  return c;
+#endif
+}
+
+// 16 bytes per lane from base + voff + soff to LDS at dst + 16 lane; lanes with voff
+// >= OOB write zeros.  Offsets in bounds lie below OOB: the bases are those of a
+// tile's first row, and the host bounds 256 rows of an operand.  An instruction that the compiler does
+// not see through: it would have reads of LDS wait for all copies in flight.  The kernels' own waits
+// and barriers order them, and scheduling fences keep their place.
+constexpr uint32_t OOB = 0x80000000u;
+__device__ __forceinline__ void copy16_unseen(const void* base, const void* dst, uint32_t voff, uint32_t soff) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const uint64_t b = (uint64_t)base;
+  const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, OOB, 0x00020000u};
+  const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)dst;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(l), "v"(voff), "s"(r), "s"(soff));
+#endif
+}
+// 4 bytes per lane the same way.
+__device__ __forceinline__ void copy4_unseen(const void* base, const void* dst, uint32_t voff, uint32_t soff) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const uint64_t b = (uint64_t)base;
+  const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, OOB, 0x00020000u};
+  const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)dst;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(l), "v"(voff), "s"(r), "s"(soff));
+#endif
+}
+
+__device__ __forceinline__ i32x4_t lds_chunk(const char* p) { return *(const i32x4_t*)p; }
+
+// Scale bytes in LDS.  A row has nd dwords of them, one per 128 of K; a group is four
+// (512 of K, two slices), 16 bytes a row, and the last group begins early enough to lie in
+// the row: dword d is at d - start(group).
+struct Scales {
+  int nd, blocks;  // dwords of a row, blocks of 32
+  __device__ __forceinline__ explicit Scales(int K) : nd((K + 127) >> 7), blocks(K >> 5) {}
+  __device__ __forceinline__ int start(int g) const { return g == 0 ? 0 : min(4 * g, nd - 4); }
+  // place of dword d of group g
+  __device__ __forceinline__ int place(int g, int d) const { return min(d - start(g), 3); }
+  // bytes of dword d that belong to blocks, the rest zeros (a NaN there would spoil sums of zeros)
+  __device__ __forceinline__ uint32_t valid(int d) const {
+    const int n = blocks - 4 * d;
+    return n >= 4 ? ~0u : (1u << (8 * max(n, 0))) - 1u;
+  }
+  // group 0 of a row, through registers: its dwords that exist
+  __device__ __forceinline__ void first(const uint8_t* row, char* dst) const {
+    i32x4_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *(const int*)(row + 4 * min(i, nd - 1));
+    *(i32x4_t*)dst = x;
+  }
+};
 
 // Origin of tile lt: M-grouped order, eight tile rows per group.
 __device__ __forceinline__ void tile_at(const Fp4Prob& P, int lt, int& tm, int& tn) {
@@ -228,7 +293,7 @@ struct Epi : EpiLdsT<KIND == EPI_K_FP4 ? EPI_K_ANY : KIND, Fp4Prob> {
 #pragma unroll
           for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(v[hh][e]) & 0x7fffffffu);
           const uint32_t byte = scale4_of(max_over<8>(top));
-          const float inv = e8m0_inverse(byte);
+          [[maybe_unused]] const float inv = e8m0_inverse(byte);
           const int n = this->ncol0 + 64 * hh + 4 * cq;
           if (m < P.M && n < P.N) {
             uint32_t w = 0;
@@ -245,48 +310,294 @@ struct Epi : EpiLdsT<KIND == EPI_K_FP4 ? EPI_K_ANY : KIND, Fp4Prob> {
   }
 };
 
-// 64 x 128 tiles, four waves of 32 x 64, operands straight from memory to
-// registers: the simplest form.
+// 256 x 256 tiles, 8 waves of 64 x 128.  LDS: two slices of 256 of K each of W and A
+// (32 KB, 16-byte chunks of a 128-byte row XOR-swizzled by ((row >> 1) & 7)) and two groups of
+// both's scales.  32x32x64 MFMAs: a slice is four substeps of eight, and a
+// substep's six fragments are read under the MFMAs of the one before it.
+//
+// The waves meet after substep 2, whose reads were the last of their slice: slice kt +
+// 1 has landed, and slice kt's places take slice kt + 2 during substep 3.  Slices past the
+// last one are copied as zeros (no memory traffic), which keeps every iteration alike.
 template <int KIND>
-__global__ __launch_bounds__(256) void gemm_fp4_tile_kernel(Fp4Prob P) {
-  constexpr int BM = 64, WM = 32, TM = 2, TN = 4;
-  __shared__ __attribute__((aligned(1024))) char smem[BM * 128 * 4];
+__global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
+  constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4, SC = 4 * UNIT, GROUP = 512 * 16;
+  __shared__ __attribute__((aligned(1024))) char smem[SC + 2 * GROUP];
+  int tm, tn;
+  tile_at(P, xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n), tm, tn);
+  const int m0 = tm * 256, n0 = tn * 256;
+  const int nk = (P.K + 255) >> 8;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const int lr = lane & 31, lh = lane >> 5;
+
+  // copy j of this wave moves rows 8 (4 wave + j) .. + 7 of an operand's slice
+  const uint8_t* Ab = P.A + (int64_t)m0 * P.lda;
+  const uint8_t* Wb = P.W + (int64_t)n0 * P.ldw;
+  const int c0 = (lane & 7) ^ (lane >> 4);  // chunk of even copies; odd ones: c0 ^ 4
+  uint32_t aoff[INS], woff[INS];
+#pragma unroll
+  for (int j = 0; j < INS; ++j) {
+    const int row = 8 * (wave * INS + j) + (lane >> 3);
+    aoff[j] = (uint32_t)min(row, P.M - 1 - m0) * (uint32_t)P.lda + 16 * (c0 ^ (4 * (j & 1)));
+    woff[j] = (uint32_t)min(row, P.N - 1 - n0) * (uint32_t)P.ldw + 16 * (c0 ^ (4 * (j & 1)));
+  }
+  auto issue1 = [&](const uint8_t* base, const uint32_t (&off)[INS], int u, int s, int j) {
+    copy16_unseen(base, smem + u + (wave * INS + j) * 1024,
+                  16 * (c0 ^ (4 * (j & 1))) < (P.K >> 1) - 128 * s ? off[j] : OOB, (uint32_t)s * 128);
+  };
+  // scales: waves 0 .. 3 rows of A, 4 .. 7 rows of W, 64 each
+  const Scales sc(P.K);
+  const uint8_t* sbase = wave < 4 ? P.As + (int64_t)m0 * P.ldas : P.Ws + (int64_t)n0 * P.ldws;
+  const uint32_t soff = wave < 4 ? (uint32_t)min(tid, P.M - 1 - m0) * (uint32_t)P.ldas
+                                 : (uint32_t)min(tid - 256, P.N - 1 - n0) * (uint32_t)P.ldws;
+  auto issue_scales = [&](int g) {
+    if (4 * g < sc.nd) copy16_unseen(sbase, smem + SC + (g & 1) * GROUP + wave * 1024, soff, 4 * sc.start(g));
+  };
+  const int srow = SC + 16 * (64 * wm + lr), wrow = SC + 16 * (256 + 128 * wn + lr);
+  uint32_t sa[2][TM], sw[2][TN];
+  auto read_scales = [&](int kt) {  // of slice kt (past the last one: zeros)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int d = 2 * kt + h, g = kt >> 1, at = (g & 1) * GROUP + 4 * sc.place(g, d);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) sa[h][i] = *(const uint32_t*)(smem + srow + at + 512 * i);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sw[h][j] = *(const uint32_t*)(smem + wrow + at + 512 * j);
+    }
+  };
+  auto place_scales = [&](int kt) {  // this lane's half into bytes 0 and 2
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t v = sc.valid(2 * kt + h);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) sa[h][i] = (sa[h][i] & v) >> (8 * lh);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sw[h][j] = (sw[h][j] & v) >> (8 * lh);
+    }
+  };
+
+  // this lane's chunk inside 32 rows of a unit: half lh of substep s
+  int loff[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) loff[s] = lr * 128 + (((2 * s + lh) ^ ((lr >> 1) & 7)) << 4);
+  const int wa = wm * 64 * 128, ww = wn * 128 * 128;
+  f32x16_t acc[TM][TN] = {};
+  // A substep's MFMAs, and between them one by one the fragment reads of the next
+  // substep (s of the slice in units uw, ua) in the order of their use and a copy.
+  // The fences keep that order.
+  auto substep = [&](const i32x4_t(&a)[TM], const i32x4_t(&w)[TN], i32x4_t(&an)[TM], i32x4_t(&wn2)[TN], int uw, int ua,
+                     int s, const uint32_t(&xa)[TM], const uint32_t(&xw)[TN], auto b_, auto copy) {
+    constexpr int B = decltype(b_)::value;
+#pragma unroll
+    for (int q = 0; q < TM * TN; ++q) {
+      const int i = q & 1, j = q >> 1;
+      acc[i][j] = mfma_fp4_32<B>(a[i], w[j], acc[i][j], xa[i], xw[j]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (q == 0 || q == 2) an[q >> 1] = lds_chunk(smem + ua + wa + (q >> 1) * 4096 + loff[s]);
+      else if (q < 6) wn2[q == 1 ? 0 : q - 2] = lds_chunk(smem + uw + ww + (q == 1 ? 0 : q - 2) * 4096 + loff[s]);
+      copy(q);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto none = [](int) {};
+  using std::integral_constant;
+  const integral_constant<int, 0> b0{};
+  const integral_constant<int, 2> b2{};
+
+  // W slice kt in unit kt % 2, A slice kt in unit 2 + kt % 2
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+#pragma unroll
+    for (int j = 0; j < INS; ++j) {
+      issue1(Wb, woff, s * UNIT, s, j);
+      issue1(Ab, aoff, (2 + s) * UNIT, s, j);
+    }
+  }
+  issue_scales(1);
+  sc.first(sbase + soff, smem + SC + 16 * tid);
+  wait_vmcnt_lgkm0<0>();
+  barrier_no_fence();
+  i32x4_t a0[TM], w0[TN], a1[TM], w1[TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) a0[i] = lds_chunk(smem + 2 * UNIT + wa + i * 4096 + loff[0]);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) w0[j] = lds_chunk(smem + ww + j * 4096 + loff[0]);
+  read_scales(0);
+  place_scales(0);
+#pragma unroll 1
+  for (int kt = 0; kt < nk; ++kt) {
+    const int wu = (kt & 1) * UNIT, au = wu + 2 * UNIT;
+    __builtin_amdgcn_sched_barrier(0);
+    substep(a0, w0, a1, w1, wu, au, 1, sa[0], sw[0], b0, none);
+    substep(a1, w1, a0, w0, wu, au, 2, sa[0], sw[0], b2, none);
+    substep(a0, w0, a1, w1, wu, au, 3, sa[1], sw[1], b0, none);
+    // this wave's reads of slice kt and its copies of slice kt + 1 are done; then everyone's are
+    wait_vmcnt_lgkm0<0>();
+    barrier_no_fence();
+    // (slice kt's group of scales is read, too: the next but one takes its place)
+    if ((kt & 1) == 1) issue_scales((kt >> 1) + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    const uint32_t xa[TM] = {sa[1][0], sa[1][1]}, xw[TN] = {sw[1][0], sw[1][1], sw[1][2], sw[1][3]};
+    read_scales(kt + 1);
+    substep(a1, w1, a0, w0, wu ^ UNIT, au ^ UNIT, 0, xa, xw, b2, [&](int q) {
+      if (q & 1) issue1(Ab, aoff, au, kt + 2, q >> 1);
+      else issue1(Wb, woff, wu, kt + 2, q >> 1);
+    });
+    place_scales(kt + 1);
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
+  __syncthreads();
+  float* slab = (float*)smem + wave * (32 * 128);
+  Epi<KIND> epi(P, m0 + 64 * wm, n0 + 128 * wn, lr, lh, slab);
+  epi.prep();
+  uint2 old[2][8][2];
+  if (epi.gated) { epi.load_old(0, old[0]); epi.load_old(1, old[1]); }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = 8 * (r >> 2) + 4 * lh + (r & 3);
+        slab[row * 128 + ((j * 32 + lr) ^ (((row >> 2) & 1) << 5))] = acc[i][j][r];
+      }
+    epi.template rows<1, 5, 32>(i, old[i]);
+  }
+}
+
+// BM x 128 tiles, waves of 64 x 64 (BM = 64: 32 x 64), a ring of slices of 256 of K
+// in LDS: two work-groups of 64 x 128 (three slices) or 128 x 128 (two) per CU, or
+// one of 256 x 128 (three).  For launches that 256 x 256 tiles would not fill.  The waves
+// meet before every step kt; slice kt + 1 has landed, and slice kt, whose fragments are all in
+// registers, gives its place to slice kt + ST.  The fragments of kt + 1 are read under the MFMAs of kt.
+template <int BM, int KIND>
+__global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel(Fp4Prob P) {
+  constexpr int ST = BM == 128 ? 2 : 3;
+  constexpr int NW = BM == 256 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
+  constexpr int TM = WM / 16, TN = 4, NF = TM + TN;
+  constexpr int SLICE = (BM + 128) * 128, RING = ST * SLICE, GROUP = (BM + 128) * 16;
+  constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW, INS = A_INS + W_INS;
+  constexpr int TILE = BM * 128 * 4;
+  __shared__ __attribute__((aligned(1024))) char smem[RING + 2 * GROUP > TILE ? RING + 2 * GROUP : TILE];
   int tm, tn;
   tile_at(P, xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n), tm, tn);
   const int m0 = tm * BM, n0 = tn * 128;
+  const int nk = (P.K + 255) >> 8;
+
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   const int lr = lane & 15, lq = lane >> 4;
-  const uint8_t *row[TM + TN], *sc[TM + TN];
+
+  const uint8_t* Ab = P.A + (int64_t)m0 * P.lda;
+  const uint8_t* Wb = P.W + (int64_t)n0 * P.ldw;
+  // copy j of this wave: rows 8 (A_INS wave + j) .. + 7 of A, then the like of W
+  uint32_t off[INS];
+  int ch[INS];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t m = min(m0 + WM * wm + 16 * i + lr, P.M - 1);
-    row[i] = P.A + m * P.lda;
-    sc[i] = P.As + m * P.ldas;
+  for (int j = 0; j < INS; ++j) {
+    const int row = 8 * (j < A_INS ? wave * A_INS + j : wave * W_INS + j - A_INS) + (lane >> 3);
+    ch[j] = 16 * ((lane & 7) ^ ((row >> 1) & 7));
+    off[j] = (uint32_t)min(row, (j < A_INS ? P.M - 1 - m0 : P.N - 1 - n0)) * (uint32_t)(j < A_INS ? P.lda : P.ldw) + ch[j];
   }
+  auto issue1 = [&](int u, int s, int j) {
+    const int at = j < A_INS ? (wave * A_INS + j) * 1024 : BM * 128 + (wave * W_INS + j - A_INS) * 1024;
+    copy16_unseen(j < A_INS ? Ab : Wb, smem + u + at, ch[j] < (P.K >> 1) - 128 * s ? off[j] : OOB, (uint32_t)s * 128);
+  };
+  // scales: 64 rows a wave, of A, then of W
+  const Scales sc(P.K);
+  const bool of_a = 64 * wave < BM, of_any = 64 * wave < BM + 128;
+  const uint8_t* sbase = of_a ? P.As + (int64_t)m0 * P.ldas : P.Ws + (int64_t)n0 * P.ldws;
+  const uint32_t soff = of_a ? (uint32_t)min(tid, P.M - 1 - m0) * (uint32_t)P.ldas
+                             : (uint32_t)min(tid - BM, P.N - 1 - n0) * (uint32_t)P.ldws;
+  auto issue_scales = [&](int g) {
+    if (of_any && 4 * g < sc.nd)
+      copy16_unseen(sbase, smem + RING + (g & 1) * GROUP + wave * 1024, soff, 4 * sc.start(g));
+  };
+  auto read_scales = [&](int kt, uint32_t(&x)[NF][2], int f) {
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int64_t n = min(n0 + 64 * wn + 16 * j + lr, P.N - 1);
-    row[TM + j] = P.W + n * P.ldw;
-    sc[TM + j] = P.Ws + n * P.ldws;
-  }
-  f32x4_t acc[TM][TN] = {};
-  for (int k = 0; k < P.K; k += 128) {
-    const int at = k + 32 * lq;
-    const bool in = at < P.K;  // K % 32 == 0: a block is inside or not
-    i32x4_t f[TM + TN];
-    int s[TM + TN];
-#pragma unroll
-    for (int i = 0; i < TM + TN; ++i) {
-      f[i] = in ? *(const i32x4_t*)(row[i] + (at >> 1)) : i32x4_t{0, 0, 0, 0};
-      s[i] = in ? sc[i][at >> 5] : 127;
+    for (int h = 0; h < 2; ++h) {
+      const int g = kt >> 1, at = RING + (g & 1) * GROUP + 4 * sc.place(g, 2 * kt + h);
+      x[f][h] = *(const uint32_t*)(smem + at + 16 * ((f < TM ? WM * wm + 16 * f : BM + 64 * wn + 16 * (f - TM)) + lr));
     }
+  };
+  auto place_scales = [&](int kt, uint32_t(&x)[NF][2]) {  // this lane's block into byte 0
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t v = sc.valid(2 * kt + h);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = mfma_fp4(f[i], f[TM + j], acc[i][j], s[i], s[TM + j]);
+      for (int f = 0; f < NF; ++f) x[f][h] = (x[f][h] & v) >> (8 * lq);
+    }
+  };
+  int loff[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) loff[h] = lr * 128 + (((4 * h + lq) ^ ((lr >> 1) & 7)) << 4);
+  auto rd = [&](int u, int f, int h) {  // fragment f: A, then W
+    const int at = u + (f < TM ? wm * WM * 128 + f * 2048 : BM * 128 + wn * 64 * 128 + (f - TM) * 2048);
+    return lds_chunk(smem + at + loff[h]);
+  };
+  f32x4_t acc[TM][TN] = {};
+
+#pragma unroll
+  for (int s = 0; s < ST; ++s) {
+#pragma unroll
+    for (int j = 0; j < INS; ++j) issue1(s * SLICE, s, j);
+    if (s == 0) {
+      issue_scales(1);
+      if (tid < BM + 128) sc.first(sbase + soff, smem + RING + 16 * tid);  // (waits for slice 0 and group 1, too)
+    }
   }
+  wait_vmcnt_lgkm0<(ST - 1) * INS>();
+  barrier_no_fence();
+  i32x4_t f0[NF][2], f1[NF][2];
+  uint32_t s0[NF][2], s1[NF][2];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    f0[f][0] = rd(0, f, 0);
+    f0[f][1] = rd(0, f, 1);
+    read_scales(0, s0, f);
+  }
+  place_scales(0, s0);
+  int u = 0;  // place of slice kt
+  auto step = [&](int kt, i32x4_t(&f)[NF][2], i32x4_t(&fn)[NF][2], uint32_t(&x)[NF][2], uint32_t(&xn)[NF][2]) {
+    const int un = u == (ST - 1) * SLICE ? 0 : u + SLICE;
+    // this wave's reads of slice kt and its copies of slice kt + 1 are done (those
+    // of the next ST - 2 may stay in flight); then everyone's are
+    wait_vmcnt_lgkm0<(ST - 2) * INS>();
+    barrier_no_fence();
+    if (kt & 1) issue_scales((kt >> 1) + 2);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 2 * TM * TN; ++q) {
+      const int h = q / (TM * TN), i = q % TM, j = q % (TM * TN) / TM;
+      acc[i][j] = mfma_fp4(f[i][h], f[TM + j][h], acc[i][j], x[i][h], x[TM + j][h]);
+      __builtin_amdgcn_sched_barrier(0);
+      // in the order of their use: A 0, W 0, the other A, the other W
+      if (q < 2 * NF) {
+        const int hq = q / NF, e = q % NF, r = e == 0 ? 0 : e == 1 ? TM : e <= TM ? e - 1 : e;
+        fn[r][hq] = rd(un, r, hq);
+        if (hq == 0) read_scales(kt + 1, xn, r);
+      }
+      if (q >= 2 * TM * TN - INS) issue1(u, kt + ST, q - (2 * TM * TN - INS));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    place_scales(kt + 1, xn);
+    u = un;
+  };
+  int kt = 0;
+#pragma unroll 1
+  for (; kt + 2 <= nk; kt += 2) {
+    step(kt, f0, f1, s0, s1);
+    step(kt + 1, f1, f0, s1, s0);
+  }
+  if (kt < nk) step(kt, f0, f1, s0, s1);
+  __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
+  __syncthreads();
+  // The tile in LDS as slabs of ROWS rows x 128, one per wave, columns XOR 16
+  // ((row >> 2) & 3): then each wave has whole 128-column rows.
+  constexpr int ROWS = BM / NW;
   float* tile = (float*)smem;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -296,12 +607,170 @@ __global__ __launch_bounds__(256) void gemm_fp4_tile_kernel(Fp4Prob P) {
       for (int r = 0; r < 4; ++r)
         tile[(wm * WM + 16 * i + 4 * lq + r) * 128 + ((64 * wn + 16 * j + lr) ^ (lq << 4))] = acc[i][j][r];
   __syncthreads();
-  constexpr int ROWS = BM / 4;
   Epi<KIND> epi(P, m0 + ROWS * wave, n0, lane & 31, lane >> 5, tile + ROWS * wave * 128);
   epi.prep();
   uint2 old[8][2];
   if (epi.gated) epi.load_old(0, old);
   epi.template rows<3, 4, ROWS>(0, old);
+}
+
+// Few rows or few tiles: 16 RB x NT outputs per work-group, eight waves of 16 RB x 32
+// that share K (NT = 32: eight ways, 64: four, 128: two).  Each wave copies its own
+// rows' slices and their scales to a ring of its own in LDS, so that no wave waits for another until
+// their sums meet at the end; the copies read whole 128-byte lines, eight lanes
+// each.  Bound by the way of W from memory.
+template <int NT, int RB, int KIND>
+__global__ __launch_bounds__(512) void gemm_fp4_small_kernel(Fp4Prob P) {
+  constexpr int NH = NT / 32, KS = 8 / NH, NF = 2 + RB, ST = RB == 1 ? 3 : 2;
+  constexpr int INS = 2 * NF, SLICE = INS * 1024 + 512, LD = 36;  // W's two fragments, A's, scales
+  constexpr int RING = 8 * ST * SLICE, PART = 8 * 16 * RB * LD * 4;
+  static_assert(PART <= RING, "the waves' sums take the rings' place");
+  __shared__ __attribute__((aligned(1024))) char smem[RING];
+  const int lt = xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n);
+  const int m0 = lt % P.tiles_m * (16 * RB), n0 = lt / P.tiles_m * NT;  // neighbours share the weights
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lq = lane >> 4;
+  const int ks = wave % KS, nh = wave / KS;
+  const int nw = min(n0 + 32 * nh, P.N - 1);  // (a wave past the last column repeats it)
+  const uint8_t* Wb = P.W + (int64_t)nw * P.ldw;
+  const uint8_t* Ab = P.A + (int64_t)m0 * P.lda;
+  // copy j: rows 8 j .. + 7 of W, then of A
+  uint32_t off[INS];
+  int ch[INS];
+#pragma unroll
+  for (int j = 0; j < INS; ++j) {
+    const int row = 8 * (j < 4 ? j : j - 4) + (lane >> 3);
+    ch[j] = 16 * ((lane & 7) ^ ((row >> 1) & 7));
+    off[j] = (uint32_t)min(row, (j < 4 ? P.N - 1 - nw : P.M - 1 - m0)) * (uint32_t)(j < 4 ? P.ldw : P.lda) + ch[j];
+  }
+  // scales of row lane: 32 of W, 16 RB of A, each from its own operand
+  const Scales sc(P.K);
+  const uint8_t* Wsb = P.Ws + (int64_t)nw * P.ldws;
+  const uint8_t* Asb = P.As + (int64_t)m0 * P.ldas;
+  const uint32_t soff = lane < 32 ? (uint32_t)min(lane, P.N - 1 - nw) * (uint32_t)P.ldws
+                                  : (uint32_t)min((lane - 32) % (16 * RB), P.M - 1 - m0) * (uint32_t)P.ldas;
+  const int steps = (P.K + 255) >> 8, per = (steps + KS - 1) / KS;
+  const int s0 = ks * per, s1 = min(steps, s0 + per);
+  char* ring = smem + wave * (ST * SLICE);
+  // slice s of K (past the wave's last one: zeros) and its scales
+  auto issue = [&](int s, int u) {
+    const int left = s < s1 ? (P.K >> 1) - 128 * s : 0;
+    char* d = ring + u * SLICE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t at = 4 * min(2 * s + h, sc.nd - 1);
+      if (lane < 32) copy4_unseen(Wsb, d + INS * 1024 + 256 * h, soff, at);
+      else copy4_unseen(Asb, d + INS * 1024 + 256 * h, soff, at);
+    }
+#pragma unroll
+    for (int j = 0; j < INS; ++j)
+      copy16_unseen(j < 4 ? Wb : Ab, d + j * 1024, ch[j] < left ? off[j] : OOB, (uint32_t)s * 128);
+  };
+  int loff[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) loff[h] = lr * 128 + (((4 * h + lq) ^ ((lr >> 1) & 7)) << 4);
+  f32x4_t acc[RB][2] = {};
+#pragma unroll
+  for (int u = 0; u < ST; ++u) issue(s0 + u, u);
+  for (int s = s0; s < s1; s += ST) {
+#pragma unroll
+    for (int u = 0; u < ST; ++u) {  // (a slice past s1 adds zeros)
+      wait_vmcnt<(ST - 1) * (INS + 4)>();  // this slice and its scales have landed
+      asm volatile("" ::: "memory");
+      i32x4_t f[NF][2];
+      uint32_t b[NF][2];
+#pragma unroll
+      for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f[i][h] = lds_chunk(ring + u * SLICE + i * 2048 + loff[h]);
+          const uint32_t x = *(const uint32_t*)(ring + u * SLICE + INS * 1024 + 256 * h + 4 * (16 * i + lr));
+          b[i][h] = (x & (s + u < s1 ? sc.valid(2 * (s + u) + h) : 0u)) >> (8 * lq);
+        }
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): read, its place is free
+      asm volatile("" ::: "memory");
+      issue(s + u + ST, u);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[i][j] = mfma_fp4(f[2 + i][h], f[j][h], acc[i][j], b[2 + i][h], b[j][h]);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
+  __syncthreads();
+  float(*part)[16 * RB][LD] = (float(*)[16 * RB][LD])smem;
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) part[wave][16 * i + 4 * lq + r][16 * j + lr] = acc[i][j][r];
+  __syncthreads();
+
+  // NT / 4 threads per row, 4 columns each, the waves' sums added in their order
+  constexpr int TPR = NT / 4, PASS = 512 / TPR;
+  const int c = tid % TPR, n = n0 + 4 * c;
+#pragma unroll
+  for (int r0 = 0; r0 < 16 * RB; r0 += PASS) {
+    const int row = r0 + tid / TPR, m = m0 + row;
+    if (row >= 16 * RB) return;  // whole waves
+    f32x4_t t = {};
+#pragma unroll
+    for (int w = 0; w < KS; ++w) t += *(const f32x4_t*)&part[KS * (c / 8) + w][row][4 * (c % 8)];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = t[e] + (P.bias && n < P.N ? bf16_to_f32(P.bias[n + e]) : 0.f);
+    if constexpr (NT == 128) {
+      if (n0 < P.rms_cols) {  // one 128-wide head per tile
+        float ss = v[0] * v[0] + v[1] * v[1] + v[2] * v[2] + v[3] * v[3];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) ss += __shfl_xor(ss, o, 64);
+        const float f = rsqrtf(ss * (1.f / 128.f) + DIT_RMS_EPS);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= f;
+      }
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (n >= P.gelu_from) v[e] = gelu_tanh_f(v[e]);
+      if (P.flags & DIT_EPI_SILU) v[e] = silu_f(v[e]);
+      top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+    }
+    if constexpr (KIND == EPI_K_FP4) {
+      // (eight threads hold a block; those past the last column are whole blocks)
+      const uint32_t byte = scale4_of(max_over<8>(top));
+      [[maybe_unused]] const float inv = e8m0_inverse(byte);
+      if (m >= P.M || n >= P.N) continue;
+      uint32_t w = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0] * inv, v[1] * inv, 1.f, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.f, 1);
+#endif
+      *(uint16_t*)((uint8_t*)P.C + (int64_t)m * P.ldc + (n >> 1)) = (uint16_t)w;
+      if ((c & 7) == 0) P.Cs[(int64_t)m * P.ldcs + (n >> 5)] = (uint8_t)byte;
+      continue;
+    }
+    if (m >= P.M || n >= P.N) continue;
+    const int64_t at = (int64_t)m * P.ldc + n + (n >= P.gap_at ? P.gap : 0);
+    if (P.flags & DIT_EPI_F32) {
+      *(float4*)((float*)P.C + at) = make_float4(v[0], v[1], v[2], v[3]);
+      continue;
+    }
+    uint2* o = (uint2*)((bf16_t*)P.C + at);
+    if (P.flags & DIT_EPI_GATED_RES) {
+      const uint2 x = *o;
+      const float4 g = *(const float4*)(P.gate + n);
+      v[0] = __uint_as_float(x.x << 16) + g.x * v[0];
+      v[1] = __uint_as_float(x.x & 0xffff0000u) + g.y * v[1];
+      v[2] = __uint_as_float(x.y << 16) + g.z * v[2];
+      v[3] = __uint_as_float(x.y & 0xffff0000u) + g.w * v[3];
+    }
+    *o = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
 }
 
 }  // namespace
@@ -353,7 +822,45 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
     hipLaunchKernelGGL(fn, dim3((uint32_t)p.tiles_m * p.tiles_n), dim3(threads), 0, s, p);
     return hipGetLastError();
   };
-  return go(g.flags & DIT_EPI_FP4 ? gemm_fp4_tile_kernel<EPI_K_FP4> : gemm_fp4_tile_kernel<EPI_K_ANY>, 64, 128, 256);
+  const bool f32 = g.flags & DIT_EPI_F32, fp4 = g.flags & DIT_EPI_FP4, gated = g.flags & DIT_EPI_GATED_RES;
+  const bool plain = !(g.flags & DIT_EPI_SILU);
+  const bool store = plain && !gated && !fp4 && !f32 && (g.gelu_from >= g.N || g.gelu_from % 128 == 0) &&
+                     (g.gap == 0 || g.gap_at % 128 == 0);
+  const bool only_gate = plain && gated && g.rms_cols == 0 && g.gelu_from >= g.N && g.gap == 0;
+  auto tiles = [&](int bm, int bn) { return (int64_t)((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
+  // Few rows or few tiles: the narrowest tiles that fit the CUs once, to spread the way of W over them.
+  const bool one = g.M <= 16;
+  const int rows = one ? 16 : 32, widest = one ? 128 : 64;
+  int nt = g.rms_cols > 0 ? 128 : 32;
+  while (nt < widest && tiles(rows, nt) > n_cu) nt *= 2;
+  if (nt <= widest && tiles(rows, nt) <= n_cu) {
+#define DIT_SMALL(RB, K)                                                                                     \
+  go(nt == 128 ? gemm_fp4_small_kernel<128, RB, K> : nt == 64 ? gemm_fp4_small_kernel<64, RB, K>             \
+                                                              : gemm_fp4_small_kernel<32, RB, K>, rows, nt, 512)
+    if (fp4) return one ? DIT_SMALL(1, EPI_K_FP4) : DIT_SMALL(2, EPI_K_FP4);
+    return one ? DIT_SMALL(1, EPI_K_ANY) : DIT_SMALL(2, EPI_K_ANY);
+#undef DIT_SMALL
+  }
+  // Rounds of the chip times a tile's time, which is 4 us and some per slice of 256 of K.
+  struct Tile { int bm, bn, per_cu; double slice_us; };
+  auto cost = [&](const Tile& c) {
+    const int64_t slots = (int64_t)n_cu * c.per_cu;
+    return (double)((tiles(c.bm, c.bn) + slots - 1) / slots) * ((g.K + 255) / 256 * c.slice_us + 4);
+  };
+  const Tile cfg[] = {{64, 128, 2, 0.62}, {128, 128, 2, 1.0}, {256, 128, 1, 0.95}, {256, 256, 1, 1.5}};
+  int best = 0;
+  for (int c = 1; c < 4; ++c)
+    if (cost(cfg[c]) < cost(cfg[best])) best = c;
+  if (best == 3)
+    return go(fp4 ? gemm_fp4_ring_kernel<EPI_K_FP4> : store ? gemm_fp4_ring_kernel<EPI_K_STORE>
+              : only_gate ? gemm_fp4_ring_kernel<EPI_K_GATED> : gemm_fp4_ring_kernel<EPI_K_ANY>, 256, 256, 512);
+#define DIT_TILE(BM, THREADS)                                                                                  \
+  go(fp4 ? gemm_fp4_tile_kernel<BM, EPI_K_FP4> : store ? gemm_fp4_tile_kernel<BM, EPI_K_STORE>                  \
+                                                       : gemm_fp4_tile_kernel<BM, EPI_K_ANY>, BM, 128, THREADS)
+  if (best == 2) return DIT_TILE(256, 512);
+  if (best == 1) return DIT_TILE(128, 256);
+  return DIT_TILE(64, 256);
+#undef DIT_TILE
 }
 
 }  // namespace dit
