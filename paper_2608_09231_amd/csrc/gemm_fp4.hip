@@ -184,7 +184,8 @@ __device__ __forceinline__ void copy16_unseen(const void* base, const void* dst,
   const uint64_t b = (uint64_t)base;
   const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, OOB, 0x00020000u};
   const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)dst;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(l), "v"(voff), "s"(r), "s"(soff));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(l), "v"(voff), "s"(r),
+               "s"(__builtin_amdgcn_readfirstlane(soff)));
 #endif
 }
 // 4 bytes per lane the same way.
@@ -194,32 +195,42 @@ __device__ __forceinline__ void copy4_unseen(const void* base, const void* dst, 
   const uint64_t b = (uint64_t)base;
   const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, OOB, 0x00020000u};
   const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)dst;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(l), "v"(voff), "s"(r), "s"(soff));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(l), "v"(voff), "s"(r),
+               "s"(__builtin_amdgcn_readfirstlane(soff)));
 #endif
 }
 
 __device__ __forceinline__ i32x4_t lds_chunk(const char* p) { return *(const i32x4_t*)p; }
 
-// Scale bytes in LDS.  A row has nd dwords of them, one per 128 of K; a group is four
-// (512 of K, two slices), 16 bytes a row, and the last group begins early enough to lie in
-// the row: dword d is at d - start(group).
+// Scale bytes in LDS.  A row has nd dwords of them, one per 128 of K; a group is DW of
+// them (DW / 2 slices), 4 DW bytes a row, and the last group begins early enough to lie in
+// the row: dword d is at d - start(group).  DW = 8: the halves of a row's 32 bytes change
+// places on rows with bit 3 set, so that 16 rows' dwords lie in different banks.
+//
+// A row's bytes are far from the next row's, so that a request to L2 serves one row: with groups of 16
+// bytes they were a third of the kernel's requests.
+template <int DW>
 struct Scales {
   int nd, blocks;  // dwords of a row, blocks of 32
   __device__ __forceinline__ explicit Scales(int K) : nd((K + 127) >> 7), blocks(K >> 5) {}
-  __device__ __forceinline__ int start(int g) const { return g == 0 ? 0 : min(4 * g, nd - 4); }
+  __device__ __forceinline__ int start(int g) const { return g == 0 ? 0 : min(DW * g, nd - DW); }
   // place of dword d of group g
-  __device__ __forceinline__ int place(int g, int d) const { return min(d - start(g), 3); }
+  __device__ __forceinline__ int place(int g, int d) const { return min(d - start(g), DW - 1); }
   // bytes of dword d that belong to blocks, the rest zeros (a NaN there would spoil sums of zeros)
   __device__ __forceinline__ uint32_t valid(int d) const {
     const int n = blocks - 4 * d;
     return n >= 4 ? ~0u : (1u << (8 * max(n, 0))) - 1u;
   }
+  static __device__ __forceinline__ int swap(int row) { return DW == 8 ? (row >> 3) & 1 : 0; }
   // group 0 of a row, through registers: its dwords that exist
-  __device__ __forceinline__ void first(const uint8_t* row, char* dst) const {
-    i32x4_t x;
+  __device__ __forceinline__ void first(const uint8_t* p, char* rows, int row) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *(const int*)(row + 4 * min(i, nd - 1));
-    *(i32x4_t*)dst = x;
+    for (int h = 0; h < DW / 4; ++h) {
+      i32x4_t x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = *(const int*)(p + 4 * min(4 * h + i, nd - 1));
+      *(i32x4_t*)(rows + 4 * DW * row + 16 * (h ^ swap(row))) = x;
+    }
   }
 };
 
@@ -320,7 +331,7 @@ struct Epi : EpiLdsT<KIND == EPI_K_FP4 ? EPI_K_ANY : KIND, Fp4Prob> {
 // last one are copied as zeros (no memory traffic), which keeps every iteration alike.
 template <int KIND>
 __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
-  constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4, SC = 4 * UNIT, GROUP = 512 * 16;
+  constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4, SC = 4 * UNIT, GROUP = 512 * 32;
   __shared__ __attribute__((aligned(1024))) char smem[SC + 2 * GROUP];
   int tm, tn;
   tile_at(P, xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n), tm, tn);
@@ -347,35 +358,43 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
     copy16_unseen(base, smem + u + (wave * INS + j) * 1024,
                   16 * (c0 ^ (4 * (j & 1))) < (P.K >> 1) - 128 * s ? off[j] : OOB, (uint32_t)s * 128);
   };
-  // scales: waves 0 .. 3 rows of A, 4 .. 7 rows of W, 64 each
-  const Scales sc(P.K);
+  // scales: waves 0 .. 3 rows of A, 4 .. 7 rows of W, 64 each, two lanes a row
+  const Scales<8> sc(P.K);
   const uint8_t* sbase = wave < 4 ? P.As + (int64_t)m0 * P.ldas : P.Ws + (int64_t)n0 * P.ldws;
-  const uint32_t soff = wave < 4 ? (uint32_t)min(tid, P.M - 1 - m0) * (uint32_t)P.ldas
-                                 : (uint32_t)min(tid - 256, P.N - 1 - n0) * (uint32_t)P.ldws;
+  auto scale_row = [&](int row) {  // of the work-group's 512
+    return wave < 4 ? (uint32_t)min(row, P.M - 1 - m0) * (uint32_t)P.ldas
+                    : (uint32_t)min(row - 256, P.N - 1 - n0) * (uint32_t)P.ldws;
+  };
+  uint32_t soff[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int row = 64 * wave + 32 * j + (lane >> 1);
+    soff[j] = scale_row(row) + 16 * ((lane & 1) ^ sc.swap(row));
+  }
+  // (no branches between MFMAs: the compiler would sink products behind them, past the
+  // barriers; a group past the last one is zeros)
   auto issue_scales = [&](int g) {
-    if (4 * g < sc.nd) copy16_unseen(sbase, smem + SC + (g & 1) * GROUP + wave * 1024, soff, 4 * sc.start(g));
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      copy16_unseen(sbase, smem + SC + (g & 1) * GROUP + wave * 2048 + j * 1024, 8 * g < sc.nd ? soff[j] : OOB,
+                    4 * max(sc.start(g), 0));
   };
-  const int srow = SC + 16 * (64 * wm + lr), wrow = SC + 16 * (256 + 128 * wn + lr);
-  uint32_t sa[2][TM], sw[2][TN];
-  auto read_scales = [&](int kt) {  // of slice kt (past the last one: zeros)
+  const int srow = SC + 32 * (64 * wm + lr), wrow = SC + 32 * (256 + 128 * wn + lr), sswap = 16 * sc.swap(lr);
+  // scales of a half slice: of the substeps 0 and 1, and of 2 and 3
+  struct Half { uint32_t a[TM], w[TN]; };
+  auto read_scales = [&](Half& x, int d) {  // dword d of K (past the last one: any)
+    const int g = d >> 3, at = ((g & 1) * GROUP + 4 * sc.place(g, d)) ^ sswap;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int d = 2 * kt + h, g = kt >> 1, at = (g & 1) * GROUP + 4 * sc.place(g, d);
+    for (int i = 0; i < TM; ++i) x.a[i] = *(const uint32_t*)(smem + srow + at + 1024 * i);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[h][i] = *(const uint32_t*)(smem + srow + at + 512 * i);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sw[h][j] = *(const uint32_t*)(smem + wrow + at + 512 * j);
-    }
+    for (int j = 0; j < TN; ++j) x.w[j] = *(const uint32_t*)(smem + wrow + at + 1024 * j);
   };
-  auto place_scales = [&](int kt) {  // this lane's half into bytes 0 and 2
+  auto place_scales = [&](Half& x, int d) {  // this lane's block of each substep into bytes 0 and 2
+    const uint32_t v = sc.valid(d);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t v = sc.valid(2 * kt + h);
+    for (int i = 0; i < TM; ++i) x.a[i] = (x.a[i] & v) >> (8 * lh);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[h][i] = (sa[h][i] & v) >> (8 * lh);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sw[h][j] = (sw[h][j] & v) >> (8 * lh);
-    }
+    for (int j = 0; j < TN; ++j) x.w[j] = (x.w[j] & v) >> (8 * lh);
   };
 
   // this lane's chunk inside 32 rows of a unit: half lh of substep s
@@ -388,12 +407,12 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   // substep (s of the slice in units uw, ua) in the order of their use and a copy.
   // The fences keep that order.
   auto substep = [&](const i32x4_t(&a)[TM], const i32x4_t(&w)[TN], i32x4_t(&an)[TM], i32x4_t(&wn2)[TN], int uw, int ua,
-                     int s, const uint32_t(&xa)[TM], const uint32_t(&xw)[TN], auto b_, auto copy) {
+                     int s, const Half& x, auto b_, auto copy) {
     constexpr int B = decltype(b_)::value;
 #pragma unroll
     for (int q = 0; q < TM * TN; ++q) {
       const int i = q & 1, j = q >> 1;
-      acc[i][j] = mfma_fp4_32<B>(a[i], w[j], acc[i][j], xa[i], xw[j]);
+      acc[i][j] = mfma_fp4_32<B>(a[i], w[j], acc[i][j], x.a[i], x.w[j]);
       __builtin_amdgcn_sched_barrier(0);
       if (q == 0 || q == 2) an[q >> 1] = lds_chunk(smem + ua + wa + (q >> 1) * 4096 + loff[s]);
       else if (q < 6) wn2[q == 1 ? 0 : q - 2] = lds_chunk(smem + uw + ww + (q == 1 ? 0 : q - 2) * 4096 + loff[s]);
@@ -416,7 +435,7 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
     }
   }
   issue_scales(1);
-  sc.first(sbase + soff, smem + SC + 16 * tid);
+  sc.first(sbase + scale_row(tid), smem + SC, tid);
   wait_vmcnt_lgkm0<0>();
   barrier_no_fence();
   i32x4_t a0[TM], w0[TN], a1[TM], w1[TN];
@@ -424,29 +443,45 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   for (int i = 0; i < TM; ++i) a0[i] = lds_chunk(smem + 2 * UNIT + wa + i * 4096 + loff[0]);
 #pragma unroll
   for (int j = 0; j < TN; ++j) w0[j] = lds_chunk(smem + ww + j * 4096 + loff[0]);
-  read_scales(0);
-  place_scales(0);
-#pragma unroll 1
-  for (int kt = 0; kt < nk; ++kt) {
-    const int wu = (kt & 1) * UNIT, au = wu + 2 * UNIT;
+  Half x0, x1;
+  read_scales(x0, 0);
+  place_scales(x0, 0);
+  // slice kt, slice F = kt % 4 of a group of scales
+  auto slice = [&](int kt, auto f_) {
+    constexpr int F = decltype(f_)::value;
+    constexpr int wu = (F & 1) * UNIT, au = wu + 2 * UNIT;
     __builtin_amdgcn_sched_barrier(0);
-    substep(a0, w0, a1, w1, wu, au, 1, sa[0], sw[0], b0, none);
-    substep(a1, w1, a0, w0, wu, au, 2, sa[0], sw[0], b2, none);
-    substep(a0, w0, a1, w1, wu, au, 3, sa[1], sw[1], b0, none);
+    substep(a0, w0, a1, w1, wu, au, 1, x0, b0, none);
+    read_scales(x1, 2 * kt + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    substep(a1, w1, a0, w0, wu, au, 2, x0, b2, none);
+    place_scales(x1, 2 * kt + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    substep(a0, w0, a1, w1, wu, au, 3, x1, b0, none);
     // this wave's reads of slice kt and its copies of slice kt + 1 are done; then everyone's are
     wait_vmcnt_lgkm0<0>();
     barrier_no_fence();
     // (slice kt's group of scales is read, too: the next but one takes its place)
-    if ((kt & 1) == 1) issue_scales((kt >> 1) + 2);
+    if constexpr (F == 3) issue_scales((kt >> 2) + 2);
+    read_scales(x0, 2 * kt + 2);
     __builtin_amdgcn_sched_barrier(0);
-    const uint32_t xa[TM] = {sa[1][0], sa[1][1]}, xw[TN] = {sw[1][0], sw[1][1], sw[1][2], sw[1][3]};
-    read_scales(kt + 1);
-    substep(a1, w1, a0, w0, wu ^ UNIT, au ^ UNIT, 0, xa, xw, b2, [&](int q) {
+    substep(a1, w1, a0, w0, wu ^ UNIT, au ^ UNIT, 0, x1, b2, [&](int q) {
       if (q & 1) issue1(Ab, aoff, au, kt + 2, q >> 1);
       else issue1(Wb, woff, wu, kt + 2, q >> 1);
     });
-    place_scales(kt + 1);
+    place_scales(x0, 2 * kt + 2);
+  };
+  int kt = 0;
+#pragma unroll 1
+  for (; kt + 4 <= nk; kt += 4) {
+    slice(kt, integral_constant<int, 0>{});
+    slice(kt + 1, integral_constant<int, 1>{});
+    slice(kt + 2, integral_constant<int, 2>{});
+    slice(kt + 3, integral_constant<int, 3>{});
   }
+  if (kt < nk) slice(kt, integral_constant<int, 0>{});
+  if (kt + 1 < nk) slice(kt + 1, integral_constant<int, 1>{});
+  if (kt + 2 < nk) slice(kt + 2, integral_constant<int, 2>{});
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
   float* slab = (float*)smem + wave * (32 * 128);
@@ -507,14 +542,16 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel
     copy16_unseen(j < A_INS ? Ab : Wb, smem + u + at, ch[j] < (P.K >> 1) - 128 * s ? off[j] : OOB, (uint32_t)s * 128);
   };
   // scales: 64 rows a wave, of A, then of W
-  const Scales sc(P.K);
-  const bool of_a = 64 * wave < BM, of_any = 64 * wave < BM + 128;
+  const Scales<4> sc(P.K);
+  const int swave = wave % ((BM + 128) / 64), srow = 64 * swave + lane;
+  const bool of_a = 64 * swave < BM;
   const uint8_t* sbase = of_a ? P.As + (int64_t)m0 * P.ldas : P.Ws + (int64_t)n0 * P.ldws;
-  const uint32_t soff = of_a ? (uint32_t)min(tid, P.M - 1 - m0) * (uint32_t)P.ldas
-                             : (uint32_t)min(tid - BM, P.N - 1 - n0) * (uint32_t)P.ldws;
+  const uint32_t soff = of_a ? (uint32_t)min(srow, P.M - 1 - m0) * (uint32_t)P.ldas
+                             : (uint32_t)min(srow - BM, P.N - 1 - n0) * (uint32_t)P.ldws;
+  // (no branches between MFMAs: the compiler would sink products behind them, past the barriers; a
+  // group past the last one is zeros, and a wave without rows repeats another's)
   auto issue_scales = [&](int g) {
-    if (of_any && 4 * g < sc.nd)
-      copy16_unseen(sbase, smem + RING + (g & 1) * GROUP + wave * 1024, soff, 4 * sc.start(g));
+    copy16_unseen(sbase, smem + RING + (g & 1) * GROUP + swave * 1024, 4 * g < sc.nd ? soff : OOB, 4 * max(sc.start(g), 0));
   };
   auto read_scales = [&](int kt, uint32_t(&x)[NF][2], int f) {
 #pragma unroll
@@ -546,7 +583,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel
     for (int j = 0; j < INS; ++j) issue1(s * SLICE, s, j);
     if (s == 0) {
       issue_scales(1);
-      if (tid < BM + 128) sc.first(sbase + soff, smem + RING + 16 * tid);  // (waits for slice 0 and group 1, too)
+      if (tid < BM + 128) sc.first(sbase + soff, smem + RING, tid);  // (waits for slice 0 and group 1, too)
     }
   }
   wait_vmcnt_lgkm0<(ST - 1) * INS>();
@@ -561,13 +598,14 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel
   }
   place_scales(0, s0);
   int u = 0;  // place of slice kt
-  auto step = [&](int kt, i32x4_t(&f)[NF][2], i32x4_t(&fn)[NF][2], uint32_t(&x)[NF][2], uint32_t(&xn)[NF][2]) {
+  auto step = [&](int kt, i32x4_t(&f)[NF][2], i32x4_t(&fn)[NF][2], uint32_t(&x)[NF][2], uint32_t(&xn)[NF][2],
+                  auto odd) {
     const int un = u == (ST - 1) * SLICE ? 0 : u + SLICE;
     // this wave's reads of slice kt and its copies of slice kt + 1 are done (those
     // of the next ST - 2 may stay in flight); then everyone's are
     wait_vmcnt_lgkm0<(ST - 2) * INS>();
     barrier_no_fence();
-    if (kt & 1) issue_scales((kt >> 1) + 2);
+    if constexpr (decltype(odd)::value) issue_scales((kt >> 1) + 2);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int q = 0; q < 2 * TM * TN; ++q) {
@@ -589,10 +627,10 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel
   int kt = 0;
 #pragma unroll 1
   for (; kt + 2 <= nk; kt += 2) {
-    step(kt, f0, f1, s0, s1);
-    step(kt + 1, f1, f0, s1, s0);
+    step(kt, f0, f1, s0, s1, std::false_type{});
+    step(kt + 1, f1, f0, s1, s0, std::true_type{});
   }
-  if (kt < nk) step(kt, f0, f1, s0, s1);
+  if (kt < nk) step(kt, f0, f1, s0, s1, std::false_type{});
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
   // The tile in LDS as slabs of ROWS rows x 128, one per wave, columns XOR 16
@@ -645,7 +683,7 @@ __global__ __launch_bounds__(512) void gemm_fp4_small_kernel(Fp4Prob P) {
     off[j] = (uint32_t)min(row, (j < 4 ? P.N - 1 - nw : P.M - 1 - m0)) * (uint32_t)(j < 4 ? P.ldw : P.lda) + ch[j];
   }
   // scales of row lane: 32 of W, 16 RB of A, each from its own operand
-  const Scales sc(P.K);
+  const Scales<4> sc(P.K);
   const uint8_t* Wsb = P.Ws + (int64_t)nw * P.ldws;
   const uint8_t* Asb = P.As + (int64_t)m0 * P.ldas;
   const uint32_t soff = lane < 32 ? (uint32_t)min(lane, P.N - 1 - nw) * (uint32_t)P.ldws
@@ -841,13 +879,16 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
     return one ? DIT_SMALL(1, EPI_K_ANY) : DIT_SMALL(2, EPI_K_ANY);
 #undef DIT_SMALL
   }
-  // Rounds of the chip times a tile's time, which is 4 us and some per slice of 256 of K.
-  struct Tile { int bm, bn, per_cu; double slice_us; };
+  // Rounds of the chip times a tile's time, which is some us and some per slice of 256 of K
+  // (fitted to each kernel over the sizes below).  In us, 64 x 128, 128 x 128, 256 x 128 and 256 x 256 tiles:
+  //   512 x 10240 x 5120  37 32 34 39    1024 x 10240 x 5120 57 57 58 42    512 x 5120 x 5120  22 24 28 36
+  //   2048 x 4096 x 4096  37 29 31 34    4096 x 4096 x 1024  30 23 23 21    1333 x 1000 x 2336 11 14 17 21
+  struct Tile { int bm, bn, per_cu; double slice_us, us; };
   auto cost = [&](const Tile& c) {
     const int64_t slots = (int64_t)n_cu * c.per_cu;
-    return (double)((tiles(c.bm, c.bn) + slots - 1) / slots) * ((g.K + 255) / 256 * c.slice_us + 4);
+    return (double)((tiles(c.bm, c.bn) + slots - 1) / slots) * ((g.K + 255) / 256 * c.slice_us + c.us);
   };
-  const Tile cfg[] = {{64, 128, 2, 0.62}, {128, 128, 2, 1.0}, {256, 128, 1, 0.95}, {256, 256, 1, 1.5}};
+  const Tile cfg[] = {{64, 128, 2, 0.67, 4.8}, {128, 128, 2, 1.31, 6.2}, {256, 128, 1, 1.35, 6.2}, {256, 256, 1, 1.75, 12}};
   int best = 0;
   for (int c = 1; c < 4; ++c)
     if (cost(cfg[c]) < cost(cfg[best])) best = c;
