@@ -25,6 +25,7 @@ struct PackedArgs {
   bf16_t* o; int64_t ldo;
   const int32_t *qoff, *koff, *klen;
   int batch, Tq, Tk, kv_heads, group;
+  int workers, least;  // workers that share the units, and units that each takes at least
   float* ws;
   float scale_log2;
 };
@@ -86,8 +87,10 @@ __device__ __forceinline__ bool find_tile(const PackedArgs& P, int t, int rows, 
 __device__ __forceinline__ void copy16_unseen(const void* base, uint32_t bytes, const void* dst, uint32_t off) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  const uint64_t b = (uint64_t)base;
-  const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, bytes, 0x00020000u};
+  const uint64_t b = (uint64_t)base;  // (wave-uniform, also where the compiler holds it in vector registers)
+  const u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b),
+                   (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) & 0xffffu,
+                   (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
   const uint32_t l = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)dst;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(l), "v"(off), "s"(r));
 #endif
@@ -126,6 +129,393 @@ __device__ __forceinline__ bool not_finite(const bf16x8_t& f) {
     bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
   }
   return bad;
+}
+
+// A launch's work as one line of units: sequence by sequence, tile of R rows by tile and key head
+// by key head (an item), KEYS keys of it each (one unit at least).  Workers take `per`
+// consecutive units each, so that sequences of any lengths fill the chip evenly; where an item is
+// shared its parts are joined from the workspace.  Worker w's part of item i lies in slot w + i
+// there: from one part to the next either w or i grows.
+struct Place {
+  int z, tile, kh, unit, n;  // unit of n
+  int64_t item;
+};
+__device__ __forceinline__ int64_t readlane64(int64_t v, int l) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)v, l) |
+                   (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32);
+}
+template <int R, int KEYS>
+struct Line {
+  const PackedArgs& P;
+  int z0, n;                  // 64 sequences from z0 on, one a lane: units of an item,
+  int64_t items, cost;        // items and units of the sequence,
+  int64_t items_end, cost_end;  // and up to its end from z0 on
+  int64_t items_base, cost_base;  // those before z0
+
+  __device__ __forceinline__ explicit Line(const PackedArgs& P_) : P(P_), items_base(0), cost_base(0) { load(0); }
+  __device__ __forceinline__ void load(int z) {
+    z0 = z;
+    const int lane = threadIdx.x & 63;
+    Seq s{0, 0, 0, 0};
+    if (z0 + lane < P.batch) s = seq_of(P, z0 + lane);
+    n = max(1, (s.lk + KEYS - 1) / KEYS);
+    items = (int64_t)((s.lq * P.group + R - 1) / R) * P.kv_heads;
+    cost = items * n;
+    items_end = items;
+    cost_end = cost;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t a = __shfl_up((long long)items_end, o, 64), b = __shfl_up((long long)cost_end, o, 64);
+      items_end += lane >= o ? a : 0;
+      cost_end += lane >= o ? b : 0;
+    }
+  }
+  __device__ __forceinline__ void next() {
+    items_base += readlane64(items_end, 63);
+    cost_base += readlane64(cost_end, 63);
+    load(z0 + 64);
+  }
+  __device__ __forceinline__ int64_t total() const {
+    if (P.batch <= 64) return readlane64(cost_end, 63);
+    Line l(P);
+    while (l.z0 + 64 < P.batch) l.next();
+    return l.cost_base + readlane64(l.cost_end, 63);
+  }
+  // Place of unit u (below the total, not before the last one asked for).
+  __device__ __forceinline__ Place at(int64_t u) {
+    while (u >= cost_base + readlane64(cost_end, 63)) next();
+    const int l = __ffsll((unsigned long long)__ballot(cost_base + cost_end > u)) - 1;
+    Place p;
+    p.z = z0 + l;
+    p.n = __builtin_amdgcn_readlane(n, l);
+    const int64_t rest = u - cost_base - (readlane64(cost_end, l) - readlane64(cost, l));
+    const int64_t i = readlane64(rest / p.n, 0);
+    p.unit = __builtin_amdgcn_readfirstlane((int)(rest - i * p.n));
+    p.item = items_base + readlane64(items_end, l) - readlane64(items, l) + i;
+    p.tile = __builtin_amdgcn_readfirstlane((int)(i / P.kv_heads));
+    p.kh = __builtin_amdgcn_readfirstlane((int)(i - (int64_t)p.tile * P.kv_heads));
+    return p;
+  }
+};
+__device__ __forceinline__ int64_t units_each(int64_t total, int workers, int least) {
+  return max((int64_t)least, (total + workers - 1) / workers);
+}
+
+// A part of an item: its unnormalised outputs [R][128], row sums and running maxima.
+__host__ __device__ __forceinline__ int64_t part_floats(int rows) { return (int64_t)rows * (D + 2); }
+
+// Joins the parts of an item's rows and stores the normalised output.  32 threads a
+// row, 4 columns each; PG of them take consecutive parts, U at a time, whose loads are in flight
+// together, and the PG meet in LDS in their order.
+template <int R, int KEYS, int PG>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int U = 8, RB = 8 / PG;
+  __shared__ float red[6][256];
+  const int64_t item = blockIdx.x;
+  const int tid = threadIdx.x, pg = (tid >> 5) % PG, c = 4 * (tid & 31);
+  const int row = blockIdx.y * RB + (tid >> 5) / PG;
+  Line<R, KEYS> line(P);
+  const int64_t per = units_each(line.total(), P.workers, P.least);
+  while (item >= line.items_base + readlane64(line.items_end, 63)) {
+    if (line.z0 + 64 >= P.batch) return;
+    line.next();
+  }
+  const int l = __ffsll((unsigned long long)__ballot(line.items_base + line.items_end > item)) - 1;
+  const int z = line.z0 + l, n = __builtin_amdgcn_readlane(line.n, l);
+  const int64_t i = item - line.items_base - (readlane64(line.items_end, l) - readlane64(line.items, l));
+  const int64_t a = line.cost_base + readlane64(line.cost_end, l) - readlane64(line.cost, l) + i * n;
+  const int64_t w0 = a / per, w1 = (a + n - 1) / per;
+  if (w0 == w1) return;  // one worker has stored it
+  const Seq s = seq_of(P, z);
+  const int tile = (int)(i / P.kv_heads), kh = (int)(i - (int64_t)tile * P.kv_heads);
+  const int r = tile * R + row, qi = r / P.group, h = kh * P.group + r - qi * P.group;
+  const bool in = r < s.lq * P.group;
+  const int parts = (int)(w1 - w0) + 1, each = (parts + PG - 1) / PG;
+  const int p0 = pg * each, p1 = in ? min(parts, p0 + each) : 0;
+  const int64_t pf = part_floats(R);
+  const float* w = P.ws + (w0 + item) * pf;
+  float mx = -INFINITY, den = 0.f;
+  f32x4_t y = {};
+  auto rescale = [&](float nm) {
+    const float f = __builtin_amdgcn_exp2f(mx + neg_shift(nm));
+    den *= f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] *= f;
+    mx = nm;
+  };
+  auto add = [&](float m, float ls, const f32x4_t& v) {  // one more part, of weight 2^m
+    const float f = __builtin_amdgcn_exp2f(m + neg_shift(mx));
+    den += f * ls;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += f * v[e];
+  };
+  for (int p = p0; p < p1; p += U) {
+    f32x4_t v[U];
+    float m[U], ls[U], nm = mx;
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const float* x = w + min(p + j, p1 - 1) * pf;
+      v[j] = *(const f32x4_t*)(x + row * D + c);
+      ls[j] = x[R * D + row];
+      m[j] = x[R * D + R + row];
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) nm = fmaxf(nm, m[j]);
+    rescale(nm);
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (p + j < p1) add(m[j], ls[j], v[j]);
+  }
+  if constexpr (PG > 1) {
+    red[0][tid] = mx;
+    red[1][tid] = den;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[2 + e][tid] = y[e];
+    __syncthreads();
+    if (pg) return;
+    float nm = mx;
+#pragma unroll
+    for (int j = 1; j < PG; ++j) nm = fmaxf(nm, red[0][tid + 32 * j]);
+    rescale(nm);
+#pragma unroll
+    for (int j = 1; j < PG; ++j) {
+      const int t = tid + 32 * j;
+      add(red[0][t], red[1][t], f32x4_t{red[2][t], red[3][t], red[4][t], red[5][t]});
+    }
+  }
+  if (!in) return;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  *(uint2*)(P.o + (int64_t)(s.q0 + qi) * P.ldo + (int64_t)h * D + c) =
+      make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
+#endif
+}
+
+// Few rows a sequence (single tokens and their heads): what bounds it is the way of K
+// and V from memory.  Every wave is a worker with units of 32 keys in two buffers
+// of LDS of its own, and no wave waits for another.  With MFMAs to spare, probabilities
+// enter the second product as two bf16 parts, so that only the output is rounded to 8 bits.
+template <bool BOUNDED, bool CAUSAL, int NG>
+__global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int HK = 32, TILE = HK * D * 2, STAGE = 2 * TILE, R = 16 * NG;
+  __shared__ __attribute__((aligned(1024))) char smem[8 * STAGE];  // [wave][stage][K | V]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lq = lane >> 4;
+  const int worker = blockIdx.x * 4 + wave;
+  Line<R, HK> line(P);
+  const int64_t total = line.total(), per = units_each(total, P.workers, P.least);
+  const int64_t begin = worker * per, end = min(total, begin + per);
+  if (begin >= end) return;
+
+  // copy c: rows 4 c .. + 3; rows past the last key, and all of none, are zeros
+  auto issue = [&](const Place& p, const Seq& s, bool any, int st) {
+    const int key = p.unit * HK;
+    const int rows = any ? min(s.lk - key, HK) : 0;
+    const int64_t at = s.k0 + (rows > 0 ? key : 0);
+    const bf16_t* kp = P.k + at * P.ldk + (int64_t)p.kh * D;
+    const bf16_t* vp = P.v + at * P.ldv + (int64_t)p.kh * D;
+    const uint32_t kn = rows > 0 ? (uint32_t)(rows - 1) * (uint32_t)P.ldk * 2u + 2u * D : 0u;
+    const uint32_t vn = rows > 0 ? (uint32_t)(rows - 1) * (uint32_t)P.ldv * 2u + 2u * D : 0u;
+    char* d = smem + (2 * wave + st) * STAGE;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t row = 4 * c + (lane >> 4), ch = ((lane & 15) ^ (row & 15)) << 4;
+      copy16_unseen(kp, kn, d + c * 1024, row * (uint32_t)P.ldk * 2u + ch);
+      copy16_unseen(vp, vn, d + TILE + c * 1024, row * (uint32_t)P.ldv * 2u + ch);
+    }
+  };
+  int koff[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) koff[s] = k_off(lr, 4 * s + lq);
+  const int voff = k_off(4 * lq + (lr >> 2), (lr & 3) >> 1) + 8 * (lr & 1);  // as in attn_packed_kernel
+
+  bf16x8_t qf[NG][4];
+  f32x4_t acc[8][NG];
+  float m[NG], l[NG];
+  int lim[NG], common = 0, first = 0;  // first unit of this worker's part of the item
+  auto enter = [&](const Place& p, const Seq& s) {  // an item: its queries
+    const int nrows = s.lq * P.group, past = s.lk - s.lq + 1;
+    auto seen = [&](int row) { return CAUSAL ? max(past + row / P.group, 0) : s.lk; };
+    common = seen(p.tile * R);
+    first = p.unit;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int row = min(p.tile * R + 16 * g + lr, nrows - 1), qi = row / P.group, h = p.kh * P.group + row - qi * P.group;
+      lim[g] = seen(row);
+      const bf16_t* qp = P.q + (int64_t)(s.q0 + qi) * P.ldq + (int64_t)h * D + 8 * lq;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) qf[g][t] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 32 * t));
+      m[g] = BOUNDED ? BOUNDED_SHIFT_LOG2 : -INFINITY;
+      l[g] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[dt][g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g)  // (queries waited for later would wait for the copies, too)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(qf[g][t]));
+  };
+  auto leave = [&](const Place& p, const Seq& s) {
+    const int nrows = s.lq * P.group;
+    const bool whole = first == 0 && p.unit == p.n - 1;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int at = 16 * g + lr, row = p.tile * R + at;
+      const float ls = sum_quarters(l[g]);
+      if (row >= nrows) continue;
+      if (whole) {
+        const int qi = row / P.group, h = p.kh * P.group + row - qi * P.group;
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;  // no key: zeros
+        bf16_t* op = P.o + (int64_t)(s.q0 + qi) * P.ldo + (int64_t)h * D + 4 * lq;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+          *(uint2*)(op + 16 * dt) = make_uint2(pack_bf16x2(acc[dt][g][0] * inv, acc[dt][g][1] * inv),
+                                               pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
+      } else {
+        float* w = P.ws + (worker + p.item) * part_floats(R);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(w + at * D + 16 * dt + 4 * lq) = acc[dt][g];
+        if (lq == 0) {
+          w[R * D + at] = ls;
+          w[R * D + R + at] = m[g];
+        }
+      }
+    }
+  };
+
+  Place cur = line.at(begin);
+  Seq seq = seq_of(P, cur.z);
+  issue(cur, seq, true, 0);
+  enter(cur, seq);
+  int st = 0;
+  for (int64_t u = begin; u < end; ++u) {
+    Place nxt = cur;
+    Seq nseq = seq;
+    const bool more = u + 1 < end, change = more && cur.unit + 1 == cur.n;
+    if (change) {
+      nxt = line.at(u + 1);
+      nseq = seq_of(P, nxt.z);
+    } else {
+      ++nxt.unit;
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the other buffer is read
+    asm volatile("" ::: "memory");
+    issue(nxt, nseq, more, st ^ 1);
+    wait_vmcnt<16>();  // this one has landed
+    asm volatile("" ::: "memory");
+    const char* sk = smem + (2 * wave + st) * STAGE;
+    const int key = cur.unit * HK;
+    f32x4_t s[2][NG];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t] + b * 16 * 256));
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+          s[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t], t ? s[b][g] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+    const bool masked = key + HK > common;
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            if (key + 16 * b + 4 * lq + r >= lim[g]) s[b][g][r] = -INFINITY;
+    }
+    bf16x8_t ph[NG], pl[NG];  // probabilities: bf16 and what it leaves
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if constexpr (!BOUNDED) {
+        float mx = s[0][g][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; r += 2) mx = max3(mx, s[b][g][r], s[b][g][r + 1]);
+        mx = max_quarters(mx) * P.scale_log2;
+        const bool up = mx > m[g] + RESCALE_SLACK;
+        if (__builtin_amdgcn_ballot_w64(up)) {
+          const float mn = up ? mx : m[g];
+          const float a = up ? __builtin_amdgcn_exp2f(m[g] - mn) : 1.f;
+          l[g] *= a;
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[dt][g][r] *= a;
+          m[g] = mn;
+        }
+      }
+      const float mneg = BOUNDED ? -BOUNDED_SHIFT_LOG2 : neg_shift(m[g]);
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][g][e & 3], P.scale_log2, mneg));
+        ph[g][e] = (__bf16)p;
+        pl[g][e] = (__bf16)(p - (float)ph[g][e]);
+        sum += p;
+      }
+      l[g] += sum;
+    }
+    auto v_frag = [&](int dt) { return vt_frag(sk + TILE + (voff ^ (dt << 5))); };
+    // 0 times a value that is not finite would reach the rows that do not see its key
+    bool spoilt = false;
+    if (CAUSAL && masked) {
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) spoilt |= not_finite(v_frag(dt));
+      spoilt = __builtin_amdgcn_ballot_w64(spoilt) != 0;
+    }
+    if (!CAUSAL || !spoilt) {
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        const bf16x8_t vf = v_frag(dt);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[g], acc[dt][g], 0, 0, 0);
+          acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[g], acc[dt][g], 0, 0, 0);
+        }
+      }
+    } else {
+      // key by key: a lane keeps the product only if its row sees the key
+#pragma unroll 1
+      for (int j = 0; j < HK; ++j) {
+        const bool mine = ((j >> 2) & 3) == lq;
+        const int e0 = 4 * (j >> 4) + (j & 3);
+        bf16x8_t hj[NG], lj[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            hj[g][e] = mine && e == e0 ? ph[g][e] : (__bf16)0.f;
+            lj[g][e] = mine && e == e0 ? pl[g][e] : (__bf16)0.f;
+          }
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          bf16x8_t vj = v_frag(dt);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) vj[e] = mine && e == e0 ? vj[e] : (__bf16)0.f;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            f32x4_t y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vj, hj[g], acc[dt][g], 0, 0, 0);
+            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vj, lj[g], y, 0, 0, 0);
+            if (key + j < lim[g]) acc[dt][g] = y;
+          }
+        }
+      }
+    }
+    if (change || !more) {
+      leave(cur, seq);
+      if (more) enter(nxt, nseq);
+    }
+    cur = nxt;
+    seq = nseq;
+    st ^= 1;
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // no copy outlives its work-group
+#endif
 }
 
 constexpr int ROWS = 128;
@@ -341,7 +731,24 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 
 }  // namespace
 
-size_t attention_packed_ws_bytes(const dit_packed_shape&) { return 0; }
+// Few rows a sequence, on average: the memory-bound kernel, a wave of which takes 16 or 32.
+int few_rows(const dit_packed_shape& s) {
+  const int64_t rows = (int64_t)s.Tq * (s.heads / s.kv_heads);
+  return rows <= 16 * (int64_t)s.batch ? 16 : rows <= 32 * (int64_t)s.batch ? 32 : 0;
+}
+// tiles of r rows of a key head, at most: whole ones and one begun by each sequence
+int64_t tiles_of(const dit_packed_shape& s, int r) {
+  return (int64_t)s.Tq * (s.heads / s.kv_heads) / r + std::min(s.batch, s.Tq);
+}
+// Waves of 256 CUs (by the shape alone: the workspace's size does not depend on the device).
+constexpr int FEW_WORKERS = 1024, FEW_LEAST = 4;
+
+size_t attention_packed_ws_bytes(const dit_packed_shape& s) {
+  if (s.batch == 0 || s.Tq == 0) return 0;
+  const int few = few_rows(s);
+  if (few) return (FEW_WORKERS + tiles_of(s, few) * s.kv_heads) * part_floats(few) * sizeof(float);
+  return 0;
+}
 
 hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                    const void* v, int64_t ldv, void* o, int64_t ldo, bool bounded, bool causal, void* ws,
@@ -354,11 +761,23 @@ hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int
   P.batch = s.batch; P.Tq = s.Tq; P.Tk = s.Tk; P.kv_heads = s.kv_heads; P.group = s.heads / s.kv_heads;
   P.ws = (float*)ws;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
-  // tiles of a key head, at most: whole ones and one begun by each sequence
-  const int64_t tiles = (int64_t)s.Tq * P.group / ROWS + std::min(s.batch, s.Tq);
-  void (*fn)(PackedArgs) = causal ? (bounded ? attn_packed_kernel<true, true> : attn_packed_kernel<false, true>)
-                                  : (bounded ? attn_packed_kernel<true, false> : attn_packed_kernel<false, false>);
-  hipLaunchKernelGGL(fn, dim3((uint32_t)(tiles * s.kv_heads)), dim3(256), 0, st, P);
+  void (*fn)(PackedArgs);
+#define DIT_PICK(kernel, ...)                                                                              \
+  (causal ? (bounded ? kernel<true, true __VA_ARGS__> : kernel<false, true __VA_ARGS__>)                   \
+          : (bounded ? kernel<true, false __VA_ARGS__> : kernel<false, false __VA_ARGS__>))
+#define DIT_COMMA ,
+  if (const int few = few_rows(s)) {
+    P.workers = FEW_WORKERS;
+    P.least = FEW_LEAST;
+    fn = few == 16 ? DIT_PICK(attn_packed_few_kernel, DIT_COMMA 1) : DIT_PICK(attn_packed_few_kernel, DIT_COMMA 2);
+    hipLaunchKernelGGL(fn, dim3(FEW_WORKERS / 4), dim3(256), 0, st, P);
+    const uint32_t items = (uint32_t)(tiles_of(s, few) * s.kv_heads);
+    if (few == 16) hipLaunchKernelGGL((packed_join_kernel<16, 32, 4>), dim3(items, 8), dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((packed_join_kernel<32, 32, 4>), dim3(items, 16), dim3(256), 0, st, P);
+    return hipGetLastError();
+  }
+  fn = DIT_PICK(attn_packed_kernel);
+  hipLaunchKernelGGL(fn, dim3((uint32_t)(tiles_of(s, ROWS) * s.kv_heads)), dim3(256), 0, st, P);
   return hipGetLastError();
 }
 
