@@ -25,6 +25,7 @@ struct PackedArgs {
   bf16_t* o; int64_t ldo;
   const int32_t *qoff, *koff, *klen;
   int batch, Tq, Tk, kv_heads, group;
+  int ranked;          // tiles in the order of their keys, most first
   int workers, least;  // workers that share the units, and units that each takes at least
   float* ws;
   float scale_log2;
@@ -35,10 +36,6 @@ struct Seq {
   int q0, lq, k0, lk;
 };
 __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return min(max(x, lo), hi); }
-__device__ __forceinline__ int queries_of(const PackedArgs& P, int z) {
-  const int a = clamp_to(P.qoff[z], 0, P.Tq);
-  return clamp_to(P.qoff[z + 1], a, P.Tq) - a;
-}
 __device__ __forceinline__ Seq seq_of(const PackedArgs& P, int z) {
   Seq s;
   s.q0 = clamp_to(P.qoff[z], 0, P.Tq);
@@ -49,29 +46,58 @@ __device__ __forceinline__ Seq seq_of(const PackedArgs& P, int z) {
   return s;
 }
 
-// Sum of v over the lanes up to this one.
+// Sum of v over the lanes up to this one, on the VALU (rows of 16 lanes, then their
+// last lanes' sums to the rows behind).
 __device__ __forceinline__ int scan_lanes(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    v += lane >= o ? u : 0;
-  }
+#if defined(__HIP_DEVICE_COMPILE__)
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // 1, 2, 4 and 8 lanes before, in a row
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next, 31 to the upper half
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+#endif
   return v;
+}
+// The same of 64-bit values, halves moved alike.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int64_t lanes_before(int64_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROW_MASK, 0xf, false);
+  return (int64_t)((uint64_t)(uint32_t)lo | (uint64_t)(uint32_t)hi << 32);
+#else
+  return 0;
+#endif
+}
+__device__ __forceinline__ int64_t scan_lanes64(int64_t v) {
+  v += lanes_before<0x111, 0xf>(v);
+  v += lanes_before<0x112, 0xf>(v);
+  v += lanes_before<0x114, 0xf>(v);
+  v += lanes_before<0x118, 0xf>(v);
+  v += lanes_before<0x142, 0xa>(v);
+  return v + lanes_before<0x143, 0xc>(v);
+}
+__device__ __forceinline__ int sum_lanes(int v) { return __builtin_amdgcn_readlane(scan_lanes(v), 63); }
+__device__ __forceinline__ Seq seq_of_lane(const Seq& s, int l) {
+  return Seq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.lq, l), __builtin_amdgcn_readlane(s.k0, l),
+             __builtin_amdgcn_readlane(s.lk, l)};
 }
 
 // The sequence that tile t of `rows` rows falls in, 64 sequences at a time, and the
-// tile's number in it; false past the last one.
-__device__ __forceinline__ bool find_tile(const PackedArgs& P, int t, int rows, int& z, int& tile) {
+// tile's number in it, its last one first; false past the last one.
+__device__ __forceinline__ bool find_tile(const PackedArgs& P, int t, int rows, Seq& seq, int& tile) {
   const int lane = threadIdx.x & 63;
   for (int z0 = 0; z0 < P.batch; z0 += 64) {
-    const int n = z0 + lane < P.batch ? (queries_of(P, z0 + lane) * P.group + rows - 1) / rows : 0;
+    Seq s{0, 0, 0, 0};
+    if (z0 + lane < P.batch) s = seq_of(P, z0 + lane);
+    const int n = (s.lq * P.group + rows - 1) / rows;
     const int end = scan_lanes(n);
     const uint64_t past = __ballot(end > t);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;
-      z = z0 + l;
-      tile = t - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(n, l));
+      seq = seq_of_lane(s, l);
+      tile = __builtin_amdgcn_readlane(end, l) - 1 - t;
       return true;
     }
     t -= __builtin_amdgcn_readlane(end, 63);
@@ -161,14 +187,8 @@ struct Line {
     n = max(1, (s.lk + KEYS - 1) / KEYS);
     items = (int64_t)((s.lq * P.group + R - 1) / R) * P.kv_heads;
     cost = items * n;
-    items_end = items;
-    cost_end = cost;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t a = __shfl_up((long long)items_end, o, 64), b = __shfl_up((long long)cost_end, o, 64);
-      items_end += lane >= o ? a : 0;
-      cost_end += lane >= o ? b : 0;
-    }
+    items_end = scan_lanes64(items);
+    cost_end = scan_lanes64(cost);
   }
   __device__ __forceinline__ void next() {
     items_base += readlane64(items_end, 63);
@@ -207,14 +227,14 @@ __host__ __device__ __forceinline__ int64_t part_floats(int rows) { return (int6
 // Joins the parts of an item's rows and stores the normalised output.  32 threads a
 // row, 4 columns each; PG of them take consecutive parts, U at a time, whose loads are in flight
 // together, and the PG meet in LDS in their order.
+// A work-group takes `rows` rows, 8 / PG at a time.
 template <int R, int KEYS, int PG>
-__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P) {
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int U = 8, RB = 8 / PG;
   __shared__ float red[6][256];
   const int64_t item = blockIdx.x;
   const int tid = threadIdx.x, pg = (tid >> 5) % PG, c = 4 * (tid & 31);
-  const int row = blockIdx.y * RB + (tid >> 5) / PG;
   Line<R, KEYS> line(P);
   const int64_t per = units_each(line.total(), P.workers, P.least);
   while (item >= line.items_base + readlane64(line.items_end, 63)) {
@@ -229,12 +249,13 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P) {
   if (w0 == w1) return;  // one worker has stored it
   const Seq s = seq_of(P, z);
   const int tile = (int)(i / P.kv_heads), kh = (int)(i - (int64_t)tile * P.kv_heads);
-  const int r = tile * R + row, qi = r / P.group, h = kh * P.group + r - qi * P.group;
-  const bool in = r < s.lq * P.group;
   const int parts = (int)(w1 - w0) + 1, each = (parts + PG - 1) / PG;
-  const int p0 = pg * each, p1 = in ? min(parts, p0 + each) : 0;
   const int64_t pf = part_floats(R);
   const float* w = P.ws + (w0 + item) * pf;
+  for (int row0 = blockIdx.y * rows; row0 < min((int)(blockIdx.y + 1) * rows, s.lq * P.group - tile * R); row0 += RB) {
+  const int row = row0 + (tid >> 5) / PG, r = tile * R + row, qi = r / P.group, h = kh * P.group + r - qi * P.group;
+  const bool in = r < s.lq * P.group;
+  const int p0 = pg * each, p1 = in ? min(parts, p0 + each) : 0;
   float mx = -INFINITY, den = 0.f;
   f32x4_t y = {};
   auto rescale = [&](float nm) {
@@ -268,12 +289,13 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P) {
       if (p + j < p1) add(m[j], ls[j], v[j]);
   }
   if constexpr (PG > 1) {
+    __syncthreads();  // (the rows before are read)
     red[0][tid] = mx;
     red[1][tid] = den;
 #pragma unroll
     for (int e = 0; e < 4; ++e) red[2 + e][tid] = y[e];
     __syncthreads();
-    if (pg) return;
+    if (pg) continue;
     float nm = mx;
 #pragma unroll
     for (int j = 1; j < PG; ++j) nm = fmaxf(nm, red[0][tid + 32 * j]);
@@ -284,10 +306,11 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P) {
       add(red[0][t], red[1][t], f32x4_t{red[2][t], red[3][t], red[4][t], red[5][t]});
     }
   }
-  if (!in) return;
+  if (!in) continue;
   const float inv = den == 0.f ? 0.f : 1.f / den;
   *(uint2*)(P.o + (int64_t)(s.q0 + qi) * P.ldo + (int64_t)h * D + c) =
       make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
+  }
 #endif
 }
 
@@ -335,10 +358,12 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   f32x4_t acc[8][NG];
   float m[NG], l[NG];
   int lim[NG], common = 0, first = 0;  // first unit of this worker's part of the item
+  bool uneven = false;                 // whether some rows see more keys than others
   auto enter = [&](const Place& p, const Seq& s) {  // an item: its queries
     const int nrows = s.lq * P.group, past = s.lk - s.lq + 1;
     auto seen = [&](int row) { return CAUSAL ? max(past + row / P.group, 0) : s.lk; };
     common = seen(p.tile * R);
+    uneven = common != seen(min(p.tile * R + R, nrows) - 1);
     first = p.unit;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -463,7 +488,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
     auto v_frag = [&](int dt) { return vt_frag(sk + TILE + (voff ^ (dt << 5))); };
     // 0 times a value that is not finite would reach the rows that do not see its key
     bool spoilt = false;
-    if (CAUSAL && masked) {
+    if (CAUSAL && masked && uneven) {
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) spoilt |= not_finite(v_frag(dt));
       spoilt = __builtin_amdgcn_ballot_w64(spoilt) != 0;
@@ -519,39 +544,110 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
 }
 
 constexpr int ROWS = 128;
+typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
+
+// Tile of rank t among the tiles of a key head in the order of their keys, most first, so that
+// a launch ends with short ones: up to 64 sequences, one a lane; false past the last tile.
+// Of a sequence with T tiles those from first(c) on have c key blocks of 64 or more.
+template <bool CAUSAL>
+__device__ __forceinline__ bool ranked_tile(const PackedArgs& P, int t, Seq& seq, int& tile) {
+  const int lane = threadIdx.x & 63;
+  Seq s{0, 0, 0, 0};
+  if (lane < P.batch) s = seq_of(P, lane);
+  const int T = (s.lq * P.group + ROWS - 1) / ROWS, past = s.lk - s.lq + 1;
+  const int top = (s.lk + KT - 1) / KT;  // key blocks of the last tile
+  auto first = [&](int c) {
+    if (c <= 0) return 0;
+    if (c > top) return T;
+    if (!CAUSAL) return 0;
+    // the tile's last query, (128 j + 127) / group, sees past + query > 64 (c - 1) keys
+    const int64_t need = (int64_t)(KT * (c - 1) - past + 1) * P.group - (ROWS - 1);
+    return need <= 0 ? 0 : (int)min((int64_t)T - 1, (need + ROWS - 1) / ROWS);  // (the last one sees all)
+  };
+  auto count = [&](int c) {  // tiles with c blocks or more
+    return sum_lanes(T - first(c));
+  };
+  if (t >= count(0)) return false;
+  int lo = 0, hi = T ? top : 0;  // count(lo) > t >= count(hi)
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) hi = max(hi, __shfl_xor(hi, o, 64));
+  hi = __builtin_amdgcn_readfirstlane(hi) + 1;
+  while (hi - lo > 1) {
+    const int c = (lo + hi) >> 1;
+    if (count(c) > t) lo = c;
+    else hi = c;
+  }
+  t -= count(hi);
+  const int here = first(hi) - first(lo), end = scan_lanes(here);
+  const int l = __ffsll((unsigned long long)__ballot(end > t)) - 1;
+  seq = seq_of_lane(s, l);
+  tile = __builtin_amdgcn_readlane(first(lo) + here, l) - 1 -
+         (t - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(here, l)));
+  return true;
+}
 
 // 128 rows of a sequence and key head: four waves of 32, tiles of 64 keys of K and V in
 // XOR-swizzled LDS rows of 256 bytes, two of each; S^T = K Q^T, O^T = V^T P^T,
 // probabilities from one to the other in registers, V^T read from the row-major
 // tile by transposing LDS reads.  Probabilities are rounded to bf16, the type that
 // the second product takes beside V; the sum takes the rounded values, so that the weights add up to one.
-template <bool BOUNDED, bool CAUSAL>
+//
+// SPLIT: launches whose tiles are fewer than the chip's places for work-groups share the units
+// of the whole launch out (Line); a work-group may go through parts of several items.
+template <bool BOUNDED, bool CAUSAL, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int TILE = KT * D * 2, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];  // [stage][K | V]
+  __shared__ int bad[4];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lq = lane >> 4;
-  const int unit = blockIdx.x, kh = unit % P.kv_heads;
-  int z, tile;
-  if (!find_tile(P, unit / P.kv_heads, ROWS, z, tile)) return;
-  z = __builtin_amdgcn_readfirstlane(z);
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  const Seq s_ = seq_of(P, z);
+  const int worker = blockIdx.x;
+  int64_t u = 0, end = 1;
+  Place p{};
+  Seq s_;
+  if constexpr (SPLIT) {
+    Line<ROWS, KT> line(P);
+    const int64_t total = line.total(), per = units_each(total, P.workers, P.least);
+    u = worker * per;
+    end = min(total, u + per);
+    if (u >= end) return;
+  } else {
+    p.kh = worker % P.kv_heads;
+    const int t = worker / P.kv_heads;
+    // (the order matters where work-groups wait for their turn)
+    const bool any = P.ranked ? ranked_tile<CAUSAL>(P, t, s_, p.tile) : find_tile(P, t, ROWS, s_, p.tile);
+    if (!any) return;
+  }
+#pragma unroll 1
+  do {
+  if constexpr (SPLIT) {
+    Line<ROWS, KT> line(P);  // (anew for each item: few, and the registers are the loop's)
+    p = line.at(u);
+    s_ = seq_of(P, p.z);
+  }
+  const int tile = p.tile, kh = p.kh;
   const int nrows = s_.lq * P.group;
-  if (CAUSAL) tile = (nrows + ROWS - 1) / ROWS - 1 - tile;  // the longest first
   // keys that query i sees: past + i, at most all; not causal: all
   const int past = s_.lk - s_.lq + 1;
   auto seen = [&](int row) { return CAUSAL ? max(past + row / P.group, 0) : s_.lk; };
   const int wrow = tile * ROWS + 32 * wave;
-  const int nkeys = seen(min(tile * ROWS + ROWS, nrows) - 1);        // of the work-group
+  int nkeys = seen(min(tile * ROWS + ROWS, nrows) - 1);        // of the work-group
+  int key0 = 0;
+  bool whole = true;
+  if constexpr (SPLIT) {  // units of the item
+    const int units = (int)min((int64_t)(p.n - p.unit), end - u);
+    whole = units == p.n;
+    key0 = p.unit * KT;
+    nkeys = min(nkeys, key0 + units * KT);
+    u += units;
+  }
   const bool active = wrow < nrows;  // wave-uniform; idle waves copy and meet the others
-  const int wkeys = active ? seen(min(wrow + 32, nrows) - 1) : 0;    // of the wave
+  const int wkeys = active ? min(nkeys, seen(min(wrow + 32, nrows) - 1)) : 0;    // of the wave
   const int common = active ? seen(wrow) : 0;                        // of all its rows
   int lim[2];
   bf16x8_t qf[2][4];
-  bf16_t* op[2];
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const int row = min(wrow + 16 * g + lr, nrows - 1), qi = row / P.group, h = kh * P.group + row - qi * P.group;
@@ -559,7 +655,6 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
     const bf16_t* qp = P.q + (int64_t)(s_.q0 + qi) * P.ldq + (int64_t)h * D + 8 * lq;
 #pragma unroll
     for (int s = 0; s < 4; ++s) qf[g][s] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 32 * s));
-    op[g] = wrow + 16 * g + lr < nrows ? P.o + (int64_t)(s_.q0 + qi) * P.ldo + (int64_t)h * D + 4 * lq : nullptr;
   }
   const bf16_t* kbase = P.k + (int64_t)s_.k0 * P.ldk + (int64_t)kh * D;
   const bf16_t* vbase = P.v + (int64_t)s_.k0 * P.ldv + (int64_t)kh * D;
@@ -584,11 +679,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) copy16_unseen(vbase + row * P.ldv, vn, d + TILE + c * 1024, vo[c]);
   };
-  // (queries waited for later would wait for the copies, too)
-#pragma unroll
-  for (int g = 0; g < 2; ++g)
-#pragma unroll
-    for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(qf[g][s]));
+  issue(key0, 0);
   int koff[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) koff[s] = k_off(lr, 4 * s + lq);
@@ -597,15 +688,25 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
   // chunk 2 dt + (j >> 1) enters the swizzled address by XOR.
   const int voff = k_off(4 * lq + (lr >> 2), (lr & 3) >> 1) + 8 * (lr & 1);
   f32x4_t acc[8][2];
+  float m[2], l[2];
+  const bf16x2_t ones = {(__bf16)1.f, (__bf16)1.f};
+  // 0 times a value that is not finite reaches the rows of a tile that do not see its key.  Rather
+  // than look for such values in every masked tile, the work-group looks at its sums, and
+  // where one is not finite it goes through its keys again, carefully.
+  bool careful = false;
+  while (true) {
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) acc[dt][0] = acc[dt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m[2], l[2] = {0.f, 0.f};
+  l[0] = l[1] = 0.f;
   m[0] = m[1] = BOUNDED ? BOUNDED_SHIFT_LOG2 : -INFINITY;
-  const bf16x2_t ones = {(__bf16)1.f, (__bf16)1.f};
-
-  issue(0, 0);
+  // the first tile lands with the queries (waited for later, they would wait for later copies)
+  __builtin_amdgcn_s_waitcnt(0);
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(qf[g][s]));
   int at = 0;
-  for (int key = 0; key < nkeys; key += KT) {
+  for (int key = key0; key < nkeys; key += KT) {
     // this tile has landed and everyone is done with the one before it
     __builtin_amdgcn_s_waitcnt(0);
     barrier_no_fence();
@@ -671,14 +772,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
         }
       }
       auto v_frag = [&](int dt, int ks) { return vt_frag(sk + TILE + (voff ^ (dt << 5)) + ks * 32 * 256); };
-      // 0 times a value that is not finite would reach the rows that do not see its key
-      bool spoilt = false;
-      if (masked) {
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) spoilt |= not_finite(v_frag(dt, 0)) || not_finite(v_frag(dt, 1));
-        spoilt = __builtin_amdgcn_ballot_w64(spoilt) != 0;
-      }
-      if (!spoilt) {
+      const bool spoilt = CAUSAL && careful && masked;
+      if (__builtin_expect(!spoilt, 1)) {
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
@@ -688,44 +783,92 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
             for (int g = 0; g < 2; ++g) acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[ks][g], acc[dt][g], 0, 0, 0);
           }
       } else {
-        // key by key: a lane keeps the product only if its row sees the key
-#pragma unroll 1
-        for (int j = 0; j < KT; ++j) {
-          const bool second = j & 32, mine = ((j >> 2) & 3) == lq;
-          const int e0 = 4 * ((j >> 4) & 1) + (j & 3);
-          bf16x8_t pj[2];
+        // finite values as ever; of the others the rows that see their keys are told by a product
+        // of flags: +inf counts 1, -inf 128 and NaN 16384 (a tile has 64 keys), times whether the row sees the key
+        bf16x8_t sees[2][2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
           for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              pj[g][e] = mine && e == e0 ? (second ? pf[1][g][e] : pf[0][g][e]) : (__bf16)0.f;
+              sees[ks][g][e] = key + 32 * ks + 16 * (e >> 2) + 4 * lq + (e & 3) < lim[g] ? (__bf16)1.f : (__bf16)0.f;
 #pragma unroll
-          for (int dt = 0; dt < 8; ++dt) {
-            bf16x8_t vj = v_frag(dt, second);
+        for (int dt = 0; dt < 8; ++dt) {
+          f32x4_t n[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) vj[e] = mine && e == e0 ? vj[e] : (__bf16)0.f;
+          for (int ks = 0; ks < 2; ++ks) {
+            const u16x8_t bits = __builtin_bit_cast(u16x8_t, v_frag(dt, ks));
+            u16x8_t clean, flag;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool odd = (bits[e] & 0x7f80) == 0x7f80;
+              clean[e] = odd ? 0 : bits[e];
+              flag[e] = !odd ? 0 : bits[e] == 0x7f80 ? 0x3f80 : bits[e] == 0xff80 ? 0x4300 : 0x4680;
+            }
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-              const f32x4_t y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vj, pj[g], acc[dt][g], 0, 0, 0);
-              if (key + j < lim[g]) acc[dt][g] = y;
+              acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, clean), pf[ks][g], acc[dt][g], 0, 0, 0);
+              n[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, flag), sees[ks][g], n[g], 0, 0, 0);
             }
           }
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int c = (int)n[g][r];
+              const float up = c & 127 ? INFINITY : 0.f, down = c & 0x3f80 ? -INFINITY : 0.f;
+              const float nan = c >> 14 ? __uint_as_float(0x7fc00000u) : 0.f;
+              acc[dt][g][r] += (up + down) + nan;
+            }
         }
       }
     }
     at ^= STAGE;
   }
   __builtin_amdgcn_s_waitcnt(0);  // no copy outlives its work-group
+  if (!CAUSAL || careful) break;
+  float zero = 0.f;  // NaN where a sum is not finite
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(acc[dt][g][r], 0.f, zero);
+  bad[wave] = active && __builtin_amdgcn_ballot_w64(zero != 0.f) != 0;
+  lds_barrier();
+  if (!(bad[0] | bad[1] | bad[2] | bad[3])) break;
+  careful = true;
+  issue(key0, 0);  // (every wave is done with the last tile)
+  }
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const float ls = sum_quarters(l[g]);
-    const float inv = ls == 0.f ? 0.f : 1.f / ls;  // no key: zeros
-    if (!op[g]) continue;
+    const int row = wrow + 16 * g + lr;
+    if (row >= nrows) continue;
+    if (!SPLIT || whole) {
+      const int qi = row / P.group, h = kh * P.group + row - qi * P.group;
+      bf16_t* op = P.o + (int64_t)(s_.q0 + qi) * P.ldo + (int64_t)h * D + 4 * lq;
+      const float inv = ls == 0.f ? 0.f : 1.f / ls;  // no key: zeros
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
-      *(uint2*)(op[g] + 16 * dt) = make_uint2(pack_bf16x2(acc[dt][g][0] * inv, acc[dt][g][1] * inv),
-                                              pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
+      for (int dt = 0; dt < 8; ++dt)
+        *(uint2*)(op + 16 * dt) = make_uint2(pack_bf16x2(acc[dt][g][0] * inv, acc[dt][g][1] * inv),
+                                             pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
+    } else {
+      const int in = 32 * wave + 16 * g + lr;
+      float* w = P.ws + (worker + p.item) * part_floats(ROWS);
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(w + in * D + 16 * dt + 4 * lq) = acc[dt][g];
+      if (lq == 0) {
+        w[ROWS * D + in] = ls;
+        w[ROWS * D + ROWS + in] = m[g];
+      }
+    }
   }
+  if constexpr (SPLIT) {
+    if (u < end) lds_barrier();  // everyone is done with the last tile: its place takes the next item's
+  }
+  } while (SPLIT && u < end);
 #endif
 }
 
@@ -742,11 +885,24 @@ int64_t tiles_of(const dit_packed_shape& s, int r) {
 }
 // Waves of 256 CUs (by the shape alone: the workspace's size does not depend on the device).
 constexpr int FEW_WORKERS = 1024, FEW_LEAST = 4;
+// Whether the tiles are fewer than the places for work-groups of 256 CUs (two each) and sharing their
+// keys out is worth the joining: in us, whole tiles take 1.6 for 64 keys (2.1 beside
+// another work-group), shared ones 2.1 times their share of all, and 20 for parts and joining (fitted).  By the average
+// length, which is all that the host knows.  Measured, shared and whole:
+//   heads / key heads, queries x keys   32/8 256 x 16384 101 386   16/16 77 x 4096 23 92   32/8 8 of 64 x 4096 42 101
+//   8/8 2048 x 2048 causal 41 53   12/12 1000 x 1500 34 40   28/4 2048 x 2048 causal 93 63   28/4 512 x 512 causal 24 19
+constexpr int SPLIT_WORKERS = 512, SPLIT_LEAST = 8;
+bool split_tiles(const dit_packed_shape& s) {
+  const int64_t items = tiles_of(s, ROWS) * s.kv_heads;
+  const double units = (double)s.Tk / s.batch / KT;
+  return items < SPLIT_WORKERS && 20 + 2.1 * units * items / SPLIT_WORKERS < units * (items > SPLIT_WORKERS / 2 ? 2.1 : 1.6);
+}
 
 size_t attention_packed_ws_bytes(const dit_packed_shape& s) {
   if (s.batch == 0 || s.Tq == 0) return 0;
   const int few = few_rows(s);
   if (few) return (FEW_WORKERS + tiles_of(s, few) * s.kv_heads) * part_floats(few) * sizeof(float);
+  if (split_tiles(s)) return (SPLIT_WORKERS + tiles_of(s, ROWS) * s.kv_heads) * part_floats(ROWS) * sizeof(float);
   return 0;
 }
 
@@ -772,11 +928,25 @@ hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int
     fn = few == 16 ? DIT_PICK(attn_packed_few_kernel, DIT_COMMA 1) : DIT_PICK(attn_packed_few_kernel, DIT_COMMA 2);
     hipLaunchKernelGGL(fn, dim3(FEW_WORKERS / 4), dim3(256), 0, st, P);
     const uint32_t items = (uint32_t)(tiles_of(s, few) * s.kv_heads);
-    if (few == 16) hipLaunchKernelGGL((packed_join_kernel<16, 32, 4>), dim3(items, 8), dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((packed_join_kernel<32, 32, 4>), dim3(items, 16), dim3(256), 0, st, P);
+    // (few items: more work-groups for each, since they have many parts)
+    const int rows = items <= 256 ? 2 : few / 4;
+    if (few == 16) hipLaunchKernelGGL((packed_join_kernel<16, 32, 4>), dim3(items, few / rows), dim3(256), 0, st, P, rows);
+    else hipLaunchKernelGGL((packed_join_kernel<32, 32, 4>), dim3(items, few / rows), dim3(256), 0, st, P, rows);
     return hipGetLastError();
   }
-  fn = DIT_PICK(attn_packed_kernel);
+  if (split_tiles(s)) {
+    P.workers = SPLIT_WORKERS;
+    P.least = SPLIT_LEAST;
+    fn = DIT_PICK(attn_packed_kernel, DIT_COMMA true);
+    hipLaunchKernelGGL(fn, dim3(SPLIT_WORKERS), dim3(256), 0, st, P);
+    const uint32_t items = (uint32_t)(tiles_of(s, ROWS) * s.kv_heads);
+    const int rows = items <= 128 ? 8 : 32;
+    if (items <= 64) hipLaunchKernelGGL((packed_join_kernel<ROWS, KT, 4>), dim3(items, ROWS / 2), dim3(256), 0, st, P, 2);
+    else hipLaunchKernelGGL((packed_join_kernel<ROWS, KT, 1>), dim3(items, ROWS / rows), dim3(256), 0, st, P, rows);
+    return hipGetLastError();
+  }
+  P.ranked = s.batch > 1 && s.batch <= 64 && tiles_of(s, ROWS) * s.kv_heads > SPLIT_WORKERS;
+  fn = DIT_PICK(attn_packed_kernel, DIT_COMMA false);
   hipLaunchKernelGGL(fn, dim3((uint32_t)(tiles_of(s, ROWS) * s.kv_heads)), dim3(256), 0, st, P);
   return hipGetLastError();
 }
