@@ -14,18 +14,15 @@ def quantise(x):
     blk = x.reshape(M, K // 32, 32)
     a = np.abs(blk).max(2)
     fin = np.isfinite(a)
-    e = np.full(a.shape, -127)
-    for i in zip(*np.nonzero(fin & (a > 0))):
-        k = int(np.floor(np.log2(a[i]))) - 4
-        while a[i] > 6 * 2.0 ** k:
-            k += 1
-        e[i] = max(k, -127)
+    # a = m 2^k with m in [1/2, 1), and 6 = 3/4 * 2^3
+    m, k = np.frexp(np.where(fin, a, 0))
+    e = np.maximum(np.where(m > 0, k - 3 + (m > 0.75), -127), -127)
+    top = np.where(fin, a, 0)
+    assert (top <= 6 * 2.0 ** e).all() and ((top > 6 * 2.0 ** (e - 1.0)) | (e == -127)).all()
     y = np.abs(np.where(fin[..., None], blk, 0)) / (2.0 ** e)[..., None]
-    off = np.abs(y[..., None] - E2M1)
-    best = off.min(-1, keepdims=True)
-    near = off == best                       # one code, or two beside each other
-    first = near.argmax(-1)
-    code = np.where(near.sum(-1) == 2, first + first % 2, first)
+    middle = (E2M1[:-1] + E2M1[1:]) / 2
+    below, above = np.searchsorted(middle, y, "left"), np.searchsorted(middle, y, "right")   # one code, or two at a tie
+    code = np.where(below % 2 == 0, below, above)
     code = np.where(np.signbit(blk), code | 8, code)
     return np.where(fin[..., None], code, 0).reshape(M, K).astype(np.uint8), np.where(fin, e + 127, 255).astype(np.uint8)
 

@@ -647,3 +647,220 @@ def test_packed_attention_is_the_dense_one():
     torch.cuda.synchronize()
     y, d = ref.attend(*(bits_to_f64(t) for t in (qb, kb, vb)), qoff=[0, 500], koff=[0, 500], heads=3)
     assert (np.abs(host_bf16(o) - host_bf16(p)) <= 2 * (d + BF16 * (np.abs(y) + d))).all()
+
+
+# ---------------------------------------------------------------- together
+
+class Layer:
+    """One layer of a prompt encoder over packed prompts: 4-bit products, rotary positions, causal attention with
+    grouped heads, an MLP whose middle stays in 4 bits; its buffers and workspaces."""
+
+    def __init__(self, torch, seed, lengths=(70, 1, 200, 33), heads=4, kv_heads=2, F=512):
+        r = rng(seed, 21)
+        self.t, self.lengths, self.heads, self.G, self.F = torch, lengths, heads, kv_heads, F
+        H = self.H = heads * 128
+        L = self.L = sum(lengths)
+        self.N = H + 2 * kv_heads * 128
+        self.w = {name: self.rows(r.standard_normal((n, k)) / np.sqrt(k))
+                  for name, n, k in (("qkv", self.N, H), ("o", H, H), ("up", F, H), ("down", H, F))}
+        self.gate = dev(torch, r.standard_normal(H).astype(np.float32))
+        self.x0 = dev(torch, bf16_bits(r.standard_normal((L, H))))
+        self.off = dev(torch, offsets(lengths))
+        self.pos = dev(torch, np.concatenate([np.arange(n) for n in lengths]).astype(np.int32))
+        freq, self.scale = binding.rotary_freqs(64, method=binding.ROTARY_PARTS, factor=4.0, context=64.0)
+        self.freq = dev(torch, freq)
+        e = lambda *s, dt=torch.int16: torch.empty(*s, dtype=dt, device="cuda")  # noqa: E731
+        self.x, self.qkv, self.raw, self.att = e(L, H), e(L, self.N), e(L, self.N), e(L, H)
+        self.q4 = [e(L, n // 2, dt=torch.uint8) for n in (H, H, H, F)]
+        self.s4 = [e(L, binding.fp4_scale_ld(n), dt=torch.uint8) for n in (H, H, H, F)]
+        self.ws = e(max(16, binding.attention_packed_ws_bytes(batch=len(lengths), Tq=L, Tk=L, heads=heads, kv_heads=kv_heads)),
+                    dt=torch.uint8)
+
+    def rows(self, x):
+        c, s = ref.quantise(x)
+        return dev(self.t, ref.pack(c)), dev(self.t, padded_scale(s, x.shape[1])), ref.values(c, s)
+
+    def linear(self, i, name, out, N, K, **kw):
+        w = self.w[name]
+        binding.gemm_fp4(self.q4[i], self.s4[i], w[0], w[1], None, out, M=self.L, N=N, K=K, stream=self.stream, **kw)
+
+    def quant(self, i, x, K):
+        binding.quant_fp4(x, self.q4[i], self.s4[i], M=self.L, K=K, stream=self.stream)
+
+    def run(self, stream=None):
+        self.stream, H, F, L, G = stream, self.H, self.F, self.L, self.G
+        self.x.copy_(self.x0)
+        self.quant(0, self.x, H)
+        turned = (self.heads + G) * 128
+        self.linear(0, "qkv", self.raw, self.N, H, rms_cols=turned)
+        self.qkv.copy_(self.raw)
+        both = self.qkv[:, :turned]
+        binding.rotary(both, both, pos=self.pos, freq=self.freq, scale=self.scale, rows=L, heads=self.heads + G, stream=stream)
+        q, k, v = self.qkv[:, :H], self.qkv[:, H:turned], self.qkv[:, turned:]
+        binding.attention_packed_bf16(q, k, v, self.att, qoff=self.off, koff=self.off, heads=self.heads, kv_heads=G,
+                                      flags=binding.ATTN_CAUSAL, ws=self.ws, stream=stream)
+        self.quant(1, self.att, H)
+        self.linear(1, "o", self.x, H, H, flags=binding.EPI_GATED_RES, gate=self.gate)
+        self.quant(2, self.x, H)
+        self.linear(2, "up", self.q4[3], F, H, flags=binding.EPI_FP4, c_scale=self.s4[3], gelu_from=0)
+        self.linear(3, "down", self.x, H, F, flags=binding.EPI_GATED_RES, gate=self.gate)
+        return self.x
+
+    def host4(self, i):
+        q, s = self.q4[i].cpu().numpy(), self.s4[i].cpu().numpy()
+        return ref.values(ref.unpack(q), s[:, :q.shape[1] // 16])
+
+    def step4(self, i, y, d):
+        """Half the distance between the codes around y +- d."""
+        q, s = self.q4[i], self.s4[i].cpu().numpy()
+        s = np.repeat(2.0 ** (s[:, :q.shape[1] // 16].astype(np.float64) - 127), 32, 1)
+        z = (np.abs(y) + d) / s
+        return np.where(z <= 2, 0.25, np.where(z <= 4, 0.5, 1.0)) * s
+
+
+def test_a_layer_of_a_prompt_encoder():
+    """Each stage against float64 on the device's own input of that stage, so that every tolerance is one stage's."""
+    torch = torch_cuda()
+    b = Layer(torch, 1)
+    H, L, G, turned = b.H, b.L, b.G, (b.heads + b.G) * 128
+    out = host_bf16(b.run())
+    x0 = host_bf16(b.x0)
+    np.testing.assert_array_equal(b.host4(0), ref.values(*ref.quantise(x0)))
+    y, d = ref8.product(b.host4(0), b.w["qkv"][2], None, f32=True, rms_cols=turned)
+    raw = host_bf16(b.raw)
+    assert (np.abs(raw - y) <= d + BF16 * (np.abs(y) + d) + 1e-30).all()
+    qkv = host_bf16(b.qkv)
+    y, d = ref.rotate(raw[:, :turned], b.pos.cpu().numpy()[None], b.freq.cpu().numpy(), heads=b.heads + G, head_dim=128,
+                      pairs=[64], half=True, scale=b.scale)
+    assert (np.abs(qkv[:, :turned] - y) <= d + BF16 * (np.abs(y) + d)).all()
+    assert (qkv[:, turned:] == raw[:, turned:]).all()
+    off = b.off.cpu().numpy()
+    y, d = ref.attend(qkv[:, :H], qkv[:, H:turned], qkv[:, turned:], qoff=off, koff=off, heads=b.heads, kv_heads=G, causal=True)
+    assert (np.abs(host_bf16(b.att) - y) <= d + BF16 * (np.abs(y) + d)).all()
+    np.testing.assert_array_equal(b.host4(1), ref.values(*ref.quantise(host_bf16(b.att))))
+    gate = b.gate.cpu().numpy().astype(np.float64)
+    y, d = ref8.product(b.host4(1), b.w["o"][2], None, f32=True)
+    mid, dm = x0 + gate * y, np.abs(gate) * d + 2.0 ** -22 * (np.abs(x0) + np.abs(gate * y))
+    dm = dm + BF16 * (np.abs(mid) + dm)
+    m4 = b.host4(2)
+    assert (np.abs(m4 - mid) <= dm + b.step4(2, mid, dm)).all()
+    y, d = ref8.product(m4, b.w["up"][2], None, f32=True, gelu_from=0)
+    u4 = b.host4(3)
+    assert (np.abs(u4 - y) <= d + b.step4(3, y, d)).all()
+    y, d = ref8.product(u4, b.w["down"][2], None, f32=True)
+    fin = mid + gate * y
+    tol = dm + np.abs(gate) * d + 2.0 ** -22 * (np.abs(mid) + np.abs(gate * y))
+    assert (np.abs(out - fin) <= tol + BF16 * (np.abs(fin) + tol)).all()
+
+
+def test_tokens_one_by_one_are_the_prompt_at_once():
+    """Keys and values appended to a cache, each token's query alone: the rows of the whole prompt, up to both calls'
+    roundings."""
+    torch = torch_cuda()
+    r = rng(50)
+    heads, G, n, slots = 6, 2, 150, 160
+    qb, kb, vb = (bf16_bits(r.standard_normal((2 * n, h * 128))) for h in (heads, G, G))
+    q, k, v = (dev(torch, t) for t in (qb, kb, vb))
+    off = dev(torch, np.array([0, n, 2 * n], np.int32))
+    whole = torch.empty_like(q)
+    shape = dict(heads=heads, kv_heads=G, flags=binding.ATTN_CAUSAL)
+    binding.attention_packed_bf16(q, k, v, whole, qoff=off, koff=off, **shape)
+    ck, cv = (torch.full((2 * slots, G * 128), 0x7FC0, dtype=torch.int16, device="cuda") for _ in range(2))
+    one = torch.empty_like(q)
+    qoff, koff = (dev(torch, np.array(t, np.int32)) for t in ([0, 1, 2], [0, slots, 2 * slots]))
+    for i in range(n):
+        rows = [i, n + i]
+        ck[[i, slots + i]], cv[[i, slots + i]] = k[rows], v[rows]
+        o = torch.empty(2, heads * 128, dtype=torch.int16, device="cuda")
+        binding.attention_packed_bf16(q[rows].contiguous(), ck, cv, o, qoff=qoff, koff=koff,
+                                      klen=torch.full((2,), i + 1, dtype=torch.int32, device="cuda"), **shape)
+        one[rows] = o
+    y, d = ref.attend(*(bits_to_f64(t) for t in (qb, kb, vb)), qoff=[0, n, 2 * n], koff=[0, n, 2 * n], heads=heads,
+                      kv_heads=G, causal=True)
+    for got in (whole, one):
+        assert (np.abs(host_bf16(got) - y) <= d + BF16 * (np.abs(y) + d)).all()
+
+
+# lengths whose attention shares its keys out, has few rows a sequence, or goes whole tiles
+LAYERS = [(70, 1, 200, 33), (1, 2, 1, 3, 1, 1), (2100,)]
+
+
+def test_layers_captured_into_graphs():
+    """Layers captured into graphs with their own workspaces, replayed in turn with eager work between: every
+    replay gives the eager bits."""
+    torch = torch_cuda()
+    layers = [Layer(torch, s, lengths=n) for s, n in enumerate(LAYERS, 2)]
+    want = [b.run().clone() for b in layers]
+    other = Layer(torch, 9)
+    stream = torch.cuda.Stream()
+    graphs = []
+    torch.cuda.synchronize()
+    for b in layers:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            b.run(stream)
+        graphs.append(g)
+    for i in range(4):
+        for b, g, w in zip(layers, graphs, want):
+            b.x.zero_()
+            b.ws.fill_(0xFF)
+            g.replay()
+            other.run()
+            torch.cuda.synchronize()
+            assert torch.equal(b.x, w), i
+
+
+def test_layers_on_two_streams():
+    torch = torch_cuda()
+    layers = [Layer(torch, s, lengths=n) for s, n in ((5, (400, 900)), (6, (1, 1, 5)))]
+    want = [b.run().clone() for b in layers]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    for b, s in zip(layers, streams):
+        for _ in range(6):
+            with torch.cuda.stream(s):
+                b.run(s)
+    torch.cuda.synchronize()
+    for b, w in zip(layers, want):
+        assert torch.equal(b.x, w)
+
+
+@pytest.mark.parametrize("ql,kl,heads,kv_heads", [([1, 1, 3], [5000, 20, 900], 4, 1), ([300], [9000], 4, 2), ([20, 9], [700, 650], 8, 8),
+                                                 ([1] * 200, [17] * 200, 4, 4)])
+@pytest.mark.parametrize("bounded", [False, True])
+def test_packed_attention_in_a_workspace_of_its_size(ql, kl, heads, kv_heads, bounded):
+    """A workspace between guards: nothing before or behind it changes, and what it held does not matter."""
+    torch = torch_cuda()
+    r = rng(60, len(ql))
+    q, k, v = (dev(torch, bf16_bits(r.standard_normal((n, h * 128)) / 4)) for n, h in ((sum(ql), heads), (sum(kl), kv_heads),
+                                                                                     (sum(kl), kv_heads)))
+    nbytes = binding.attention_packed_ws_bytes(batch=len(ql), Tq=sum(ql), Tk=sum(kl), heads=heads, kv_heads=kv_heads)
+    assert nbytes > 0
+    res = []
+    for fill in (0x00, 0xFF, 0x7F):
+        buf = torch.full((nbytes + 512,), fill, dtype=torch.uint8, device="cuda")
+        o = torch.zeros_like(q)
+        binding.attention_packed_bf16(q, k, v, o, qoff=dev(torch, offsets(ql)), koff=dev(torch, offsets(kl)), heads=heads,
+                                      kv_heads=kv_heads, ws=buf[256:256 + nbytes],
+                                      flags=binding.ATTN_CAUSAL | (binding.ATTN_BOUNDED_LOGITS if bounded else 0))
+        assert bool((buf[:256] == fill).all()) and bool((buf[256 + nbytes:] == fill).all())
+        res.append(o)
+    assert torch.equal(res[0], res[1]) and torch.equal(res[0], res[2])
+
+
+def test_calls_lie_on_the_stream_they_are_given():
+    """Calls behind others on a stream see their results."""
+    torch = torch_cuda()
+    s = torch.cuda.Stream()
+    x = torch.zeros(4096, 4096, device="cuda")
+    q = torch.empty(4096, 2048, dtype=torch.uint8, device="cuda")
+    sc = torch.empty(4096, 128, dtype=torch.uint8, device="cuda")
+    y = torch.empty_like(x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            x.add_(1.0)
+    binding.quant_fp4(x, q, sc, M=4096, K=4096, stream=s)
+    binding.dequant_fp4(q, sc, y, M=4096, K=4096, stream=s)
+    s.synchronize()
+    assert bool((y == 16.0).all())          # 20 = 5 * 4: a tie, to the even code
