@@ -321,6 +321,91 @@ struct Epi : EpiLdsT<KIND == EPI_K_FP4 ? EPI_K_ANY : KIND, Fp4Prob> {
   }
 };
 
+// 4-bit rows straight from the accumulators of 32 x 32 blocks whose operands changed places:
+// lane (lr, lh) holds row 32 i + lr's columns 8 q + 4 lh .. + 3 of block j, so that a
+// lane and its other half hold a row's 32 TN columns.
+template <int TM, int TN>
+__device__ __forceinline__ void store_fp4(const Fp4Prob& P, f32x16_t (&acc)[TM][TN], int m0, int n0, int lr, int lh) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  static_assert(TN == 4, "a head's 128 columns, a dword of scales");
+  auto other_half = [](uint32_t v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (threadIdx.x & 32) ? s[0] : s[1];
+  };
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int n = n0 + 32 * j + 8 * (r >> 2) + 4 * lh + (r & 3);
+      const float b = P.bias && n0 + 32 * j < P.N ? bf16_to_f32(P.bias[n]) : 0.f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) acc[i][j][r] += b;
+    }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + 32 * i + lr;
+    if (n0 < P.rms_cols) {
+      float ss = 0.f;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ss += acc[i][j][r] * acc[i][j][r];
+      ss += __uint_as_float(other_half(__float_as_uint(ss)));
+      const float f = rsqrtf(ss * (1.f / 128.f) + DIT_RMS_EPS);
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] *= f;
+    }
+    if (n0 >= P.gelu_from) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = gelu_tanh_f(acc[i][j][r]);
+    }
+    if (P.flags & DIT_EPI_SILU) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = silu_f(acc[i][j][r]);
+    }
+    uint32_t scales = 0;
+    uint8_t* c = (uint8_t*)P.C + (int64_t)m * P.ldc + (n0 >> 1) + 8 * lh;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = max(top, __float_as_uint(acc[i][j][r]) & 0x7fffffffu);
+      const uint32_t byte = scale4_of(max(top, other_half(top)));
+      const float inv = e8m0_inverse(byte);
+      scales |= byte << (8 * j);
+      uint32_t w[2];  // 16 bits for q = 0, 1 and for 2, 3
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = acc[i][j][8 * h + e] * inv;
+        w[h] = pack_fp4x8(v);
+      }
+      // the lower half takes both halves' first two, the upper one the last two
+      const auto s = __builtin_amdgcn_permlane32_swap(w[0], w[1], false, false);
+      if (m < P.M && n0 + 32 * j < P.N)
+        *(uint2*)(c + 16 * j) = make_uint2((s[0] & 0xffffu) | s[1] << 16, s[0] >> 16 | (s[1] & 0xffff0000u));
+    }
+    if (m < P.M && lh == 0) {
+      uint8_t* cs = P.Cs + (int64_t)m * P.ldcs + (n0 >> 5);
+      if (n0 + 128 <= P.N) {
+        *(uint32_t*)cs = scales;
+      } else {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          if (n0 + 32 * j < P.N) cs[j] = (uint8_t)(scales >> (8 * j));
+      }
+    }
+  }
+#endif
+}
+
 // 256 x 256 tiles, 8 waves of 64 x 128.  LDS: two slices of 256 of K each of W and A
 // (32 KB, 16-byte chunks of a 128-byte row XOR-swizzled by ((row >> 1) & 7)) and two groups of
 // both's scales.  32x32x64 MFMAs: a slice is four substeps of eight, and a
@@ -412,7 +497,8 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
 #pragma unroll
     for (int q = 0; q < TM * TN; ++q) {
       const int i = q & 1, j = q >> 1;
-      acc[i][j] = mfma_fp4_32<B>(a[i], w[j], acc[i][j], x.a[i], x.w[j]);
+      if constexpr (KIND == EPI_K_FP4) acc[i][j] = mfma_fp4_32<B>(w[j], a[i], acc[i][j], x.w[j], x.a[i]);
+      else acc[i][j] = mfma_fp4_32<B>(a[i], w[j], acc[i][j], x.a[i], x.w[j]);
       __builtin_amdgcn_sched_barrier(0);
       if (q == 0 || q == 2) an[q >> 1] = lds_chunk(smem + ua + wa + (q >> 1) * 4096 + loff[s]);
       else if (q < 6) wn2[q == 1 ? 0 : q - 2] = lds_chunk(smem + uw + ww + (q == 1 ? 0 : q - 2) * 4096 + loff[s]);
@@ -484,6 +570,10 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   if (kt + 2 < nk) slice(kt + 2, integral_constant<int, 2>{});
   __builtin_amdgcn_s_waitcnt(0);  // the copies past the end have landed
   __syncthreads();
+  if constexpr (KIND == EPI_K_FP4) {
+    store_fp4<TM, TN>(P, acc, m0 + 64 * wm, n0 + 128 * wn, lr, lh);
+    return;
+  }
   float* slab = (float*)smem + wave * (32 * 128);
   Epi<KIND> epi(P, m0 + 64 * wm, n0 + 128 * wn, lr, lh, slab);
   epi.prep();
@@ -502,15 +592,15 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   }
 }
 
-// BM x 128 tiles, waves of 64 x 64 (BM = 64: 32 x 64), a ring of slices of 256 of K
+// BM x 128 tiles, waves of 64 x 64 (BM = 64: 32 x 64, 192: 48 x 64), a ring of slices of 256 of K
 // in LDS: two work-groups of 64 x 128 (three slices) or 128 x 128 (two) per CU, or
 // one of 256 x 128 (three).  For launches that 256 x 256 tiles would not fill.  The waves
 // meet before every step kt; slice kt + 1 has landed, and slice kt, whose fragments are all in
 // registers, gives its place to slice kt + ST.  The fragments of kt + 1 are read under the MFMAs of kt.
 template <int BM, int KIND>
-__global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel(Fp4Prob P) {
+__global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel(Fp4Prob P) {
   constexpr int ST = BM == 128 ? 2 : 3;
-  constexpr int NW = BM == 256 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
+  constexpr int NW = BM >= 192 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
   constexpr int TM = WM / 16, TN = 4, NF = TM + TN;
   constexpr int SLICE = (BM + 128) * 128, RING = ST * SLICE, GROUP = (BM + 128) * 16;
   constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW, INS = A_INS + W_INS;
@@ -635,7 +725,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel
   __syncthreads();
   // The tile in LDS as slabs of ROWS rows x 128, one per wave, columns XOR 16
   // ((row >> 2) & 3): then each wave has whole 128-column rows.
-  constexpr int ROWS = BM / NW;
+  constexpr int ROWS = BM == 192 ? 16 : BM / NW;
   float* tile = (float*)smem;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -645,11 +735,14 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256, 2) void gemm_fp4_tile_kernel
       for (int r = 0; r < 4; ++r)
         tile[(wm * WM + 16 * i + 4 * lq + r) * 128 + ((64 * wn + 16 * j + lr) ^ (lq << 4))] = acc[i][j][r];
   __syncthreads();
-  Epi<KIND> epi(P, m0 + ROWS * wave, n0, lane & 31, lane >> 5, tile + ROWS * wave * 128);
-  epi.prep();
-  uint2 old[8][2];
-  if (epi.gated) epi.load_old(0, old);
-  epi.template rows<3, 4, ROWS>(0, old);
+#pragma unroll 1
+  for (int slab = wave; slab < BM / ROWS; slab += NW) {
+    Epi<KIND> epi(P, m0 + ROWS * slab, n0, lane & 31, lane >> 5, tile + ROWS * slab * 128);
+    epi.prep();
+    uint2 old[8][2];
+    if (epi.gated) epi.load_old(0, old);
+    epi.template rows<3, 4, ROWS>(0, old);
+  }
 }
 
 // Few rows or few tiles: 16 RB x NT outputs per work-group, eight waves of 16 RB x 32
@@ -888,9 +981,10 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
     const int64_t slots = (int64_t)n_cu * c.per_cu;
     return (double)((tiles(c.bm, c.bn) + slots - 1) / slots) * ((g.K + 255) / 256 * c.slice_us + c.us);
   };
-  const Tile cfg[] = {{64, 128, 2, 0.67, 4.8}, {128, 128, 2, 1.31, 6.2}, {256, 128, 1, 1.35, 6.2}, {256, 256, 1, 1.75, 12}};
+  const Tile cfg[] = {{64, 128, 2, 0.67, 4.8}, {128, 128, 2, 1.31, 6.2}, {256, 128, 1, 1.35, 6.2}, {256, 256, 1, 1.75, 12},
+                      {192, 128, 1, 1.05, 6.2}};
   int best = 0;
-  for (int c = 1; c < 4; ++c)
+  for (int c = 1; c < 5; ++c)
     if (cost(cfg[c]) < cost(cfg[best])) best = c;
   if (best == 3)
     return go(fp4 ? gemm_fp4_ring_kernel<EPI_K_FP4> : store ? gemm_fp4_ring_kernel<EPI_K_STORE>
@@ -898,6 +992,7 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
 #define DIT_TILE(BM, THREADS)                                                                                  \
   go(fp4 ? gemm_fp4_tile_kernel<BM, EPI_K_FP4> : store ? gemm_fp4_tile_kernel<BM, EPI_K_STORE>                  \
                                                        : gemm_fp4_tile_kernel<BM, EPI_K_ANY>, BM, 128, THREADS)
+  if (best == 4) return DIT_TILE(192, 512);
   if (best == 2) return DIT_TILE(256, 512);
   if (best == 1) return DIT_TILE(128, 256);
   return DIT_TILE(64, 256);
