@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_tile.h"
 #include "common.h"
@@ -130,6 +131,23 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 #else
   return fmaxf(fmaxf(a, b), c);
+#endif
+}
+
+// Waits until the products in s are written: the compiler knows when its own instructions may
+// read a matrix instruction's result, but not when max3 may.
+template <int N, int NG>
+__device__ __forceinline__ void settle(f32x4_t (&s)[N][NG]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(s[b][g]));
+  asm volatile("s_nop 15" : "+v"(s[N - 1][NG - 1]));
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(s[b][g]));
 #endif
 }
 
@@ -453,6 +471,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
             if (key + 16 * b + 4 * lq + r >= lim[g]) s[b][g][r] = -INFINITY;
     }
     bf16x8_t ph[NG], pl[NG];  // probabilities: bf16 and what it leaves
+    if constexpr (!BOUNDED) settle(s);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if constexpr (!BOUNDED) {
@@ -594,12 +613,12 @@ __device__ __forceinline__ bool ranked_tile(const PackedArgs& P, int t, Seq& seq
 //
 // SPLIT: launches whose tiles are fewer than the chip's places for work-groups share the units
 // of the whole launch out (Line); a work-group may go through parts of several items.
-template <bool BOUNDED, bool CAUSAL, bool SPLIT>
+template <bool BOUNDED, bool CAUSAL, bool SPLIT, bool PIPE>
 __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int TILE = KT * D * 2, STAGE = 2 * TILE;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];  // [stage][K | V]
-  __shared__ int bad[4];
+  constexpr int TILE = KT * D * 2, STAGE = 2 * TILE, VBASE = 3 * TILE;
+  // [stage][K | V], or three tiles of K and two of V
+  __shared__ __attribute__((aligned(1024))) char smem[PIPE ? 5 * TILE : 2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lq = lane >> 4;
@@ -658,15 +677,12 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
   }
   const bf16_t* kbase = P.k + (int64_t)s_.k0 * P.ldk + (int64_t)kh * D;
   const bf16_t* vbase = P.v + (int64_t)s_.k0 * P.ldv + (int64_t)kh * D;
-  // copy c of this wave: rows 4 (4 wave + c) .. + 3 of a tile
-  uint32_t ko[4], vo[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int row = 4 * (4 * wave + c) + (lane >> 4);
-    const uint32_t ch = ((lane & 15) ^ (row & 15)) << 4;
-    ko[c] = (uint32_t)row * (uint32_t)P.ldk * 2u + ch;
-    vo[c] = (uint32_t)row * (uint32_t)P.ldv * 2u + ch;
-  }
+  // copy c of this wave: rows 4 (4 wave + c) .. + 3 of a tile, chunks swizzled by the row's lowest four bits
+  const int crow = 16 * wave + (lane >> 4);
+  const uint32_t kr = (uint32_t)crow * (uint32_t)P.ldk * 2u, vr = (uint32_t)crow * (uint32_t)P.ldv * 2u;
+  const uint32_t chunk = ((lane & 15) ^ (lane >> 4)) << 4;
+  auto ko = [&](int c) { return kr + (uint32_t)(8 * c) * (uint32_t)P.ldk + (chunk ^ (uint32_t)(c << 6)); };
+  auto vo = [&](int c) { return vr + (uint32_t)(8 * c) * (uint32_t)P.ldv + (chunk ^ (uint32_t)(c << 6)); };
   // rows past the last key are zeros
   auto issue = [&](int key, int at) {
     const int n = min(nkeys - key, KT);
@@ -675,14 +691,36 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
     const int64_t row = n <= 0 ? 0 : key;
     char* d = smem + at + wave * 4096;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) copy16_unseen(kbase + row * P.ldk, kn, d + c * 1024, ko[c]);
+    for (int c = 0; c < 4; ++c) copy16_unseen(kbase + row * P.ldk, kn, d + c * 1024, ko(c));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) copy16_unseen(vbase + row * P.ldv, vn, d + TILE + c * 1024, vo[c]);
+    for (int c = 0; c < 4; ++c) copy16_unseen(vbase + row * P.ldv, vn, d + TILE + c * 1024, vo(c));
   };
-  issue(key0, 0);
-  int koff[4];
+  struct Src {
+    const bf16_t* p;
+    uint32_t bytes;
+  };
+  auto src = [&](const bf16_t* base, int64_t ld, int key) {
+    const int n = min(nkeys - key, KT);
+    return Src{base + (n <= 0 ? 0 : key) * ld, n <= 0 ? 0u : (uint32_t)(n - 1) * (uint32_t)ld * 2u + 2u * D};
+  };
+  auto copy = [&](const Src& x, int at, uint32_t off, int c) {
+    copy16_unseen(x.p, x.bytes, smem + at + (4 * wave + c) * 1024, off);
+  };
+  const bool piped = PIPE && nkeys - key0 > 2 * KT;
+  if (piped) {
 #pragma unroll
-  for (int s = 0; s < 4; ++s) koff[s] = k_off(lr, 4 * s + lq);
+    for (int u_ = 0; u_ < 3; ++u_) {
+      const Src x = src(kbase, P.ldk, key0 + u_ * KT);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) copy(x, u_ * TILE, ko(c), c);
+    }
+    const Src none{vbase, 0u};  // values of the tile before the first
+#pragma unroll
+    for (int c = 0; c < 4; ++c) copy(none, VBASE + TILE, vo(c), c);
+  } else {
+    issue(key0, 0);
+  }
+  const int koff0 = k_off(lr, lq);  // chunk 4 s + lq of the row: XOR 64 s
   // V^T fragment (d = 16 dt + lr; keys 4 lq .. + 3 of a 16-key block): lane 4 k + j of a
   // quarter addresses row 4 lq + k, columns 16 dt + 4 j, and receives column lr.  The
   // chunk 2 dt + (j >> 1) enters the swizzled address by XOR.
@@ -705,6 +743,144 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
   for (int g = 0; g < 2; ++g)
 #pragma unroll
     for (int s = 0; s < 4; ++s) asm volatile("" : "+v"(qf[g][s]));
+  bool done = false;
+  if constexpr (PIPE) if (piped && !careful) {
+    done = true;
+    barrier_no_fence();  // the first three tiles of K have landed
+    // Iteration t issues the score product of tile t + 1 and the PV product of tile t - 1
+    // on MFMA with the softmax of tile t, which depends on neither, between them in 32 fenced slots of
+    // two MFMAs, a fragment read AHEAD slots before its use and a share of the softmax.  Its copies
+    // are V of tile t and K of tile t + 3.  Tiles come in pairs; a last one without keys adds nothing.
+    // A tile's fragments in the order of their use, K 0..15 and V^T 0..15, so that four
+    // independent accumulators stand between the steps of a dependent chain.
+    auto k_kb = [](int i) { return 2 * (i >> 3) + (i & 1); };
+    auto k_s = [](int i) { return (i >> 1) & 3; };
+    auto v_dt = [](int i) { return 2 * (i >> 2) + (i & 1); };
+    auto v_ks = [](int i) { return (i >> 1) & 1; };
+    auto k_frag = [&](int at, int i) {
+      return __builtin_bit_cast(bf16x8_t, *(const uint4*)(smem + at + (koff0 ^ (k_s(i) << 6)) + k_kb(i) * 16 * 256));
+    };
+    auto v_frag = [&](int at, int i) { return vt_frag(smem + (voff ^ (v_dt(i) << 5)) + at + v_ks(i) * 32 * 256); };
+    f32x4_t sb[2][4][2];
+    bf16x8_t pb[2][2][2];
+    auto score_step = [&](int i, const bf16x8_t& kf, f32x4_t (&s)[4][2]) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        f32x4_t& c = s[k_kb(i)][g];
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][k_s(i)], k_s(i) ? c : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+    };
+    auto pv_step = [&](int i, const bf16x8_t& vf, const bf16x8_t (&pf)[2][2]) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        acc[v_dt(i)][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[v_ks(i)][g], acc[v_dt(i)][g], 0, 0, 0);
+    };
+    // Step i of 16 of a tile's softmax: two probabilities of a query group.
+    struct Soft {
+      float sum[2];
+      uint32_t w[4];
+    };
+    auto exp_step = [&](int i, const f32x4_t (&s)[4][2], bf16x8_t (&pf)[2][2], Soft& x) {
+      const int g = i >> 3, ks = (i >> 2) & 1, e = i & 3;
+      const f32x4_t& c = s[2 * ks + (e >> 1)][g];
+      x.w[e] = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(c[2 * (e & 1)], P.scale_log2, -m[g])),
+                           __builtin_amdgcn_exp2f(__builtin_fmaf(c[2 * (e & 1) + 1], P.scale_log2, -m[g])));
+      // formed here: the branches between iterations would otherwise draw the softmax
+      // past the barrier, away from the MFMAs
+      asm volatile("" : "+v"(x.w[e]));
+      x.sum[g] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.w[e]), ones, (i & 7) ? x.sum[g] : 0.f, false);
+      if (e == 3) pf[ks][g] = __builtin_bit_cast(bf16x8_t, make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]));
+    };
+    auto mask = [&](int key, f32x4_t (&s)[4][2]) {
+#pragma unroll
+      for (int b_ = 0; b_ < 4; ++b_)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+            if (key + 16 * b_ + 4 * lq + r >= min(lim[g], nkeys)) s[b_][g][r] = -INFINITY;
+    };
+    const int clear = min(common, nkeys);  // keys that every row of the wave sees
+    // places of K of tiles t, t + 1, t + 2
+    int ks0 = 0, ks1 = TILE, ks2 = 2 * TILE;
+    // End of an iteration: its copies have landed and the waves meet.  Fragments still
+    // on their way are of K of tile t + 2, which stays for another iteration.
+    auto meet = [&]() {
+      wait_vmcnt<0>();
+      barrier_no_fence();
+      const int k = ks0;
+      ks0 = ks1; ks1 = ks2; ks2 = k;
+    };
+    constexpr int AHEAD = 4;
+    bf16x8_t fr[AHEAD];
+    auto iter = [&](int key, auto par) {
+      constexpr int B = decltype(par)::value;
+      const Src vs = src(vbase, P.ldv, key), kn = src(kbase, P.ldk, key + 3 * KT);
+      if (key + KT > clear) mask(key, sb[B]);
+      Soft x;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i_ = 0; i_ < 32; ++i_) {
+        if (i_ < 16) score_step(i_, fr[i_ % AHEAD], sb[B ^ 1]);
+        else pv_step(i_ - 16, fr[i_ % AHEAD], pb[B ^ 1]);
+        const int n = i_ + AHEAD;
+        fr[i_ % AHEAD] = n < 16 ? k_frag(ks1, n) : n < 32 ? v_frag(VBASE + (B ^ 1) * TILE, n - 16) : k_frag(ks2, n - 32);
+        if (i_ % 2 == 0 && i_ < 16) {
+          if (i_ < 8) copy(vs, VBASE + B * TILE, vo(i_ / 2), i_ / 2);
+          else copy(kn, ks0, ko(i_ / 2 - 4), i_ / 2 - 4);
+        }
+        if (i_ & 1) exp_step(i_ >> 1, sb[B], pb[B], x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int g = 0; g < 2; ++g) l[g] += x.sum[g];
+      meet();
+    };
+    if (active) {
+#pragma unroll
+      for (int i_ = 0; i_ < 16; ++i_) score_step(i_, k_frag(0, i_), sb[0]);
+#pragma unroll
+      for (int f = 0; f < AHEAD; ++f) fr[f] = k_frag(ks1, f);
+      pb[1][0][0] = pb[1][0][1] = pb[1][1][0] = pb[1][1][1] = __builtin_bit_cast(bf16x8_t, make_uint4(0, 0, 0, 0));
+      if constexpr (!BOUNDED) {
+        // The shift is the first tile's maximum.  Later logits may be larger: probabilities
+        // and sums are floating point numbers and lose nothing up to 2^100, where the
+        // work-group goes through its keys again.  (Of no key: finite, so that -inf logits stay zeros.)
+        if (key0 + KT > clear) mask(key0, sb[0]);
+        settle(sb[0]);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          float mx = sb[0][0][g][0];
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) mx = max3(mx, sb[0][kb][g][r], sb[0][kb][g][r + 1]);
+          m[g] = fmaxf(max_quarters(mx) * P.scale_log2, -1e30f);
+        }
+      }
+      wait_vmcnt_lgkm0<0>();
+      barrier_no_fence();  // K of tile 0 is read: its place is free
+#pragma unroll 1
+      for (int key = key0; key < nkeys; key += 2 * KT) {
+        iter(key, std::integral_constant<int, 0>{});
+        iter(key + KT, std::integral_constant<int, 1>{});
+      }
+#pragma unroll
+      for (int i_ = 0; i_ < 16; ++i_) pv_step(i_, v_frag(VBASE + TILE, i_), pb[1]);
+    } else {
+      barrier_no_fence();
+      for (int key = key0; key < nkeys; key += 2 * KT)
+        for (int par = 0; par < 2; ++par) {
+          const Src vs = src(vbase, P.ldv, key + par * KT), kn = src(kbase, P.ldk, key + par * KT + 3 * KT);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) copy(vs, VBASE + par * TILE, vo(c), c);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) copy(kn, ks0, ko(c), c);
+          meet();
+        }
+    }
+  }
+  if (!PIPE || !done) {
   int at = 0;
   for (int key = key0; key < nkeys; key += KT) {
     // this tile has landed and everyone is done with the one before it
@@ -719,7 +895,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
         s[kb][0] = s[kb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t4 = 0; t4 < 4; ++t4) {
-          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t4] + kb * 16 * 256));
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + (koff0 ^ (t4 << 6)) + kb * 16 * 256));
 #pragma unroll
           for (int g = 0; g < 2; ++g) s[kb][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t4], s[kb][g], 0, 0, 0);
         }
@@ -735,6 +911,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
               if (key + 16 * kb + 4 * lq + r >= lim[g]) s[kb][g][r] = -INFINITY;
       }
       bf16x8_t pf[2][2];
+      if constexpr (!BOUNDED) settle(s);
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         if constexpr (!BOUNDED) {
@@ -826,20 +1003,26 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
     }
     at ^= STAGE;
   }
+  }
   __builtin_amdgcn_s_waitcnt(0);  // no copy outlives its work-group
-  if (!CAUSAL || careful) break;
-  float zero = 0.f;  // NaN where a sum is not finite
+  if ((!CAUSAL && (BOUNDED || !piped)) || careful) break;
+  float zero = 0.f;  // NaN where a sum is not finite or passes 2^100
 #pragma unroll
-  for (int dt = 0; dt < 8; ++dt)
+  for (int g = 0; g < 2; ++g) {
+    zero = __builtin_fmaf(l[g] * 0x1p28f, 0.f, zero);
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(acc[dt][g][r], 0.f, zero);
+      for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(acc[dt][g][r] * 0x1p28f, 0.f, zero);
+  }
+  int* bad = (int*)smem;
+  lds_barrier();  // everyone has read the last tiles
   bad[wave] = active && __builtin_amdgcn_ballot_w64(zero != 0.f) != 0;
   lds_barrier();
   if (!(bad[0] | bad[1] | bad[2] | bad[3])) break;
   careful = true;
-  issue(key0, 0);  // (every wave is done with the last tile)
+  lds_barrier();  // everyone has read the flags
+  issue(key0, 0);
   }
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
@@ -898,6 +1081,15 @@ bool split_tiles(const dit_packed_shape& s) {
   return items < SPLIT_WORKERS && 20 + 2.1 * units * items / SPLIT_WORKERS < units * (items > SPLIT_WORKERS / 2 ? 2.1 : 1.6);
 }
 
+// Whether the pipelined loop is the faster one: it fills and drains over some tiles.  In us, pipelined and
+// not, whole tiles: 8 of 512 x 512 causal, 28 / 4 heads 29.8 26.7; 1024 x 1024 29.0 31.8; 4096 x 4096, 16 / 4 99 114;
+// 16384 x 16384 983 1107.  Shares of 24 tiles (5 of 701 x 5003, 12 / 4, bounded) 97 75, of 36 (256 x 16384, 32 / 8) 90
+// 96, of 128 (1024 x 16384) 265 304.
+bool pipelined(const dit_packed_shape& s) {
+  const double units = (double)s.Tk / s.batch / KT;
+  return split_tiles(s) ? units * (double)(tiles_of(s, ROWS) * s.kv_heads) >= 32.0 * SPLIT_WORKERS : units >= 12;
+}
+
 size_t attention_packed_ws_bytes(const dit_packed_shape& s) {
   if (s.batch == 0 || s.Tq == 0) return 0;
   const int few = few_rows(s);
@@ -934,10 +1126,12 @@ hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int
     else hipLaunchKernelGGL((packed_join_kernel<32, 32, 4>), dim3(items, few / rows), dim3(256), 0, st, P, rows);
     return hipGetLastError();
   }
+  const bool pipe = pipelined(s);
   if (split_tiles(s)) {
     P.workers = SPLIT_WORKERS;
     P.least = SPLIT_LEAST;
-    fn = DIT_PICK(attn_packed_kernel, DIT_COMMA true);
+    fn = pipe ? DIT_PICK(attn_packed_kernel, DIT_COMMA true DIT_COMMA true)
+              : DIT_PICK(attn_packed_kernel, DIT_COMMA true DIT_COMMA false);
     hipLaunchKernelGGL(fn, dim3(SPLIT_WORKERS), dim3(256), 0, st, P);
     const uint32_t items = (uint32_t)(tiles_of(s, ROWS) * s.kv_heads);
     const int rows = items <= 128 ? 8 : 32;
@@ -946,7 +1140,8 @@ hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int
     return hipGetLastError();
   }
   P.ranked = s.batch > 1 && s.batch <= 64 && tiles_of(s, ROWS) * s.kv_heads > SPLIT_WORKERS;
-  fn = DIT_PICK(attn_packed_kernel, DIT_COMMA false);
+  fn = pipe ? DIT_PICK(attn_packed_kernel, DIT_COMMA false DIT_COMMA true)
+            : DIT_PICK(attn_packed_kernel, DIT_COMMA false DIT_COMMA false);
   hipLaunchKernelGGL(fn, dim3((uint32_t)(tiles_of(s, ROWS) * s.kv_heads)), dim3(256), 0, st, P);
   return hipGetLastError();
 }

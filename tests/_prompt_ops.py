@@ -68,7 +68,8 @@ def attend(q, k, v, *, qoff, koff, heads, kv_heads=None, klen=None, causal=False
     With weights w_j: every probability carries a relative error of at most e = 2^-8 (its rounding to bf16) plus
     that of its logit: f32 sums of 128 products (128 2^-24 |q||k|), two roundings and exp2's.  Numerator and
     sum take the same rounded values, so the output moves by at most e sum w_j |v_j - o| / (1 - e); the f32 sums
-    over n keys add n 2^-24 sum w_j |v_j|."""
+    over n keys add n 2^-24 sum w_j |v_j|.  Of many keys sum w_j |v_j - o| is bounded by the square root of
+    sum w_j (v_j - o)^2 = sum w_j v_j^2 - o^2, as means are by root mean squares."""
     G = kv_heads or heads
     Tq, Tk = q.shape[0], k.shape[0]
     out = np.full((Tq, heads * 128), np.nan)
@@ -100,7 +101,7 @@ def attend(q, k, v, *, qoff, koff, heads, kv_heads=None, klen=None, causal=False
                 o = w @ vv
                 size = np.linalg.norm(qq, axis=1, keepdims=True) * np.linalg.norm(kk, axis=1).max() / np.sqrt(128)
                 e = 2.0 ** -8 + (130 * 2.0 ** -24) * size + 2.0 ** -21 * (1 + np.abs(np.where(see, s, 0)).max(1, keepdims=True))
-                spread = np.stack([(w * np.abs(vv[:, i][None] - o[:, i][:, None])).sum(1) for i in range(128)], 1)
+                spread = np.sqrt(np.maximum(w @ vv ** 2 - o ** 2, 0)) if m > 600 else np.stack([(w * np.abs(vv[:, i][None] - o[:, i][:, None])).sum(1) for i in range(128)], 1)
                 out[r0:r1, c] = o
                 tol[r0:r1, c] = e * spread * 1.01 + (m + 16) * 2.0 ** -24 * (w @ np.abs(vv))
     return out, tol

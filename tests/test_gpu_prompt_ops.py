@@ -529,8 +529,51 @@ def test_packed_attention_of_long_sequences(bounded, causal):
     packed(torch, [100], [8000], 3, 3, causal=causal, bounded=bounded, seed=3)
 
 
-@pytest.mark.parametrize("ql,kl", [([300, 80], [300, 80]), ([3, 2], [900, 700]), ([20], [500])])
-def test_keys_that_a_query_does_not_see_do_not_reach_it(ql, kl):
+# long enough for the pipelined loop: whole tiles (odd and even counts of them, ragged ends, short sequences among long
+# ones), and shares of few long ones
+LONG = [([1100], [1100], 16, 16), ([1500, 40, 2000], [1500, 900, 2001], 12, 4), ([1300, 5], [1216, 1344], 16, 8),
+        ([300], [30000], 12, 12)]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("bounded", [False, True])
+@pytest.mark.parametrize("ql,kl,heads,kv_heads", LONG)
+def test_packed_attention_pipelined(ql, kl, heads, kv_heads, bounded, causal):
+    torch = torch_cuda()
+    packed(torch, ql, kl, heads, kv_heads, causal=causal, bounded=bounded, pad=8 if len(ql) % 2 else 0)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("top", [1.0, 60.0, 90.0, 400.0])
+@pytest.mark.parametrize("ql,kl,heads", [([1100], [1100], 16), ([300], [30000], 12)])
+def test_logits_far_above_the_first_tile_s(ql, kl, heads, top, causal):
+    """Logits that rise along the keys by `top`: the first tile's maximum is no shift for the last one's where
+    e^top passes 2^100."""
+    torch = torch_cuda()
+
+    def rising(qb, kb, vb, qoff, koff):
+        n = kb.shape[0]
+        ramp = np.linspace(0, top / (2 * np.sqrt(128)), n)[:, None] * np.ones((1, 128))
+        for h in range(0, kb.shape[1], 256):        # every other head; the others' logits are ordinary
+            kb[:, h:h + 128] = bf16_bits(ramp)
+            qb[:, h:h + 128] = bf16_bits(np.full((qb.shape[0], 128), 2.0))
+    packed(torch, ql, kl, heads, heads, causal=causal, change=rising)
+
+
+def test_values_near_the_largest_number():
+    """Sums of values of 2^100 and more leave f32's range before they are divided, or pass it in parts."""
+    torch = torch_cuda()
+
+    def large(qb, kb, vb, qoff, koff):
+        vb[:] = bf16_bits(bits_to_f64(vb) * 2.0 ** 118)
+    for ql, kl, heads in (([1100], [1100], 16), ([300], [3000], 2), ([70], [70], 2), ([2], [5000], 2)):
+        for causal in (True, False):
+            packed(torch, ql, kl, heads, heads, causal=causal, change=large, bounded=True, scale=0.5)
+
+
+@pytest.mark.parametrize("ql,kl,heads,kv_heads", [([300, 80], [300, 80], 4, 2), ([3, 2], [900, 700], 4, 2), ([20], [500], 4, 2),
+                                                  ([2100], [2100], 4, 2), ([1100], [1100], 16, 16)])
+def test_keys_that_a_query_does_not_see_do_not_reach_it(ql, kl, heads, kv_heads):
     """Infinities and NaN in later keys' values: causal queries before them keep their results, those from them on do not."""
     torch = torch_cuda()
     for bad in (0x7FC0, 0x7F80, 0xFF80):
@@ -541,14 +584,14 @@ def test_keys_that_a_query_does_not_see_do_not_reach_it(ql, kl):
                 j = kl[z] - max(1, ql[z] // 2)          # seen by the later half of the queries
                 vb[koff[z] + j, 5], kb[koff[z] + j, 7] = bad, 0x7FC0 if bad == 0x7FC0 else kb[koff[z] + j, 7]
                 at.append(j)
-        got, y, d = packed(torch, ql, kl, 4, 2, change=change, exact_rows=False)
+        got, y, d = packed(torch, ql, kl, heads, kv_heads, change=change, exact_rows=False)
         for z, j in enumerate(at):
             rows = np.arange(int(np.sum(ql[:z])), int(np.sum(ql[:z + 1])))
             before = rows[np.arange(ql[z]) + kl[z] - ql[z] < j]
             after = rows[np.arange(ql[z]) + kl[z] - ql[z] >= j]
             g, w, t = got[before], y[before], d[before]
             with np.errstate(invalid="ignore"):
-                full, dd = packed(torch, ql, kl, 4, 2, change=lambda qb, kb, vb, qo, ko: clear(vb, kb, ko, at), exact_rows=False)[1:]
+                full, dd = packed(torch, ql, kl, heads, kv_heads, change=lambda qb, kb, vb, qo, ko: clear(vb, kb, ko, at), exact_rows=False)[1:]
             assert (np.abs(g - full[before]) <= dd[before] + BF16 * (np.abs(full[before]) + dd[before])).all()
             bad_col = got[after][:, 5]
             assert (~np.isfinite(bad_col)).all()
@@ -576,7 +619,7 @@ def test_packed_attention_rising_and_overflowing_logits():
     def falling_out(qb, kb, vb, qoff, koff):
         qb[:, :128] = bf16_bits(np.full((qb.shape[0], 128), 1e30))
         kb[:, :128] = bf16_bits(np.where(np.arange(kb.shape[0])[:, None] % 3 == 0, 1.0, -1e30) * np.ones((1, 128)))
-    for ql, kl in (([130], [400]), ([1], [400])):
+    for ql, kl in (([130], [400]), ([1], [400]), ([1100], [1100])):
         got, _, _ = packed(torch, ql, kl, 1, 1, causal=False, change=falling_out, exact_rows=False)
         assert np.isfinite(got).all()       # -inf logits count for nothing beside finite ones
 
