@@ -361,8 +361,8 @@ def check_rotary(rows, heads, head_dim, rot, *, half, bf16, pairs=None, reach=50
 @pytest.mark.parametrize("half", [True, False])
 @pytest.mark.parametrize("rows,heads,head_dim,rot,pairs", [
     (1, 1, 128, 128, None), (1, 40, 128, 128, None), (37, 7, 128, 64, None), (5, 3, 64, 64, None), (300, 5, 128, 128, [22, 21, 21]),
-    (33, 2, 256, 96, [8, 20, 20]), (70, 3, 96, 20, None), (9, 2, 8, 2, None), (21, 3, 40, 26, [6, 0, 7]), (3, 2, 512, 512, [64, 64, 64, 64]),
-    (1000, 24, 128, 128, [8, 28, 28])])
+    (33, 2, 256, 96, [8, 20, 20]), (70, 3, 96, 20, None), (9, 2, 8, 2, None), (21, 3, 40, 26, [6, 0, 7]), (3, 2, 512, 512, [64, 64, 64, 64]), (6, 3, 128, 100, None),
+    (7, 2, 24, 22, None), (4, 5, 16, 10, None), (5, 2, 72, 70, [30, 5]), (2, 3, 128, 126, None), (3, 2, 40, 16, None), (1000, 24, 128, 128, [8, 28, 28])])
 def test_rotary(rows, heads, head_dim, rot, pairs, half, bf16, in_place):
     check_rotary(rows, heads, head_dim, rot, half=half, bf16=bf16, pairs=pairs, in_place=in_place,
                  pad=16 if rows % 2 else 0, scale=1.0 if rows % 3 else 1.277)
