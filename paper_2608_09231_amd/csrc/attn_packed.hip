@@ -178,8 +178,8 @@ __device__ __forceinline__ bool not_finite(const bf16x8_t& f) {
 // A launch's work as one line of units: sequence by sequence, tile of R rows by tile and key head
 // by key head (an item), KEYS keys of it each (one unit at least).  Workers take `per`
 // consecutive units each, so that sequences of any lengths fill the chip evenly; where an item is
-// shared its parts are joined from the workspace.  Worker w's part of item i lies in slot w + i
-// there: from one part to the next either w or i grows.
+// shared its parts are joined from the workspace.  Worker w's part that begins where its units do
+// lies in slot 2 w there, one that begins later (and is cut off by the worker's end) in slot 2 w + 1.
 struct Place {
   int z, tile, kh, unit, n;  // unit of n
   int64_t item;
@@ -219,11 +219,17 @@ struct Line {
     while (l.z0 + 64 < P.batch) l.next();
     return l.cost_base + readlane64(l.cost_end, 63);
   }
-  // Place of unit u (below the total, not before the last one asked for).
+  // Place of unit u (below the total, not before the last one asked for).  Offsets that
+  // change under a running call may find none: then a place of no rows.
   __device__ __forceinline__ Place at(int64_t u) {
-    while (u >= cost_base + readlane64(cost_end, 63)) next();
-    const int l = __ffsll((unsigned long long)__ballot(cost_base + cost_end > u)) - 1;
+    while (u >= cost_base + readlane64(cost_end, 63) && z0 + 64 < P.batch) next();
+    const uint64_t here = __ballot(cost_base + cost_end > u);
     Place p;
+    if (!here) {
+      p.z = -1;
+      return p;
+    }
+    const int l = __ffsll((unsigned long long)here) - 1;
     p.z = z0 + l;
     p.n = __builtin_amdgcn_readlane(n, l);
     const int64_t rest = u - cost_base - (readlane64(cost_end, l) - readlane64(cost, l));
@@ -263,13 +269,14 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows
   const int z = line.z0 + l, n = __builtin_amdgcn_readlane(line.n, l);
   const int64_t i = item - line.items_base - (readlane64(line.items_end, l) - readlane64(line.items, l));
   const int64_t a = line.cost_base + readlane64(line.cost_end, l) - readlane64(line.cost, l) + i * n;
-  const int64_t w0 = a / per, w1 = (a + n - 1) / per;
+  const int64_t w0 = a / per, w1 = (a + n - 1) / per;  // the item's workers
   if (w0 == w1) return;  // one worker has stored it
   const Seq s = seq_of(P, z);
   const int tile = (int)(i / P.kv_heads), kh = (int)(i - (int64_t)tile * P.kv_heads);
   const int parts = (int)(w1 - w0) + 1, each = (parts + PG - 1) / PG;
   const int64_t pf = part_floats(R);
-  const float* w = P.ws + (w0 + item) * pf;
+  const int64_t late = a != w0 * per;  // the first worker's part is not its units' beginning
+  auto part_of = [&](int p) { return P.ws + (2 * (w0 + p) + (p == 0 ? late : 0)) * pf; };
   for (int row0 = blockIdx.y * rows; row0 < min((int)(blockIdx.y + 1) * rows, s.lq * P.group - tile * R); row0 += RB) {
   const int row = row0 + (tid >> 5) / PG, r = tile * R + row, qi = r / P.group, h = kh * P.group + r - qi * P.group;
   const bool in = r < s.lq * P.group;
@@ -294,7 +301,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows
     float m[U], ls[U], nm = mx;
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const float* x = w + min(p + j, p1 - 1) * pf;
+      const float* x = part_of(min(p + j, p1 - 1));
       v[j] = *(const f32x4_t*)(x + row * D + c);
       ls[j] = x[R * D + row];
       m[j] = x[R * D + R + row];
@@ -400,7 +407,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(qf[g][t]));
   };
-  auto leave = [&](const Place& p, const Seq& s) {
+  auto leave = [&](const Place& p, const Seq& s, int late) {
     const int nrows = s.lq * P.group;
     const bool whole = first == 0 && p.unit == p.n - 1;
 #pragma unroll
@@ -417,7 +424,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
           *(uint2*)(op + 16 * dt) = make_uint2(pack_bf16x2(acc[dt][g][0] * inv, acc[dt][g][1] * inv),
                                                pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
       } else {
-        float* w = P.ws + (worker + p.item) * part_floats(R);
+        float* w = P.ws + (2 * (int64_t)worker + late) * part_floats(R);
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(w + at * D + 16 * dt + 4 * lq) = acc[dt][g];
         if (lq == 0) {
@@ -429,17 +436,21 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   };
 
   Place cur = line.at(begin);
+  if (cur.z < 0) return;
   Seq seq = seq_of(P, cur.z);
+  int late = 0;
   issue(cur, seq, true, 0);
   enter(cur, seq);
   int st = 0;
   for (int64_t u = begin; u < end; ++u) {
     Place nxt = cur;
     Seq nseq = seq;
-    const bool more = u + 1 < end, change = more && cur.unit + 1 == cur.n;
+    bool more = u + 1 < end;
+    const bool change = more && cur.unit + 1 == cur.n;
     if (change) {
       nxt = line.at(u + 1);
-      nseq = seq_of(P, nxt.z);
+      if (nxt.z < 0) more = false;
+      else nseq = seq_of(P, nxt.z);
     } else {
       ++nxt.unit;
     }
@@ -551,9 +562,11 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
       }
     }
     if (change || !more) {
-      leave(cur, seq);
+      leave(cur, seq, late);
+      late = 1;
       if (more) enter(nxt, nseq);
     }
+    if (!more) break;
     cur = nxt;
     seq = nseq;
     st ^= 1;
@@ -626,6 +639,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
   int64_t u = 0, end = 1;
   Place p{};
   Seq s_;
+  [[maybe_unused]] int late = 0;
   if constexpr (SPLIT) {
     Line<ROWS, KT> line(P);
     const int64_t total = line.total(), per = units_each(total, P.workers, P.least);
@@ -644,6 +658,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
   if constexpr (SPLIT) {
     Line<ROWS, KT> line(P);  // (anew for each item: few, and the registers are the loop's)
     p = line.at(u);
+    if (p.z < 0) return;
     s_ = seq_of(P, p.z);
   }
   const int tile = p.tile, kh = p.kh;
@@ -1039,7 +1054,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
                                              pack_bf16x2(acc[dt][g][2] * inv, acc[dt][g][3] * inv));
     } else {
       const int in = 32 * wave + 16 * g + lr;
-      float* w = P.ws + (worker + p.item) * part_floats(ROWS);
+      float* w = P.ws + (2 * (int64_t)worker + late) * part_floats(ROWS);
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(w + in * D + 16 * dt + 4 * lq) = acc[dt][g];
       if (lq == 0) {
@@ -1049,6 +1064,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
     }
   }
   if constexpr (SPLIT) {
+    late = 1;
     if (u < end) lds_barrier();  // everyone is done with the last tile: its place takes the next item's
   }
   } while (SPLIT && u < end);
@@ -1083,18 +1099,18 @@ bool split_tiles(const dit_packed_shape& s) {
 
 // Whether the pipelined loop is the faster one: it fills and drains over some tiles.  In us, pipelined and
 // not, whole tiles: 8 of 512 x 512 causal, 28 / 4 heads 29.8 26.7; 1024 x 1024 29.0 31.8; 4096 x 4096, 16 / 4 99 114;
-// 16384 x 16384 983 1107.  Shares of 24 tiles (5 of 701 x 5003, 12 / 4, bounded) 97 75, of 36 (256 x 16384, 32 / 8) 90
-// 96, of 128 (1024 x 16384) 265 304.
+// 16384 x 16384 983 1107.  Shares of 33 tiles (5 of up to 701 x 5003 in a cache, half filled, 12 / 4, bounded) 86 75, of 36
+// (256 x 16384, 32 / 8) 90 96, of 128 (1024 x 16384) 265 304.
 bool pipelined(const dit_packed_shape& s) {
   const double units = (double)s.Tk / s.batch / KT;
-  return split_tiles(s) ? units * (double)(tiles_of(s, ROWS) * s.kv_heads) >= 32.0 * SPLIT_WORKERS : units >= 12;
+  return split_tiles(s) ? units * (double)(tiles_of(s, ROWS) * s.kv_heads) >= 64.0 * SPLIT_WORKERS : units >= 12;
 }
 
 size_t attention_packed_ws_bytes(const dit_packed_shape& s) {
   if (s.batch == 0 || s.Tq == 0) return 0;
   const int few = few_rows(s);
-  if (few) return (FEW_WORKERS + tiles_of(s, few) * s.kv_heads) * part_floats(few) * sizeof(float);
-  if (split_tiles(s)) return (SPLIT_WORKERS + tiles_of(s, ROWS) * s.kv_heads) * part_floats(ROWS) * sizeof(float);
+  if (few) return 2 * FEW_WORKERS * part_floats(few) * sizeof(float);
+  if (split_tiles(s)) return 2 * SPLIT_WORKERS * part_floats(ROWS) * sizeof(float);
   return 0;
 }
 

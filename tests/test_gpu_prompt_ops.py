@@ -531,8 +531,7 @@ def test_packed_attention_of_long_sequences(bounded, causal):
 
 # long enough for the pipelined loop: whole tiles (odd and even counts of them, ragged ends, short sequences among long
 # ones), and shares of few long ones
-LONG = [([1100], [1100], 16, 16), ([1500, 40, 2000], [1500, 900, 2001], 12, 4), ([1300, 5], [1216, 1344], 16, 8),
-        ([300], [30000], 12, 12)]
+LONG = [([1100], [1100], 16, 16), ([1500, 40, 2000], [1500, 900, 2001], 12, 4), ([1300, 5], [1216, 1344], 16, 8)]
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -543,9 +542,15 @@ def test_packed_attention_pipelined(ql, kl, heads, kv_heads, bounded, causal):
     packed(torch, ql, kl, heads, kv_heads, causal=causal, bounded=bounded, pad=8 if len(ql) % 2 else 0)
 
 
-@pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("top", [1.0, 60.0, 90.0, 400.0])
-@pytest.mark.parametrize("ql,kl,heads", [([1100], [1100], 16), ([300], [30000], 12)])
+@pytest.mark.parametrize("bounded,causal", [(False, True), (True, True), (False, False)])
+def test_packed_attention_pipelined_shares(bounded, causal):
+    torch = torch_cuda()
+    packed(torch, [300], [60000], 12, 12, causal=causal, bounded=bounded)
+
+
+@pytest.mark.parametrize("ql,kl,heads,top,causal", [
+    *[([1100], [1100], 16, top, causal) for top in (1.0, 60.0, 90.0, 400.0) for causal in (True, False)],
+    ([300], [60000], 12, 60.0, True), ([300], [60000], 12, 400.0, False)])
 def test_logits_far_above_the_first_tile_s(ql, kl, heads, top, causal):
     """Logits that rise along the keys by `top`: the first tile's maximum is no shift for the last one's where
     e^top passes 2^100."""
@@ -889,6 +894,24 @@ def test_packed_attention_in_a_workspace_of_its_size(ql, kl, heads, kv_heads, bo
         assert bool((buf[:256] == fill).all()) and bool((buf[256 + nbytes:] == fill).all())
         res.append(o)
     assert torch.equal(res[0], res[1]) and torch.equal(res[0], res[2])
+
+
+@pytest.mark.parametrize("n,heads,kv_heads,Tk", [(1, 4, 4, 500), (64, 2, 1, 5000), (300, 4, 2, 600)])
+def test_sequences_that_overlap_stay_inside(n, heads, kv_heads, Tk):
+    """Offsets that fall back name the same rows many times: nothing outside o's rows and the workspace is written."""
+    torch = torch_cuda()
+    g = torch.Generator("cuda").manual_seed(n)
+    batch = 41
+    q, k, v = (torch.randn(t, h * 128, device="cuda", generator=g).bfloat16() for t, h in ((n, heads), (Tk, kv_heads), (Tk, kv_heads)))
+    qoff = torch.tensor([0, n] * (batch // 2) + [0, n], dtype=torch.int32, device="cuda")
+    koff = torch.tensor([0, Tk] * (batch // 2) + [0, Tk], dtype=torch.int32, device="cuda")
+    nbytes = binding.attention_packed_ws_bytes(batch=batch, Tq=n, Tk=Tk, heads=heads, kv_heads=kv_heads)
+    buf = torch.full((nbytes + 512,), FILL, dtype=torch.uint8, device="cuda")
+    o = torch.full((n + 2, heads * 128), 7.0, device="cuda", dtype=torch.bfloat16)
+    binding.attention_packed_bf16(q, k, v, o[1:n + 1], qoff=qoff, koff=koff, heads=heads, kv_heads=kv_heads,
+                                  ws=buf[256:256 + nbytes] if nbytes else None)
+    assert bool((buf[:256] == FILL).all()) and bool((buf[256 + nbytes:] == FILL).all())
+    assert bool((o[0] == 7).all()) and bool((o[n + 1] == 7).all())
 
 
 def test_calls_lie_on_the_stream_they_are_given():
