@@ -601,7 +601,12 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
 // in LDS: two work-groups of 64 x 128 (three slices) or 128 x 128 (two) per CU, or
 // one of 256 x 128 (three).  For launches that 256 x 256 tiles would not fill.  The waves
 // meet before every step kt; slice kt + 1 has landed, and slice kt, whose fragments are all in
-// registers, gives its place to slice kt + ST.  The fragments of kt + 1 are read under the MFMAs of kt.
+// registers, gives its place to slice kt + ST at once (late in the step: 20 K slices of 192 and 128 x 128
+// tiles 29 and 30 us for 27 and 29).  The fragments of kt + 1 are read under the MFMAs of kt.
+//
+// 512 x 10240 x 5120 (192 x 128 tiles): 27 us, 2.0 PFLOP/s, and 0.86 us for each further 256 of K: without the
+// copies 0.58, without the reads of fragments 0.86, MFMAs alone 0.47.  What bounds it is the way
+// from L2: 40 KB a slice and CU, 11 TB/s over the chip.
 template <int BM, int KIND>
 __global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel(Fp4Prob P) {
   constexpr int ST = BM == 128 ? 2 : 3;
@@ -610,7 +615,8 @@ __global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel
   constexpr int SLICE = (BM + 128) * 128, RING = ST * SLICE, GROUP = (BM + 128) * 16;
   constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW, INS = A_INS + W_INS;
   constexpr int TILE = BM * 128 * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[RING + 2 * GROUP > TILE ? RING + 2 * GROUP : TILE];
+  constexpr int LDS = RING + 2 * GROUP + 16;  // (16: behind the last row's scales, see read_scales)
+  __shared__ __attribute__((aligned(1024))) char smem[LDS > TILE ? LDS : TILE];
   int tm, tn;
   tile_at(P, xcd_remap(blockIdx.x, P.tiles_m * P.tiles_n), tm, tn);
   const int m0 = tm * BM, n0 = tn * 128;
@@ -648,10 +654,11 @@ __global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel
   auto issue_scales = [&](int g) {
     copy16_unseen(sbase, smem + RING + (g & 1) * GROUP + swave * 1024, 4 * g < sc.nd ? soff : OOB, 4 * max(sc.start(g), 0));
   };
+  // (two dwords in one read; a second one past the row's last is another row's, and valid() clears it)
   auto read_scales = [&](int kt, uint32_t(&x)[NF][2], int f) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int g = kt >> 1, at = RING + (g & 1) * GROUP + 4 * sc.place(g, 2 * kt + h);
+      const int g = kt >> 1, at = RING + (g & 1) * GROUP + 4 * sc.place(g, 2 * kt) + 4 * h;
       x[f][h] = *(const uint32_t*)(smem + at + 16 * ((f < TM ? WM * wm + 16 * f : BM + 64 * wn + 16 * (f - TM)) + lr));
     }
   };
@@ -713,7 +720,7 @@ __global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel
         fn[r][hq] = rd(un, r, hq);
         if (hq == 0) read_scales(kt + 1, xn, r);
       }
-      if (q >= 2 * TM * TN - INS) issue1(u, kt + ST, q - (2 * TM * TN - INS));
+      if (q < INS) issue1(u, kt + ST, q);
       __builtin_amdgcn_sched_barrier(0);
     }
     place_scales(kt + 1, xn);
@@ -977,17 +984,18 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
     return one ? DIT_SMALL(1, EPI_K_ANY) : DIT_SMALL(2, EPI_K_ANY);
 #undef DIT_SMALL
   }
-  // Rounds of the chip times a tile's time, which is some us and some per slice of 256 of K
-  // (fitted to each kernel over the sizes below).  In us, 64 x 128, 128 x 128, 256 x 128 and 256 x 256 tiles:
-  //   512 x 10240 x 5120  37 32 34 39    1024 x 10240 x 5120 57 57 58 42    512 x 5120 x 5120  22 24 28 36
-  //   2048 x 4096 x 4096  37 29 31 34    4096 x 4096 x 1024  30 23 23 21    1333 x 1000 x 2336 11 14 17 21
-  struct Tile { int bm, bn, per_cu; double slice_us, us; };
+  // Rounds of the chip times a tile's time, which is some us and some per slice of 256 of K, fewer in a round
+  // that fills at most half of the chip (fitted to each kernel over the sizes below).  In us, 64 x 128, 128 x 128,
+  // 192 x 128, 256 x 128 and 256 x 256 tiles:
+  //   512 x 10240 x 5120  34 29 27 30 39    1024 x 10240 x 5120 53 48 48 55 42    512 x 5120 x 5120  21 20 23 27 36
+  //   2048 x 4096 x 4096  35 28 38 28 34    4096 x 4096 x 1024  29 22 27 22 21    1333 x 1000 x 2336 10 12 14 16 21
+  struct Tile { int bm, bn, per_cu; double half_us, slice_us, us; };
   auto cost = [&](const Tile& c) {
-    const int64_t slots = (int64_t)n_cu * c.per_cu;
-    return (double)((tiles(c.bm, c.bn) + slots - 1) / slots) * ((g.K + 255) / 256 * c.slice_us + c.us);
+    const int64_t slots = (int64_t)n_cu * c.per_cu, n = tiles(c.bm, c.bn), full = (n - 1) / slots, slices = (g.K + 255) / 256;
+    return full * (slices * c.slice_us + c.us) + slices * (2 * (n - full * slots) <= slots ? c.half_us : c.slice_us) + c.us;
   };
-  const Tile cfg[] = {{64, 128, 2, 0.67, 4.8}, {128, 128, 2, 1.31, 6.2}, {256, 128, 1, 1.35, 6.2}, {256, 256, 1, 1.75, 12},
-                      {192, 128, 1, 1.05, 6.2}};
+  const Tile cfg[] = {{64, 128, 2, 0.55, 0.8, 4}, {128, 128, 2, 0.69, 1.25, 6}, {256, 128, 1, 1.0, 1.3, 6},
+                      {256, 256, 1, 1.35, 1.75, 12}, {192, 128, 1, 0.75, 1.0, 6}};
   int best = 0;
   for (int c = 1; c < 5; ++c)
     if (cost(cfg[c]) < cost(cfg[best])) best = c;
