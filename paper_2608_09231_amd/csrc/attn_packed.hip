@@ -251,7 +251,7 @@ __host__ __device__ __forceinline__ int64_t part_floats(int rows) { return (int6
 // Joins the parts of an item's rows and stores the normalised output.  32 threads a
 // row, 4 columns each; PG of them take consecutive parts, U at a time, whose loads are in flight
 // together, and the PG meet in LDS in their order.
-// A work-group takes `rows` rows, 8 / PG at a time.
+// A work-group takes `rows` rows, 8 / PG at a time.  Bound by memory: 44 MB of parts of 128 rows 13 us.
 template <int R, int KEYS, int PG>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -343,6 +343,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows
 // and V from memory.  Every wave is a worker with units of 32 keys in two buffers
 // of LDS of its own, and no wave waits for another.  With MFMAs to spare, probabilities
 // enter the second product as two bf16 parts, so that only the output is rounded to 8 bits.
+// 16 tokens against up to 8192 keys each, 32 heads on 8: 46 us for 263 MB, 5.7 TB/s, and 5 for joining.
 template <bool BOUNDED, bool CAUSAL, int NG>
 __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -626,6 +627,11 @@ __device__ __forceinline__ bool ranked_tile(const PackedArgs& P, int t, Seq& seq
 //
 // SPLIT: launches whose tiles are fewer than the chip's places for work-groups share the units
 // of the whole launch out (Line); a work-group may go through parts of several items.
+//
+// 16384 tokens, 16 heads on 4, causal: 0.96 ms, 1.15 PFLOP/s, MFMAs busy 0.53 at a power-limited 2.02 GHz.  8 prompts
+// of up to 512, 28 on 4: 26 us, one round of eight tiles of keys one after the other.  5 of up to 701 x 5003, 12 on
+// 4: 66 us and 13 for joining; workers in the order of the XCDs, key heads first, so that neighbours share keys in L2: 5 %
+// less there, but up to 10 more elsewhere (256 x 16384 98 to 109, 1000 x 1500 35 to 37).
 template <bool BOUNDED, bool CAUSAL, bool SPLIT, bool PIPE>
 __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -1073,7 +1079,9 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 
 }  // namespace
 
-// Few rows a sequence, on average: the memory-bound kernel, a wave of which takes 16 or 32.
+// Few rows a sequence, on average: the memory-bound kernel, a wave of which takes 16 or 32.  In us, against tiles of
+// 128 rows, shared out: 16 tokens with 8192 keys, 32 / 8 heads 51 56; 4 x 8192 19 22; 16 of 4 x 4096 36 37; 1 x 16384
+// 25 23; 64 tokens with 1024 keys 34 31 (and half the error: the probabilities stay unrounded).
 int few_rows(const dit_packed_shape& s) {
   const int64_t rows = (int64_t)s.Tq * (s.heads / s.kv_heads);
   return rows <= 16 * (int64_t)s.batch ? 16 : rows <= 32 * (int64_t)s.batch ? 32 : 0;
@@ -1086,31 +1094,37 @@ int64_t tiles_of(const dit_packed_shape& s, int r) {
 constexpr int FEW_WORKERS = 1024, FEW_LEAST = 4;
 // Whether the tiles are fewer than the places for work-groups of 256 CUs (two each) and sharing their
 // keys out is worth the joining: in us, whole tiles take 1.6 for 64 keys (2.1 beside
-// another work-group), shared ones 2.1 times their share of all, and 20 for parts and joining (fitted).  By the average
+// another work-group, and less where causal tiles of few keys stand beside those of many), shared ones 2.1 times their
+// share of all, masked or not, and 20 for parts and joining (fitted; shares of what causal tiles see alone begin and
+// end inside items: 2/2 16384 x 16384 183, but 16/4 2048 x 8192 177).  By the average
 // length, which is all that the host knows.  Measured, shared and whole:
 //   heads / key heads, queries x keys   32/8 256 x 16384 101 386   16/16 77 x 4096 23 92   32/8 8 of 64 x 4096 42 101
-//   8/8 2048 x 2048 causal 41 53   12/12 1000 x 1500 34 40   28/4 2048 x 2048 causal 93 63   28/4 512 x 512 causal 24 19
+//   8/8 2048 x 2048 causal 43 47, 2 of up to 4096 x 4096 106 89, 3 of up to 2048 x 2048 65 47   12/12 1000 x 1500 34 40
+//   28/4 2048 x 2048 causal 93 63   28/4 512 x 512 causal 24 19   16/4 2048 x 8192 causal 141 165   2/2 16384 x 16384 causal 230 308
 constexpr int SPLIT_WORKERS = 512, SPLIT_LEAST = 8;
-bool split_tiles(const dit_packed_shape& s) {
+bool split_tiles(const dit_packed_shape& s, bool causal) {
   const int64_t items = tiles_of(s, ROWS) * s.kv_heads;
   const double units = (double)s.Tk / s.batch / KT;
-  return items < SPLIT_WORKERS && 20 + 2.1 * units * items / SPLIT_WORKERS < units * (items > SPLIT_WORKERS / 2 ? 2.1 : 1.6);
+  const double seen = causal ? 1 - 0.5 * std::min(s.Tq, s.Tk) / std::max(s.Tk, 1) : 1;  // of the keys, by the average tile
+  const double whole = std::max(1.6, items > SPLIT_WORKERS / 2 ? 2.1 * seen : 0);
+  return items < SPLIT_WORKERS && 20 + 2.1 * units * items / SPLIT_WORKERS < units * whole;
 }
 
 // Whether the pipelined loop is the faster one: it fills and drains over some tiles.  In us, pipelined and
 // not, whole tiles: 8 of 512 x 512 causal, 28 / 4 heads 29.8 26.7; 1024 x 1024 29.0 31.8; 4096 x 4096, 16 / 4 99 114;
 // 16384 x 16384 983 1107.  Shares of 33 tiles (5 of up to 701 x 5003 in a cache, half filled, 12 / 4, bounded) 86 75, of 36
 // (256 x 16384, 32 / 8) 90 96, of 128 (1024 x 16384) 265 304.
-bool pipelined(const dit_packed_shape& s) {
+bool pipelined(const dit_packed_shape& s, bool split) {
   const double units = (double)s.Tk / s.batch / KT;
-  return split_tiles(s) ? units * (double)(tiles_of(s, ROWS) * s.kv_heads) >= 64.0 * SPLIT_WORKERS : units >= 12;
+  return split ? units * (double)(tiles_of(s, ROWS) * s.kv_heads) >= 64.0 * SPLIT_WORKERS : units >= 12;
 }
 
 size_t attention_packed_ws_bytes(const dit_packed_shape& s) {
   if (s.batch == 0 || s.Tq == 0) return 0;
   const int few = few_rows(s);
   if (few) return 2 * FEW_WORKERS * part_floats(few) * sizeof(float);
-  if (split_tiles(s)) return 2 * SPLIT_WORKERS * part_floats(ROWS) * sizeof(float);
+  // (a causal launch shares out only where another would: seen <= 1)
+  if (split_tiles(s, false)) return 2 * SPLIT_WORKERS * part_floats(ROWS) * sizeof(float);
   return 0;
 }
 
@@ -1142,8 +1156,8 @@ hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int
     else hipLaunchKernelGGL((packed_join_kernel<32, 32, 4>), dim3(items, few / rows), dim3(256), 0, st, P, rows);
     return hipGetLastError();
   }
-  const bool pipe = pipelined(s);
-  if (split_tiles(s)) {
+  const bool split = split_tiles(s, causal), pipe = pipelined(s, split);
+  if (split) {
     P.workers = SPLIT_WORKERS;
     P.least = SPLIT_LEAST;
     fn = pipe ? DIT_PICK(attn_packed_kernel, DIT_COMMA true DIT_COMMA true)
@@ -1155,7 +1169,7 @@ hipError_t launch_attention_packed(const dit_packed_shape& s, const void* q, int
     else hipLaunchKernelGGL((packed_join_kernel<ROWS, KT, 1>), dim3(items, ROWS / rows), dim3(256), 0, st, P, rows);
     return hipGetLastError();
   }
-  P.ranked = s.batch > 1 && s.batch <= 64 && tiles_of(s, ROWS) * s.kv_heads > SPLIT_WORKERS;
+  P.ranked = s.batch > 1 && s.batch <= 64 && tiles_of(s, ROWS) * s.kv_heads > SPLIT_WORKERS / 2;
   fn = pipe ? DIT_PICK(attn_packed_kernel, DIT_COMMA false DIT_COMMA true)
             : DIT_PICK(attn_packed_kernel, DIT_COMMA false DIT_COMMA false);
   hipLaunchKernelGGL(fn, dim3((uint32_t)(tiles_of(s, ROWS) * s.kv_heads)), dim3(256), 0, st, P);

@@ -328,24 +328,30 @@ struct Epi : EpiLdsT<KIND == EPI_K_FP4 ? EPI_K_ANY : KIND, Fp4Prob> {
 
 // 4-bit rows straight from the accumulators of 32 x 32 blocks whose operands changed places:
 // lane (lr, lh) holds row 32 i + lr's columns 8 q + 4 lh .. + 3 of block j, so that a
-// lane and its other half hold a row's 32 TN columns.
+// lane and its other half hold a row's 32 TN columns.  (bf16 rows so stored, 32 bytes at a time, take
+// 1 us a tile more than whole lines by way of LDS.)
 template <int TM, int TN>
 __device__ __forceinline__ void store_fp4(const Fp4Prob& P, f32x16_t (&acc)[TM][TN], int m0, int n0, int lr, int lh) {
 #if defined(__HIP_DEVICE_COMPILE__)
   static_assert(TN == 4, "a head's 128 columns, a dword of scales");
+  typedef uint32_t half_run __attribute__((ext_vector_type(2), aligned(2)));
   auto other_half = [](uint32_t v) {
     const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
     return (threadIdx.x & 32) ? s[0] : s[1];
   };
+  if (P.bias) {
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int n = n0 + 32 * j + 8 * (r >> 2) + 4 * lh + (r & 3);
-      const float b = P.bias && n0 + 32 * j < P.N ? bf16_to_f32(P.bias[n]) : 0.f;
+      for (int q = 0; q < 4; ++q) {
+        const int n = n0 + 32 * j + 8 * q + 4 * lh;  // (N % 32 == 0)
+        const half_run b = *(const half_run*)(P.bias + min(n, P.N - 4));
 #pragma unroll
-      for (int i = 0; i < TM; ++i) acc[i][j][r] += b;
-    }
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][j][4 * q + e] += __uint_as_float(e & 1 ? b[e >> 1] & 0xffff0000u : b[e >> 1] << 16);
+      }
+  }
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = m0 + 32 * i + lr;
@@ -419,6 +425,12 @@ __device__ __forceinline__ void store_fp4(const Fp4Prob& P, f32x16_t (&acc)[TM][
 // The waves meet after substep 2, whose reads were the last of their slice: slice kt +
 // 1 has landed, and slice kt's places take slice kt + 2 during substep 3.  Slices past the
 // last one are copied as zeros (no memory traffic), which keeps every iteration alike.
+//
+// 32760 x 5120 x 13824 1.08 ms, 4.3 PFLOP/s; 32760 x 13824 x 5120 1.24 ms, with GELU and 4-bit rows out 1.38 and 3.4.
+// What bounds it is power (the clock falls to 1.94 GHz, MFMAs busy 0.53 there) and the way through LDS (0.42, and 0.15
+// in conflicts of the scale reads, 2.5 % of the time): without copies 0.93 ms, without
+// fragment reads 1.11, without both 0.87.  A tile's beginning and end take 7 us, 12 with bf16 rows out,
+// which only another work-group on the CU could hide and LDS has no room for.
 template <int KIND>
 __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4, SC = 4 * UNIT, GROUP = 512 * 32;
@@ -761,7 +773,7 @@ __global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel
 // that share K (NT = 32: eight ways, 64: four, 128: two).  Each wave copies its own
 // rows' slices and their scales to a ring of its own in LDS, so that no wave waits for another until
 // their sums meet at the end; the copies read whole 128-byte lines, eight lanes
-// each.  Bound by the way of W from memory.
+// each.  Bound by the way of W from memory: 1 x 13824 x 5120 9.6 us, 3.9 TB/s.
 template <int NT, int RB, int KIND>
 __global__ __launch_bounds__(512) void gemm_fp4_small_kernel(Fp4Prob P) {
   constexpr int NH = NT / 32, KS = 8 / NH, NF = 2 + RB, ST = RB == 1 ? 3 : 2;
@@ -971,7 +983,9 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
                      (g.gap == 0 || g.gap_at % 128 == 0);
   const bool only_gate = plain && gated && g.rms_cols == 0 && g.gelu_from >= g.N && g.gap == 0;
   auto tiles = [&](int bm, int bn) { return (int64_t)((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
-  // Few rows or few tiles: the narrowest tiles that fit the CUs once, to spread the way of W over them.
+  // Few rows or few tiles: the narrowest tiles that fit the CUs once, to spread the way of W over them.  In us,
+  // against 64 x 128 tiles: 1 x 13824 x 5120 10.4 14.8, 16 x 5120 x 13824 13.4 30.3, 32 x 5120 x 5120 9.0 14.7,
+  // 64 x 5120 x 5120 11.8 14.7, 128 x 1024 x 1024 9.2 9.4, 256 x 512 x 4096 8.8 12.0, 128 x 128 x 8192 9.2 19.3.
   const bool one = g.M <= 16;
   const int rows = one ? 16 : 32, widest = one ? 128 : 64;
   int nt = g.rms_cols > 0 ? 128 : 32;
