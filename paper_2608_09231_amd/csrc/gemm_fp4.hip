@@ -426,7 +426,7 @@ __device__ __forceinline__ void store_fp4(const Fp4Prob& P, f32x16_t (&acc)[TM][
 // 1 has landed, and slice kt's places take slice kt + 2 during substep 3.  Slices past the
 // last one are copied as zeros (no memory traffic), which keeps every iteration alike.
 //
-// 32760 x 5120 x 13824 1.08 ms, 4.3 PFLOP/s; 32760 x 13824 x 5120 1.24 ms, with GELU and 4-bit rows out 1.38 and 3.4.
+// 32760 x 5120 x 13824 1.08 ms, 4.3 PFLOP/s; 32760 x 13824 x 5120 1.33 ms, with 4-bit rows out 1.13, with GELU, too, 1.21.
 // What bounds it is power (the clock falls to 1.94 GHz, MFMAs busy 0.53 there) and the way through LDS (0.42, and 0.15
 // in conflicts of the scale reads, 2.5 % of the time): without copies 0.93 ms, without
 // fragment reads 1.11, without both 0.87.  A tile's beginning and end take 7 us, 12 with bf16 rows out,
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
 
 // BM x 128 tiles, waves of 64 x 64 (BM = 64: 32 x 64, 192: 48 x 64), a ring of slices of 256 of K
 // in LDS: two work-groups of 64 x 128 (three slices) or 128 x 128 (two) per CU, or
-// one of 256 x 128 (three).  For launches that 256 x 256 tiles would not fill.  The waves
+// one of 192 x 128 (three).  For launches that 256 x 256 tiles would not fill.  The waves
 // meet before every step kt; slice kt + 1 has landed, and slice kt, whose fragments are all in
 // registers, gives its place to slice kt + ST at once (late in the step: 20 K slices of 192 and 128 x 128
 // tiles 29 and 30 us for 27 and 29).  The fragments of kt + 1 are read under the MFMAs of kt.
@@ -620,9 +620,9 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
 // copies 0.58, without the reads of fragments 0.86, MFMAs alone 0.47.  What bounds it is the way
 // from L2: 40 KB a slice and CU, 11 TB/s over the chip.
 template <int BM, int KIND>
-__global__ __launch_bounds__(BM >= 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel(Fp4Prob P) {
+__global__ __launch_bounds__(BM == 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel(Fp4Prob P) {
   constexpr int ST = BM == 128 ? 2 : 3;
-  constexpr int NW = BM >= 192 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
+  constexpr int NW = BM == 192 ? 8 : 4, WM = BM / (NW / 2);  // waves, rows of a wave
   constexpr int TM = WM / 16, TN = 4, NF = TM + TN;
   constexpr int SLICE = (BM + 128) * 128, RING = ST * SLICE, GROUP = (BM + 128) * 16;
   constexpr int A_INS = BM / 8 / NW, W_INS = 128 / 8 / NW, INS = A_INS + W_INS;
@@ -1000,18 +1000,18 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
   }
   // Rounds of the chip times a tile's time, which is some us and some per slice of 256 of K, fewer in a round
   // that fills at most half of the chip (fitted to each kernel over the sizes below).  In us, 64 x 128, 128 x 128,
-  // 192 x 128, 256 x 128 and 256 x 256 tiles:
-  //   512 x 10240 x 5120  34 29 27 30 39    1024 x 10240 x 5120 53 48 48 55 42    512 x 5120 x 5120  21 20 23 27 36
-  //   2048 x 4096 x 4096  35 28 38 28 34    4096 x 4096 x 1024  29 22 27 22 21    1333 x 1000 x 2336 10 12 14 16 21
+  // 192 x 128 and 256 x 256 tiles (256 x 128 ones were nowhere the fastest):
+  //   512 x 10240 x 5120  34 29 27 39    1024 x 10240 x 5120 53 48 48 42    512 x 5120 x 5120  21 20 23 36
+  //   2048 x 4096 x 4096  35 28 38 34    4096 x 4096 x 1024  29 22 27 21    1333 x 1000 x 2336 10 12 14 21
   struct Tile { int bm, bn, per_cu; double half_us, slice_us, us; };
   auto cost = [&](const Tile& c) {
     const int64_t slots = (int64_t)n_cu * c.per_cu, n = tiles(c.bm, c.bn), full = (n - 1) / slots, slices = (g.K + 255) / 256;
     return full * (slices * c.slice_us + c.us) + slices * (2 * (n - full * slots) <= slots ? c.half_us : c.slice_us) + c.us;
   };
-  const Tile cfg[] = {{64, 128, 2, 0.55, 0.8, 4}, {128, 128, 2, 0.69, 1.25, 6}, {256, 128, 1, 1.0, 1.3, 6},
-                      {256, 256, 1, 1.35, 1.75, 12}, {192, 128, 1, 0.75, 1.0, 6}};
+  const Tile cfg[] = {{64, 128, 2, 0.55, 0.8, 4}, {128, 128, 2, 0.69, 1.25, 6}, {192, 128, 1, 0.75, 1.0, 6},
+                      {256, 256, 1, 1.35, 1.75, 12}};
   int best = 0;
-  for (int c = 1; c < 5; ++c)
+  for (int c = 1; c < 4; ++c)
     if (cost(cfg[c]) < cost(cfg[best])) best = c;
   if (best == 3)
     return go(fp4 ? gemm_fp4_ring_kernel<EPI_K_FP4> : store ? gemm_fp4_ring_kernel<EPI_K_STORE>
@@ -1019,8 +1019,7 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
 #define DIT_TILE(BM, THREADS)                                                                                  \
   go(fp4 ? gemm_fp4_tile_kernel<BM, EPI_K_FP4> : store ? gemm_fp4_tile_kernel<BM, EPI_K_STORE>                  \
                                                        : gemm_fp4_tile_kernel<BM, EPI_K_ANY>, BM, 128, THREADS)
-  if (best == 4) return DIT_TILE(192, 512);
-  if (best == 2) return DIT_TILE(256, 512);
+  if (best == 2) return DIT_TILE(192, 512);
   if (best == 1) return DIT_TILE(128, 256);
   return DIT_TILE(64, 256);
 #undef DIT_TILE

@@ -262,6 +262,28 @@ def test_gemm_scale_of_255_is_nan(M, N, K, out):
     assert np.isnan(got[gone]).all() and (np.abs(got - y)[~gone] <= tol[~gone]).all()
 
 
+# 256 x 256 tiles: one round of them, ragged and not
+LARGE_TILES = [(900, 10240, 288), (1411, 6432, 416), (4096, 4096, 544)]
+
+
+@pytest.mark.parametrize("M,N,K,act", [(*s, act) for s in LARGE_TILES for act in ("none", "gelu", "silu", "rms")
+                                       if act != "rms" or s[1] % 128 == 0])
+def test_gemm_fp4_output_of_large_tiles(M, N, K, act):
+    check_gemm(M, N, K, out="fp4", act=act, rms_cols=N if act == "rms" else 0,
+               gelu_from=0 if act == "gelu" else None, pad=16 if M % 2 else 0, bias=act != "silu")
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32", "gated", "fp4"])
+@pytest.mark.parametrize("M,N,K", LARGE_TILES)
+def test_gemm_scales_at_the_ends_of_large_tiles(M, N, K, out):
+    r = rng(M, N, K, 43)
+    nb = K // 32
+    ends = np.resize([0, 254, 1, 247, 2, 246, 9, 253, 120], nb)
+    a = r.integers(0, 16, (M, K)).astype(np.uint8), np.tile(ends, (M, 1)).astype(np.uint8)
+    w = r.integers(0, 16, (N, K)).astype(np.uint8), np.tile(254 - ends, (N, 1)).astype(np.uint8)
+    check_gemm(M, N, K, out=out, operands=(a, w), bias=False)
+
+
 def test_gemm_fp4_output_of_nan_rows():
     r = rng(23)
     for M, N in ((4, 128), (300, 2048), (4100, 4352)):
