@@ -426,11 +426,12 @@ __device__ __forceinline__ void store_fp4(const Fp4Prob& P, f32x16_t (&acc)[TM][
 // 1 has landed, and slice kt's places take slice kt + 2 during substep 3.  Slices past the
 // last one are copied as zeros (no memory traffic), which keeps every iteration alike.
 //
-// 32760 x 5120 x 13824 1.08 ms, 4.3 PFLOP/s; 32760 x 13824 x 5120 1.33 ms, with 4-bit rows out 1.13, with GELU, too, 1.21.
+// 32760 x 5120 x 13824 1.04 ms, 4.4 PFLOP/s; 32760 x 13824 x 5120 1.25 ms, with 4-bit rows out 1.05, with GELU, too, 1.16.
 // What bounds it is power (the clock falls to 1.94 GHz, MFMAs busy 0.53 there) and the way through LDS (0.42, and 0.15
-// in conflicts of the scale reads, 2.5 % of the time): without copies 0.93 ms, without
-// fragment reads 1.11, without both 0.87.  A tile's beginning and end take 7 us, 12 with bf16 rows out,
-// which only another work-group on the CU could hide and LDS has no room for.
+// in conflicts of the scale reads, 2.5 % of the time): of 1.08 ms the loop takes 0.93 without copies, 1.1 without
+// fragment reads, 0.87 without both.  A tile's beginning and end take 5 us, 10 with bf16 rows out
+// (3 more where the first products waited for both slices and the scales came by way of registers),
+// which only another work-group on the CU could hide, and LDS has no room for it.
 template <int KIND>
 __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   constexpr int UNIT = 256 * 128, INS = 4, TM = 2, TN = 4, SC = 4 * UNIT, GROUP = 512 * 32;
@@ -528,7 +529,9 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
   const integral_constant<int, 0> b0{};
   const integral_constant<int, 2> b2{};
 
-  // W slice kt in unit kt % 2, A slice kt in unit 2 + kt % 2
+  // W slice kt in unit kt % 2, A slice kt in unit 2 + kt % 2; a row that fills no group: by way of registers
+  if (sc.nd >= 8) issue_scales(0);
+  else sc.first(sbase + scale_row(tid), smem + SC, tid);
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
 #pragma unroll
@@ -538,8 +541,7 @@ __global__ __launch_bounds__(512) void gemm_fp4_ring_kernel(Fp4Prob P) {
     }
   }
   issue_scales(1);
-  sc.first(sbase + scale_row(tid), smem + SC, tid);
-  wait_vmcnt_lgkm0<0>();
+  wait_vmcnt_lgkm0<2 * INS + 2>();  // slice 1 and group 1 may be on their way
   barrier_no_fence();
   i32x4_t a0[TM], w0[TN], a1[TM], w1[TN];
 #pragma unroll
@@ -697,7 +699,8 @@ __global__ __launch_bounds__(BM == 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel
     for (int j = 0; j < INS; ++j) issue1(s * SLICE, s, j);
     if (s == 0) {
       issue_scales(1);
-      if (tid < BM + 128) sc.first(sbase + soff, smem + RING, tid);  // (waits for slice 0 and group 1, too)
+      if (sc.nd >= 4) issue_scales(0);
+      else if (tid < BM + 128) sc.first(sbase + soff, smem + RING, tid);  // (waits for slice 0, too)
     }
   }
   wait_vmcnt_lgkm0<(ST - 1) * INS>();
