@@ -444,13 +444,13 @@ class _Call:
         if stream is not None and stream.device != dev:
             raise ValueError("the stream belongs to another device than the tensors")
         self._torch, self._dev, self.stream = torch, dev, stream
-        self._guard = None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+        index = dev.index  # (of a tensor's device: the context is there, and its number needs no asking for it)
+        self._guard = None if torch._C._cuda_getDevice() == index else torch.cuda.device(dev)
+        self.ptr = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
     def __enter__(self):
         if self._guard is not None:
             self._guard.__enter__()
-        self.ptr = self._torch._C._cuda_getCurrentRawStream(self._dev.index) if self.stream is None \
-            else self.stream.cuda_stream
         return self
 
     def __exit__(self, *exc):
@@ -588,6 +588,7 @@ ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 ROTARY_AXES = 4
 _E2M1, _F64 = "pairs of e2m1", "float64"
+_FOUR = C.c_int32 * 4
 _MEANINGS["torch.float64"] = (_F64,)
 _MEANINGS["torch.float4_e2m1fn_x2"] = (_E2M1,)
 for _t in ("torch.uint8", "torch.int8"):
@@ -601,10 +602,12 @@ def fp4_scale_ld(K: int) -> int:
 
 def _values(x, name, M, K, ld):
     """Row stride and type of a matrix that is float32, or bf16 as torch.bfloat16 or int16."""
-    f32 = x.element_size() == 4
-    if f32 and not x.is_floating_point():
+    size, meanings = _TYPES.get(x.dtype) or _type(x)
+    if size != 4:
+        return _rows(x, name, M, K, ld, 2, _BF16), DTYPE_BF16
+    if _F32 not in meanings:
         raise ValueError(f"{name} must be float32 or bf16")
-    return (_rows(x, name, M, K, ld, 4, _F32), DTYPE_F32) if f32 else (_rows(x, name, M, K, ld, 2, _BF16), DTYPE_BF16)
+    return _rows(x, name, M, K, ld, 4, _F32), DTYPE_F32
 
 
 def quant_fp4(x, q, scale, *, M, K, ldx=None, ldq=None, lds=None, stream=None):
@@ -672,17 +675,19 @@ def rotary(x, y, *, pos, freq, rows, heads, head_dim=128, pairs=None, layout=ROT
     [rows] or [axes, rows]; freq: float64 cuda tensor, one per pair; pairs: those of each axis (None: one axis)."""
     lib = load()
     n = freq.numel()
-    pairs = [n] if pairs is None else list(pairs)
-    if not 1 <= len(pairs) <= ROTARY_AXES or sum(pairs) != n:
+    pairs = (n,) if pairs is None else tuple(pairs)
+    axes = len(pairs)
+    if not 1 <= axes <= ROTARY_AXES or sum(pairs) != n:
         raise ValueError(f"pairs must be those of 1 to {ROTARY_AXES} axes, {n} together")
-    (ldx, dtype), (ldy, out) = (_values(t, name, rows, heads * head_dim, ld) for t, name, ld in ((x, "x", ldx), (y, "y", ldy)))
+    ldx, dtype = _values(x, "x", rows, heads * head_dim, ldx)
+    ldy, out = _values(y, "y", rows, heads * head_dim, ldy)
     if dtype != out:
         raise ValueError("x and y must be of one type")
     _rows(freq, "freq", 1, n, None, 8, _F64)
-    ldpos = _rows(pos, "pos", len(pairs), rows, ldpos, 4, _I32) if len(pairs) > 1 or pos.dim() == 2 \
+    ldpos = _rows(pos, "pos", axes, rows, ldpos, 4, _I32) if axes > 1 or pos.dim() == 2 \
         else _rows(pos, "pos", 1, rows, rows, 4, _I32)
     d = RotaryDescC(x.data_ptr(), ldx, y.data_ptr(), ldy, pos.data_ptr(), ldpos, freq.data_ptr(), dtype, rows, heads,
-                    head_dim, 2 * n, layout, len(pairs), (C.c_int32 * 4)(*pairs), scale)
+                    head_dim, 2 * n, layout, axes, _FOUR(*pairs), scale)
     with _Call(stream, x, y, pos, freq) as call:
         _check(lib.dit_rotary(C.byref(d), call.ptr))
 
