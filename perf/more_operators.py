@@ -163,7 +163,7 @@ def prepare(case, seed):
         codes, e = _quantise(x.float())
         sc = torch.full((rows, _scale_ld(K)), 127, dtype=torch.uint8, device="cuda")
         sc[:, :e.shape[1]] = e
-        return _pack(codes).to(torch.uint8), sc.view(E8)
+        return _pack(codes), sc.view(E8)
 
     s = dict(case=c)
     if c["op"] == "rotary":
@@ -333,6 +333,8 @@ def run(state):
     s = state
     if not own:
         return _plain(s)
+    else:  # (the rows that prepare packs are whole numbers of 64 bits; the calls take bytes)
+        s = {**s, **{n: s[n].to(torch.uint8) for n in ("A", "W", "W2") if n in s}}
     from paper_2608_09231_amd import binding as lib
     c = s["case"]
     if c["op"] == "rotary":
