@@ -358,10 +358,14 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   const int64_t begin = worker * per, end = min(total, begin + per);
   if (begin >= end) return;
 
-  // copy c: rows 4 c .. + 3; rows past the last key, and all of none, are zeros
-  auto issue = [&](const Place& p, const Seq& s, bool any, int st) {
+  // keys that row `row` of a sequence's sees, and those that the tile's last row, and so any of its rows, sees
+  auto seen = [&](const Seq& s, int row) { return CAUSAL ? max(s.lk - s.lq + 1 + row / P.group, 0) : s.lk; };
+  auto seen_by = [&](const Place& p, const Seq& s) { return seen(s, min(p.tile * R + R, s.lq * P.group) - 1); };
+  // copy c: rows 4 c .. + 3; rows past the last of `keys` are zeros (what none of the tile's rows sees may
+  // hold infinities or NaN, and 0 times those is NaN)
+  auto issue = [&](const Place& p, const Seq& s, int keys, int st) {
     const int key = p.unit * HK;
-    const int rows = any ? min(s.lk - key, HK) : 0;
+    const int rows = min(keys - key, HK);
     const int64_t at = s.k0 + (rows > 0 ? key : 0);
     const bf16_t* kp = P.k + at * P.ldk + (int64_t)p.kh * D;
     const bf16_t* vp = P.v + at * P.ldv + (int64_t)p.kh * D;
@@ -385,16 +389,15 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   float m[NG], l[NG];
   int lim[NG], common = 0, first = 0;  // first unit of this worker's part of the item
   bool uneven = false;                 // whether some rows see more keys than others
-  auto enter = [&](const Place& p, const Seq& s) {  // an item: its queries
-    const int nrows = s.lq * P.group, past = s.lk - s.lq + 1;
-    auto seen = [&](int row) { return CAUSAL ? max(past + row / P.group, 0) : s.lk; };
-    common = seen(p.tile * R);
-    uneven = common != seen(min(p.tile * R + R, nrows) - 1);
+  auto enter = [&](const Place& p, const Seq& s, int keys) {  // an item: its queries
+    const int nrows = s.lq * P.group;
+    common = seen(s, p.tile * R);
+    uneven = common != keys;
     first = p.unit;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       const int row = min(p.tile * R + 16 * g + lr, nrows - 1), qi = row / P.group, h = p.kh * P.group + row - qi * P.group;
-      lim[g] = seen(row);
+      lim[g] = seen(s, row);
       const bf16_t* qp = P.q + (int64_t)(s.q0 + qi) * P.ldq + (int64_t)h * D + 8 * lq;
 #pragma unroll
       for (int t = 0; t < 4; ++t) qf[g][t] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(qp + 32 * t));
@@ -439,9 +442,9 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   Place cur = line.at(begin);
   if (cur.z < 0) return;
   Seq seq = seq_of(P, cur.z);
-  int late = 0;
-  issue(cur, seq, true, 0);
-  enter(cur, seq);
+  int late = 0, keys = seen_by(cur, seq);
+  issue(cur, seq, keys, 0);
+  enter(cur, seq, keys);
   int st = 0;
   for (int64_t u = begin; u < end; ++u) {
     Place nxt = cur;
@@ -451,13 +454,16 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
     if (change) {
       nxt = line.at(u + 1);
       if (nxt.z < 0) more = false;
-      else nseq = seq_of(P, nxt.z);
+      else {
+        nseq = seq_of(P, nxt.z);
+        keys = seen_by(nxt, nseq);
+      }
     } else {
       ++nxt.unit;
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the other buffer is read
     asm volatile("" ::: "memory");
-    issue(nxt, nseq, more, st ^ 1);
+    issue(nxt, nseq, more ? keys : 0, st ^ 1);
     wait_vmcnt<16>();  // this one has landed
     asm volatile("" ::: "memory");
     const char* sk = smem + (2 * wave + st) * STAGE;
@@ -517,7 +523,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
       l[g] += sum;
     }
     auto v_frag = [&](int dt) { return vt_frag(sk + TILE + (voff ^ (dt << 5))); };
-    // 0 times a value that is not finite would reach the rows that do not see its key
+    // 0 times a value that is not finite would reach the rows that do not see its key, where others of the tile do
     bool spoilt = false;
     if (CAUSAL && masked && uneven) {
 #pragma unroll
@@ -565,7 +571,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
     if (change || !more) {
       leave(cur, seq, late);
       late = 1;
-      if (more) enter(nxt, nseq);
+      if (more) enter(nxt, nseq, keys);
     }
     if (!more) break;
     cur = nxt;

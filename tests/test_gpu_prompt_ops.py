@@ -630,6 +630,42 @@ def clear(vb, kb, koff, at):
         kb[koff[z] + j] = 0
 
 
+# few rows a sequence: tiles of one query's heads (16 and 32 of them), of queries without a key, of both kinds in shares
+UNSEEN = [([2, 1] + [0] * 5, [40] * 7, 16, 1), ([2] + [0] * 5, [70, 5, 0, 9, 9, 9], 32, 1),
+          ([3, 1] + [0] * 6, [9000, 200] + [0] * 6, 16, 1), ([2, 1, 1, 0, 0, 0, 0, 0], [5000, 33, 700, 0, 1, 2, 3, 4], 32, 2),
+          ([20, 1, 1, 1], [4, 9, 9, 9], 1, 1), ([70, 1, 2], [30, 9, 3], 1, 1), ([40] + [1] * 30, [3000] + [1] * 30, 2, 2),
+          ([5, 1, 0], [64, 32, 33], 8, 1)]
+
+
+@pytest.mark.parametrize("slots", [False, True])
+@pytest.mark.parametrize("ql,kl,heads,kv_heads", UNSEEN)
+def test_values_that_no_row_of_a_tile_sees(ql, kl, heads, kv_heads, slots):
+    """Infinities and NaN in the last key, which a sequence's last query alone sees: every other row, whatever tile it
+    shares, is as if that key were zeros, and zeros where it sees no key."""
+    torch = torch_cuda()
+    assert (sum(ql) + 4) * (heads // kv_heads) <= 32 * len(ql)  # (the few-row kernels; `packed` adds four rows)
+    kw = dict(slots=max(kl) + 3 if slots else None, exact_rows=False)
+    last = np.cumsum(ql)[[n > 0 for n in ql]] - 1
+    rest = np.setdiff1d(np.arange(sum(ql)), last)
+    keyless = np.concatenate([np.arange(n) + m - n < 0 for n, m in zip(ql, kl)])
+
+    def put(value, key):
+        def change(qb, kb, vb, qoff, koff):
+            for z, m in enumerate(kl):
+                if m:
+                    vb[koff[z] + m - 1, 5::128] = value
+                    if key:
+                        kb[koff[z] + m - 1] = value
+        return change
+    _, y, d = packed(torch, ql, kl, heads, kv_heads, change=put(0, True), **kw)
+    for bad in (0x7FC0, 0x7F80, 0xFF80):
+        got = packed(torch, ql, kl, heads, kv_heads, change=put(bad, bad == 0x7FC0), **kw)[0]
+        assert (np.abs(got[rest] - y[rest]) <= d[rest] + BF16 * (np.abs(y[rest]) + d[rest])).all()
+        assert (got[keyless] == 0).all()
+        sees = last[~keyless[last]]
+        assert (~np.isfinite(got[sees][:, 5::128])).all()
+
+
 def test_packed_attention_rising_and_overflowing_logits():
     """Logits that rise along the keys, so that the running maximum moves in every tile; logits that overflow to
     infinities of either sign."""
