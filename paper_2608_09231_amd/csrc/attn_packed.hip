@@ -164,15 +164,27 @@ __device__ __forceinline__ bf16x8_t vt_frag(const char* p) {
 #endif
 }
 
-__device__ __forceinline__ bool not_finite(const bf16x8_t& f) {
-  const uint4 u = __builtin_bit_cast(uint4, f);
-  bool bad = false;
+typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
+
+// Values for a careful product: finite ones as they are, and flags in place of the others, +inf 1, -inf 128 and
+// NaN 16384, so that their product with whether a row sees the key (a tile has at most 64) counts each kind.
+__device__ __forceinline__ void part_odd(const bf16x8_t& v, bf16x8_t& clean, bf16x8_t& flag) {
+  const u16x8_t bits = __builtin_bit_cast(u16x8_t, v);
+  u16x8_t c, f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
-    bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+  for (int e = 0; e < 8; ++e) {
+    const bool odd = (bits[e] & 0x7f80) == 0x7f80;
+    c[e] = odd ? 0 : bits[e];
+    f[e] = !odd ? 0 : bits[e] == 0x7f80 ? 0x3f80 : bits[e] == 0xff80 ? 0x4300 : 0x4680;
   }
-  return bad;
+  clean = __builtin_bit_cast(bf16x8_t, c);
+  flag = __builtin_bit_cast(bf16x8_t, f);
+}
+// What the counted values add to a sum.
+__device__ __forceinline__ float odd_sum(float count) {
+  const int c = (int)count;
+  const float up = c & 127 ? INFINITY : 0.f, down = c & 0x3f80 ? -INFINITY : 0.f;
+  return (up + down) + (c >> 14 ? __uint_as_float(0x7fc00000u) : 0.f);
 }
 
 // A launch's work as one line of units: sequence by sequence, tile of R rows by tile and key head
@@ -343,6 +355,9 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows
 // and V from memory.  Every wave is a worker with units of 32 keys in two buffers
 // of LDS of its own, and no wave waits for another.  With MFMAs to spare, probabilities
 // enter the second product as two bf16 parts, so that only the output is rounded to 8 bits.
+// An infinity among the values meets a second part of zero or of the other sign, and one that a row does not see a
+// probability of zero: both give NaN. So where an item's sums are not finite, the wave goes through its units
+// again, and adds what is not finite by product of flags.
 // 16 tokens against up to 8192 keys each, 32 heads on 8: 46 us for 263 MB, 5.7 TB/s, and 5 for joining.
 template <bool BOUNDED, bool CAUSAL, int NG>
 __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
@@ -388,11 +403,9 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   f32x4_t acc[8][NG];
   float m[NG], l[NG];
   int lim[NG], common = 0, first = 0;  // first unit of this worker's part of the item
-  bool uneven = false;                 // whether some rows see more keys than others
-  auto enter = [&](const Place& p, const Seq& s, int keys) {  // an item: its queries
+  auto enter = [&](const Place& p, const Seq& s) {  // an item: its queries
     const int nrows = s.lq * P.group;
     common = seen(s, p.tile * R);
-    uneven = common != keys;
     first = p.unit;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -410,6 +423,80 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
     for (int g = 0; g < NG; ++g)  // (queries waited for later would wait for the copies, too)
 #pragma unroll
       for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(qf[g][t]));
+  };
+  // logits of the keys from `key` on; -inf where a row does not see them
+  auto scores = [&](const char* sk, int key, f32x4_t(&s)[2][NG]) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t] + b * 16 * 256));
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+          s[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t], t ? s[b][g] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+    if (key + HK > common) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            if (key + 16 * b + 4 * lq + r >= lim[g]) s[b][g][r] = -INFINITY;
+    }
+  };
+  // probabilities of a query group, bf16 and what it leaves; their sum
+  auto weights = [&](const f32x4_t(&s)[2][NG], int g, bf16x8_t& ph, bf16x8_t& pl) {
+    const float mneg = BOUNDED ? -BOUNDED_SHIFT_LOG2 : neg_shift(m[g]);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][g][e & 3], P.scale_log2, mneg));
+      ph[e] = (__bf16)p;
+      pl[e] = (__bf16)(p - (float)ph[e]);
+      sum += p;
+    }
+    return sum;
+  };
+  // An item's sums anew, unit by unit through the buffer of the last one, with the maxima that are known by now.
+  auto again = [&](Place p, const Seq& s, int st) {
+    const int keys = seen_by(p, s), last = p.unit;
+    const char* sk = smem + (2 * wave + st) * STAGE;
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[dt][g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (p.unit = first; p.unit <= last; ++p.unit) {
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the buffer is read
+      asm volatile("" ::: "memory");
+      issue(p, s, keys, st);
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+      const int key = p.unit * HK;
+      f32x4_t t[2][NG];
+      scores(sk, key, t);
+      bf16x8_t ph[NG], pl[NG], sees[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        weights(t, g, ph[g], pl[g]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sees[g][e] = key + 16 * (e >> 2) + 4 * lq + (e & 3) < lim[g] ? (__bf16)1.f : (__bf16)0.f;
+      }
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        bf16x8_t clean, flag;
+        part_odd(vt_frag(sk + TILE + (voff ^ (dt << 5))), clean, flag);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(clean, ph[g], acc[dt][g], 0, 0, 0);
+          acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(clean, pl[g], acc[dt][g], 0, 0, 0);
+          const f32x4_t n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(flag, sees[g], f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[dt][g][r] += odd_sum(n[r]);
+        }
+      }
+    }
   };
   auto leave = [&](const Place& p, const Seq& s, int late) {
     const int nrows = s.lq * P.group;
@@ -444,7 +531,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
   Seq seq = seq_of(P, cur.z);
   int late = 0, keys = seen_by(cur, seq);
   issue(cur, seq, keys, 0);
-  enter(cur, seq, keys);
+  enter(cur, seq);
   int st = 0;
   for (int64_t u = begin; u < end; ++u) {
     Place nxt = cur;
@@ -467,28 +554,9 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
     wait_vmcnt<16>();  // this one has landed
     asm volatile("" ::: "memory");
     const char* sk = smem + (2 * wave + st) * STAGE;
-    const int key = cur.unit * HK;
     f32x4_t s[2][NG];
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, *(const uint4*)(sk + koff[t] + b * 16 * 256));
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-          s[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][t], t ? s[b][g] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-      }
-    const bool masked = key + HK > common;
-    if (masked) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int g = 0; g < NG; ++g)
-            if (key + 16 * b + 4 * lq + r >= lim[g]) s[b][g][r] = -INFINITY;
-    }
-    bf16x8_t ph[NG], pl[NG];  // probabilities: bf16 and what it leaves
+    scores(sk, cur.unit * HK, s);
+    bf16x8_t ph[NG], pl[NG];
     if constexpr (!BOUNDED) settle(s);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -511,67 +579,29 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
           m[g] = mn;
         }
       }
-      const float mneg = BOUNDED ? -BOUNDED_SHIFT_LOG2 : neg_shift(m[g]);
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][g][e & 3], P.scale_log2, mneg));
-        ph[g][e] = (__bf16)p;
-        pl[g][e] = (__bf16)(p - (float)ph[g][e]);
-        sum += p;
-      }
-      l[g] += sum;
+      l[g] += weights(s, g, ph[g], pl[g]);
     }
-    auto v_frag = [&](int dt) { return vt_frag(sk + TILE + (voff ^ (dt << 5))); };
-    // 0 times a value that is not finite would reach the rows that do not see its key, where others of the tile do
-    bool spoilt = false;
-    if (CAUSAL && masked && uneven) {
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) spoilt |= not_finite(v_frag(dt));
-      spoilt = __builtin_amdgcn_ballot_w64(spoilt) != 0;
-    }
-    if (!CAUSAL || !spoilt) {
+    for (int dt = 0; dt < 8; ++dt) {
+      const bf16x8_t vf = vt_frag(sk + TILE + (voff ^ (dt << 5)));
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        const bf16x8_t vf = v_frag(dt);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[g], acc[dt][g], 0, 0, 0);
-          acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[g], acc[dt][g], 0, 0, 0);
-        }
-      }
-    } else {
-      // key by key: a lane keeps the product only if its row sees the key
-#pragma unroll 1
-      for (int j = 0; j < HK; ++j) {
-        const bool mine = ((j >> 2) & 3) == lq;
-        const int e0 = 4 * (j >> 4) + (j & 3);
-        bf16x8_t hj[NG], lj[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            hj[g][e] = mine && e == e0 ? ph[g][e] : (__bf16)0.f;
-            lj[g][e] = mine && e == e0 ? pl[g][e] : (__bf16)0.f;
-          }
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          bf16x8_t vj = v_frag(dt);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) vj[e] = mine && e == e0 ? vj[e] : (__bf16)0.f;
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            f32x4_t y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vj, hj[g], acc[dt][g], 0, 0, 0);
-            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vj, lj[g], y, 0, 0, 0);
-            if (key + j < lim[g]) acc[dt][g] = y;
-          }
-        }
+      for (int g = 0; g < NG; ++g) {
+        acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[g], acc[dt][g], 0, 0, 0);
+        acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[g], acc[dt][g], 0, 0, 0);
       }
     }
     if (change || !more) {
+      float zero = 0.f;  // NaN where a sum is not finite
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(acc[dt][g][r], 0.f, zero);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(zero != 0.f) != 0, 0)) again(cur, seq, st);
       leave(cur, seq, late);
       late = 1;
-      if (more) enter(nxt, nseq, keys);
+      if (more) enter(nxt, nseq);
     }
     if (!more) break;
     cur = nxt;
@@ -583,7 +613,6 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
 }
 
 constexpr int ROWS = 128;
-typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
 
 // Tile of rank t among the tiles of a key head in the order of their keys, most first, so that
 // a launch ends with short ones: up to 64 sequences, one a lane; false past the last tile.
@@ -992,8 +1021,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
             for (int g = 0; g < 2; ++g) acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[ks][g], acc[dt][g], 0, 0, 0);
           }
       } else {
-        // finite values as ever; of the others the rows that see their keys are told by a product
-        // of flags: +inf counts 1, -inf 128 and NaN 16384 (a tile has 64 keys), times whether the row sees the key
+        // finite values as ever; of the others the rows that see their keys are told by a product of flags
         bf16x8_t sees[2][2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
@@ -1007,29 +1035,18 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
           f32x4_t n[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks) {
-            const u16x8_t bits = __builtin_bit_cast(u16x8_t, v_frag(dt, ks));
-            u16x8_t clean, flag;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool odd = (bits[e] & 0x7f80) == 0x7f80;
-              clean[e] = odd ? 0 : bits[e];
-              flag[e] = !odd ? 0 : bits[e] == 0x7f80 ? 0x3f80 : bits[e] == 0xff80 ? 0x4300 : 0x4680;
-            }
+            bf16x8_t clean, flag;
+            part_odd(v_frag(dt, ks), clean, flag);
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-              acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, clean), pf[ks][g], acc[dt][g], 0, 0, 0);
-              n[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, flag), sees[ks][g], n[g], 0, 0, 0);
+              acc[dt][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(clean, pf[ks][g], acc[dt][g], 0, 0, 0);
+              n[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(flag, sees[ks][g], n[g], 0, 0, 0);
             }
           }
 #pragma unroll
           for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int c = (int)n[g][r];
-              const float up = c & 127 ? INFINITY : 0.f, down = c & 0x3f80 ? -INFINITY : 0.f;
-              const float nan = c >> 14 ? __uint_as_float(0x7fc00000u) : 0.f;
-              acc[dt][g][r] += (up + down) + nan;
-            }
+            for (int r = 0; r < 4; ++r) acc[dt][g][r] += odd_sum(n[g][r]);
         }
       }
     }

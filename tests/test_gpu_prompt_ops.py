@@ -666,6 +666,45 @@ def test_values_that_no_row_of_a_tile_sees(ql, kl, heads, kv_heads, slots):
         assert (~np.isfinite(got[sees][:, 5::128])).all()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("bounded", [False, True])
+@pytest.mark.parametrize("ql,kl,heads,kv_heads", [
+    ([1] * 5, [700, 1, 33, 64, 0], 4, 2), ([3] + [0] * 6, [9000] + [5] * 6, 8, 4), ([9, 2], [40, 300], 2, 2),   # few rows
+    ([2, 1, 0, 0, 0], [3000, 40, 0, 0, 0], 32, 2), ([90], [100], 3, 1), ([300], [6000], 2, 2), ([1100], [1100], 16, 16)])
+def test_infinite_values_that_a_query_sees(ql, kl, heads, kv_heads, bounded, causal):
+    """An infinite value times a probability above zero: infinities of its sign, NaN where both signs meet or a NaN is
+    seen, and every other column and row as ever."""
+    torch = torch_cuda()
+    kw = dict(causal=causal, bounded=bounded, exact_rows=False)
+    cols = {3: (0x7F80, None), 40: (None, 0xFF80), 77: (0x7F80, 0xFF80), 100: (0xFF80, 0x7FC0), 127: (None, 0x7F80)}
+    first = [m // 3 for m in kl]                    # a key that some see, and the last one
+    at = {}
+
+    def put(spoil):
+        def change(qb, kb, vb, qoff, koff):
+            for z, m in enumerate(kl):
+                for c, bad in cols.items():
+                    for key, b in zip((first[z], m - 1), bad):
+                        if b is not None and m:
+                            vb[koff[z] + key, c::128] = b if spoil else 0
+            at["vb"], at["koff"] = vb.copy(), koff
+        return change
+    _, y, d = packed(torch, ql, kl, heads, kv_heads, change=put(False), **kw)
+    got = packed(torch, ql, kl, heads, kv_heads, change=put(True), **kw)[0]
+    v = bits_to_f64(at["vb"])
+    want = np.zeros_like(y)                         # what is not finite adds up as it is
+    for z, (n, m) in enumerate(zip(ql, kl)):
+        for i in range(n):
+            see = min(m, max(0, m - n + 1 + i)) if causal else m
+            t = v[at["koff"][z]:at["koff"][z] + see]
+            with np.errstate(invalid="ignore"):
+                t = np.where(np.isfinite(t), 0, t).sum(0).reshape(kv_heads, 1, 128)
+            want[sum(ql[:z]) + i] = np.broadcast_to(t, (kv_heads, heads // kv_heads, 128)).reshape(-1)
+    fine = want == 0
+    assert (np.abs(got - y) <= d + BF16 * (np.abs(y) + d))[fine].all()
+    np.testing.assert_array_equal(got[~fine], want[~fine])
+
+
 def test_packed_attention_rising_and_overflowing_logits():
     """Logits that rise along the keys, so that the running maximum moves in every tile; logits that overflow to
     infinities of either sign."""
