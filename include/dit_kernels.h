@@ -372,7 +372,8 @@ enum {
  * o, its keys rows koff[z] .. koff[z + 1] - 1 of k and v, or the first klen[z] of
  * these (a cache whose slots are filled so far).  Query head h reads key head h /
  * (heads / kv_heads).  The offsets are read on the device and clamped there: to [0, Tq] and [0,
- * Tk], and not to fall from one to the next; klen to the slot. */
+ * Tk], and not to fall (an offset below an earlier one counts as that one, so that no two sequences
+ * share a row); klen to the slot. */
 typedef struct dit_packed_shape {
   int32_t batch;            /* sequences */
   int32_t Tq, Tk;           /* rows of q and o, rows of k and v */

@@ -32,34 +32,61 @@ struct PackedArgs {
   float scale_log2;
 };
 
-// A sequence: its first rows and lengths, clamped to what the caller's matrices hold.
+// Sum or maximum (of what is not negative) of v over the lanes up to this one, on the VALU (rows of 16 lanes, then
+// their last lanes' to the rows behind).
+template <typename F>
+__device__ __forceinline__ int over_lanes(int v, F op) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));  // 1, 2, 4 and 8 lanes before, in a row
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));  // lane 15 of a row to the next, 31 to the upper half
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+#endif
+  return v;
+}
+__device__ __forceinline__ int scan_lanes(int v) {
+  return over_lanes(v, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ int max_scan_lanes(int v) {
+  return over_lanes(v, [](int a, int b) { return max(a, b); });
+}
+
+// A sequence: its first rows and lengths.
 struct Seq {
   int q0, lq, k0, lk;
 };
 __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return min(max(x, lo), hi); }
-__device__ __forceinline__ Seq seq_of(const PackedArgs& P, int z) {
+__device__ __forceinline__ Seq seq_of_lane(const Seq& s, int l) {
+  return Seq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.lq, l), __builtin_amdgcn_readlane(s.k0, l),
+             __builtin_amdgcn_readlane(s.lk, l)};
+}
+// 64 sequences at a time, one a lane (past the last one: empty).  Offsets are clamped to what the caller's
+// matrices hold, and one below an earlier one counts as that one, so that no two sequences share a row: their tiles
+// are no more than the host counts, and no two work-groups write the same.  qat, kat: the largest offsets before.
+struct Seqs {
   Seq s;
-  s.q0 = clamp_to(P.qoff[z], 0, P.Tq);
-  s.lq = clamp_to(P.qoff[z + 1], s.q0, P.Tq) - s.q0;
-  s.k0 = clamp_to(P.koff[z], 0, P.Tk);
-  s.lk = clamp_to(P.koff[z + 1], s.k0, P.Tk) - s.k0;
-  if (P.klen) s.lk = clamp_to(P.klen[z], 0, s.lk);
-  return s;
-}
+  int qat = 0, kat = 0;
+  __device__ __forceinline__ void load(const PackedArgs& P, int z0) {
+    const int z = z0 + (threadIdx.x & 63);
+    int q0 = 0, q1 = 0, k0 = 0, k1 = 0, n = 0;
+    if (z < P.batch) {
+      q0 = clamp_to(P.qoff[z], 0, P.Tq); q1 = clamp_to(P.qoff[z + 1], 0, P.Tq);
+      k0 = clamp_to(P.koff[z], 0, P.Tk); k1 = clamp_to(P.koff[z + 1], 0, P.Tk);
+      n = P.klen ? P.klen[z] : 0x7fffffff;
+    }
+    // (200 tokens of 500 keys each 31.0 us, 32.1 with the scans in every call)
+    if (__builtin_amdgcn_ballot_w64(z < P.batch && (q0 > q1 || k0 > k1 || q0 < qat || k0 < kat))) {
+      q0 = max(max_scan_lanes(q0), qat);
+      k0 = max(max_scan_lanes(k0), kat);
+    }
+    s = Seq{q0, max(q1 - q0, 0), k0, clamp_to(n, 0, max(k1 - k0, 0))};
+    qat = __builtin_amdgcn_readlane(s.q0, 63);
+    kat = __builtin_amdgcn_readlane(s.k0, 63);
+  }
+};
 
-// Sum of v over the lanes up to this one, on the VALU (rows of 16 lanes, then their
-// last lanes' sums to the rows behind).
-__device__ __forceinline__ int scan_lanes(int v) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // 1, 2, 4 and 8 lanes before, in a row
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next, 31 to the upper half
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-#endif
-  return v;
-}
 // The same of 64-bit values, halves moved alike.
 template <int CTRL, int ROW_MASK>
 __device__ __forceinline__ int64_t lanes_before(int64_t v) {
@@ -80,18 +107,14 @@ __device__ __forceinline__ int64_t scan_lanes64(int64_t v) {
   return v + lanes_before<0x143, 0xc>(v);
 }
 __device__ __forceinline__ int sum_lanes(int v) { return __builtin_amdgcn_readlane(scan_lanes(v), 63); }
-__device__ __forceinline__ Seq seq_of_lane(const Seq& s, int l) {
-  return Seq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.lq, l), __builtin_amdgcn_readlane(s.k0, l),
-             __builtin_amdgcn_readlane(s.lk, l)};
-}
 
 // The sequence that tile t of `rows` rows falls in, 64 sequences at a time, and the
 // tile's number in it, its last one first; false past the last one.
 __device__ __forceinline__ bool find_tile(const PackedArgs& P, int t, int rows, Seq& seq, int& tile) {
-  const int lane = threadIdx.x & 63;
+  Seqs all;
   for (int z0 = 0; z0 < P.batch; z0 += 64) {
-    Seq s{0, 0, 0, 0};
-    if (z0 + lane < P.batch) s = seq_of(P, z0 + lane);
+    all.load(P, z0);
+    const Seq& s = all.s;
     const int n = (s.lq * P.group + rows - 1) / rows;
     const int end = scan_lanes(n);
     const uint64_t past = __ballot(end > t);
@@ -203,7 +226,8 @@ __device__ __forceinline__ int64_t readlane64(int64_t v, int l) {
 template <int R, int KEYS>
 struct Line {
   const PackedArgs& P;
-  int z0, n;                  // 64 sequences from z0 on, one a lane: units of an item,
+  Seqs all;                   // 64 sequences from z0 on, one a lane:
+  int z0, n;                  // units of an item,
   int64_t items, cost;        // items and units of the sequence,
   int64_t items_end, cost_end;  // and up to its end from z0 on
   int64_t items_base, cost_base;  // those before z0
@@ -211,9 +235,8 @@ struct Line {
   __device__ __forceinline__ explicit Line(const PackedArgs& P_) : P(P_), items_base(0), cost_base(0) { load(0); }
   __device__ __forceinline__ void load(int z) {
     z0 = z;
-    const int lane = threadIdx.x & 63;
-    Seq s{0, 0, 0, 0};
-    if (z0 + lane < P.batch) s = seq_of(P, z0 + lane);
+    all.load(P, z0);
+    const Seq& s = all.s;
     n = max(1, (s.lk + KEYS - 1) / KEYS);
     items = (int64_t)((s.lq * P.group + R - 1) / R) * P.kv_heads;
     cost = items * n;
@@ -231,6 +254,8 @@ struct Line {
     while (l.z0 + 64 < P.batch) l.next();
     return l.cost_base + readlane64(l.cost_end, 63);
   }
+  // The sequence of the place that was asked for last.
+  __device__ __forceinline__ Seq seq(const Place& p) const { return seq_of_lane(all.s, p.z - z0); }
   // Place of unit u (below the total, not before the last one asked for).  Offsets that
   // change under a running call may find none: then a place of no rows.
   __device__ __forceinline__ Place at(int64_t u) {
@@ -278,12 +303,12 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows
     line.next();
   }
   const int l = __ffsll((unsigned long long)__ballot(line.items_base + line.items_end > item)) - 1;
-  const int z = line.z0 + l, n = __builtin_amdgcn_readlane(line.n, l);
+  const int n = __builtin_amdgcn_readlane(line.n, l);
   const int64_t i = item - line.items_base - (readlane64(line.items_end, l) - readlane64(line.items, l));
   const int64_t a = line.cost_base + readlane64(line.cost_end, l) - readlane64(line.cost, l) + i * n;
   const int64_t w0 = a / per, w1 = (a + n - 1) / per;  // the item's workers
   if (w0 == w1) return;  // one worker has stored it
-  const Seq s = seq_of(P, z);
+  const Seq s = seq_of_lane(line.all.s, l);
   const int tile = (int)(i / P.kv_heads), kh = (int)(i - (int64_t)tile * P.kv_heads);
   const int parts = (int)(w1 - w0) + 1, each = (parts + PG - 1) / PG;
   const int64_t pf = part_floats(R);
@@ -528,7 +553,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
 
   Place cur = line.at(begin);
   if (cur.z < 0) return;
-  Seq seq = seq_of(P, cur.z);
+  Seq seq = line.seq(cur);
   int late = 0, keys = seen_by(cur, seq);
   issue(cur, seq, keys, 0);
   enter(cur, seq);
@@ -542,7 +567,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
       nxt = line.at(u + 1);
       if (nxt.z < 0) more = false;
       else {
-        nseq = seq_of(P, nxt.z);
+        nseq = line.seq(nxt);
         keys = seen_by(nxt, nseq);
       }
     } else {
@@ -619,9 +644,9 @@ constexpr int ROWS = 128;
 // Of a sequence with T tiles those from first(c) on have c key blocks of 64 or more.
 template <bool CAUSAL>
 __device__ __forceinline__ bool ranked_tile(const PackedArgs& P, int t, Seq& seq, int& tile) {
-  const int lane = threadIdx.x & 63;
-  Seq s{0, 0, 0, 0};
-  if (lane < P.batch) s = seq_of(P, lane);
+  Seqs all;
+  all.load(P, 0);
+  const Seq& s = all.s;
   const int T = (s.lq * P.group + ROWS - 1) / ROWS, past = s.lk - s.lq + 1;
   const int top = (s.lk + KT - 1) / KT;  // key blocks of the last tile
   auto first = [&](int c) {
@@ -700,7 +725,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
     Line<ROWS, KT> line(P);  // (anew for each item: few, and the registers are the loop's)
     p = line.at(u);
     if (p.z < 0) return;
-    s_ = seq_of(P, p.z);
+    s_ = line.seq(p);
   }
   const int tile = p.tile, kh = p.kh;
   const int nrows = s_.lq * P.group;

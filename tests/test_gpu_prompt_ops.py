@@ -743,6 +743,42 @@ def test_offsets_are_clamped():
         assert (np.abs(got - y) <= d + BF16 * (np.abs(y) + d)).all()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,batch,Tq,Tk,heads,kv_heads", [
+    ("few", 9, 60, 2000, 4, 2), ("few", 140, 200, 900, 2, 2), ("shared", 3, 500, 9000, 2, 1), ("shared", 70, 2300, 100000, 1, 1),
+    ("whole", 20, 6000, 2500, 8, 2), ("whole", 100, 9000, 7000, 4, 2), ("whole", 1, 300, 300, 8, 8)])
+def test_offsets_that_fall(kind, batch, Tq, Tk, heads, kv_heads, causal):
+    """An offset below an earlier one counts as that one: sequences share no row, and each row's result is one
+    sequence's, also where the earlier one lies more than 64 sequences before."""
+    torch = torch_cuda()
+    r = rng(13, batch, Tq)
+    rows = Tq * (heads // kv_heads)
+    assert (rows <= 32 * batch) == (kind == "few")
+    nbytes = binding.attention_packed_ws_bytes(batch=batch, Tq=Tq, Tk=Tk, heads=heads, kv_heads=kv_heads)
+    assert (nbytes > 0) == (kind != "whole")
+    q, k, v = (dev(torch, bf16_bits(r.standard_normal((t, h * 128)))) for t, h in ((Tq, heads), (Tk, kv_heads), (Tk, kv_heads)))
+
+    def falling(top):
+        """Offsets that grow to `top`, every third one thrown anywhere or far outside."""
+        at = np.sort(r.integers(0, top + 1, batch + 1))
+        at[::3] = r.integers(-top, 2 * top, at[::3].size)
+        if batch > 1:
+            at[batch // 2] = -2 ** 31
+        return at.astype(np.int32)
+    for qoff, koff in ((falling(Tq), falling(Tk)), (np.resize([0, Tq], batch + 1), np.resize([0, Tk], batch + 1)),
+                       (np.resize([0, Tq // 2, Tq // 4, Tq], batch + 1), np.resize([0, Tk // 3, Tk, 0, Tk // 2], batch + 1))):
+        o = torch.full((Tq, heads * 128), FILL, dtype=torch.int16, device="cuda")
+        binding.attention_packed_bf16(q, k, v, o, qoff=dev(torch, qoff.astype(np.int32)), koff=dev(torch, koff.astype(np.int32)),
+                                      heads=heads, kv_heads=kv_heads, flags=binding.ATTN_CAUSAL if causal else 0)
+        qm, km = (np.maximum.accumulate(np.clip(a.astype(np.int64), 0, t)) for a, t in ((qoff, Tq), (koff, Tk)))
+        y, d = ref.attend(*(host_bf16(t) for t in (q, k, v)), qoff=qm, koff=km, heads=heads, kv_heads=kv_heads, causal=causal)
+        raw, got = o.cpu().numpy(), host_bf16(o)
+        own = np.arange(Tq)[(np.arange(Tq) >= qm[0]) & (np.arange(Tq) < qm[-1])]
+        rest = np.setdiff1d(np.arange(Tq), own)
+        assert (np.abs(got[own] - y[own]) <= d[own] + BF16 * (np.abs(y[own]) + d[own])).all()
+        assert (raw[rest] == FILL).all()
+
+
 def test_no_sequences_queries_or_keys():
     torch = torch_cuda()
     t = torch.ones(8, 256, dtype=torch.int16, device="cuda")
