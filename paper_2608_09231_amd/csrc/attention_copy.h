@@ -12,7 +12,7 @@ namespace {
 // would have every transposing read of LDS wait for all copies in flight.  The
 // kernel's own waits and barriers order them.  (No registers come back; the
 // address escapes, so that the barriers' memory clobbers cover what is written.  m0 is
-// a reserved register, set before each use: the compiler refuses it among the clobbers.)
+// a reserved register, set before each use: clang warns against it among the clobbers.)
 __device__ __forceinline__ void copy16_unseen(const void* base, uint32_t bytes, const void* dst, uint32_t off) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -705,6 +705,24 @@ def test_infinite_values_that_a_query_sees(ql, kl, heads, kv_heads, bounded, cau
     np.testing.assert_array_equal(got[~fine], want[~fine])
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,batch,queries,keys,heads,kv_heads", [
+    ("whole", 65, 100, 130, 2, 1), ("whole", 130, 70, 60, 4, 2), ("whole", 200, 45, 90, 1, 1), ("shared", 70, 50, 1300, 1, 1),
+    ("shared", 130, 45, 1700, 1, 1)])
+def test_many_sequences_of_many_rows(kind, batch, queries, keys, heads, kv_heads, causal):
+    """More than 64 sequences in tiles of 128 rows, whole and shared out: lengths around the averages, every fifth
+    sequence without queries and every seventh without keys, but for the 64th and the 65th."""
+    torch = torch_cuda()
+    r = rng(31, batch)
+    ql, kl = (r.integers(n // 2, n + n // 2 + 1, batch) for n in (queries, keys))
+    ql[::5], kl[::7] = 0, 0
+    ql[63:65], kl[63:65] = queries, keys
+    rows, Tk = (int(ql.sum()) + 4) * (heads // kv_heads), int(kl.sum()) + 4
+    nbytes = binding.attention_packed_ws_bytes(batch=batch, Tq=int(ql.sum()) + 4, Tk=Tk, heads=heads, kv_heads=kv_heads)
+    assert rows > 32 * batch and (nbytes > 0) == (kind == "shared")
+    packed(torch, list(map(int, ql)), list(map(int, kl)), heads, kv_heads, causal=causal, bounded=batch == 130)
+
+
 def test_packed_attention_rising_and_overflowing_logits():
     """Logits that rise along the keys, so that the running maximum moves in every tile; logits that overflow to
     infinities of either sign."""
