@@ -773,7 +773,7 @@ __global__ __launch_bounds__(BM == 192 ? 512 : 256, 2) void gemm_fp4_tile_kernel
 }
 
 // Few rows or few tiles: 16 RB x NT outputs per work-group, eight waves of 16 RB x 32
-// that share K (NT = 32: eight ways, 64: four, 128: two).  Each wave copies its own
+// that share K (NT = 32: eight ways, 64: four, 128, of 16 rows alone: two).  Each wave copies its own
 // rows' slices and their scales to a ring of its own in LDS, so that no wave waits for another until
 // their sums meet at the end; the copies read whole 128-byte lines, eight lanes
 // each.  Bound by the way of W from memory: 1 x 13824 x 5120 9.6 us, 3.9 TB/s.
@@ -994,11 +994,11 @@ hipError_t launch_gemm_fp4(const GemmFp4Args& g, hipStream_t s, int n_cu) {
   int nt = g.rms_cols > 0 ? 128 : 32;
   while (nt < widest && tiles(rows, nt) > n_cu) nt *= 2;
   if (nt <= widest && tiles(rows, nt) <= n_cu) {
-#define DIT_SMALL(RB, K)                                                                                     \
-  go(nt == 128 ? gemm_fp4_small_kernel<128, RB, K> : nt == 64 ? gemm_fp4_small_kernel<64, RB, K>             \
-                                                              : gemm_fp4_small_kernel<32, RB, K>, rows, nt, 512)
-    if (fp4) return one ? DIT_SMALL(1, EPI_K_FP4) : DIT_SMALL(2, EPI_K_FP4);
-    return one ? DIT_SMALL(1, EPI_K_ANY) : DIT_SMALL(2, EPI_K_ANY);
+#define DIT_SMALL(K)                                                                                         \
+  go(!one ? (nt == 64 ? gemm_fp4_small_kernel<64, 2, K> : gemm_fp4_small_kernel<32, 2, K>)                   \
+          : nt == 128 ? gemm_fp4_small_kernel<128, 1, K>                                                     \
+                      : nt == 64 ? gemm_fp4_small_kernel<64, 1, K> : gemm_fp4_small_kernel<32, 1, K>, rows, nt, 512)
+    return fp4 ? DIT_SMALL(EPI_K_FP4) : DIT_SMALL(EPI_K_ANY);
 #undef DIT_SMALL
   }
   // Rounds of the chip times a tile's time, which is some us and some per slice of 256 of K, fewer in a round

@@ -213,7 +213,7 @@ hipError_t launch_rotary(const dit_rotary_desc& d, hipStream_t s) {
     P.end[a] = a < d.axes ? end : 0x7fffffff;
   }
   // (pairs of the last axis end at rot / 2; no pair lies past it)
-  // Rows of a work-group: enough pairs for its 256 threads, at most 16384 of them in LDS.
+  // Rows of a work-group: as many as have a pair for each of its 256 threads, which take 2 KB of LDS.
   const int pairs = std::max(1, d.rot / 2);
   P.rows_wg = std::max(1, 256 / pairs);
   // (a work-group's chunks fit 32 bits: width <= 2^30, and more rows only of narrow heads)
