@@ -384,7 +384,8 @@ typedef struct dit_packed_shape {
 } dit_packed_shape;
 
 /* o = softmax(q k^T / sqrt(128)) v within each sequence, head_dim 128, bf16; f32
- * softmax and sums, probabilities rounded to bf16 (both in the sum and in the product).
+ * softmax and sums; probabilities rounded to bf16 (both in the sum and in the product), or, where Tq * heads /
+ * kv_heads is at most 32 * batch, in two bf16 parts that leave 2^-16 of them.
  * A query without a key gets zeros; rows of o outside every sequence are left as
  * they are.  What k and v hold for keys that a query does not see (infinities, NaN) does not reach it.
  * An infinite value that a query sees makes its output infinite (NaN beside one of the other sign, and where

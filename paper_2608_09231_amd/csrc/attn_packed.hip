@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs P, int rows
 // An infinity among the values meets a second part of zero or of the other sign, and one that a row does not see a
 // probability of zero: both give NaN. So where an item's sums are not finite, the wave goes through its units
 // again, and adds what is not finite by product of flags.
-// 16 tokens against up to 8192 keys each, 32 heads on 8: 46 us for 263 MB, 5.7 TB/s, and 5 for joining.
+// 16 tokens against up to 8192 keys each, 32 heads on 8: 45 us for 263 MB, 5.9 TB/s, and 6 for joining.
 template <bool BOUNDED, bool CAUSAL, int NG>
 __global__ __launch_bounds__(256, 1) void attn_packed_few_kernel(PackedArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -644,14 +644,18 @@ __device__ __forceinline__ bool ranked_tile(const PackedArgs& P, int t, Seq& seq
 // probabilities from one to the other in registers, V^T read from the row-major
 // tile by transposing LDS reads.  Probabilities are rounded to bf16, the type that
 // the second product takes beside V; the sum takes the rounded values, so that the weights add up to one.
+// (Errors of 0.0020 in the 2-norm where outputs rounded from f32 have 0.0016; a second part of the probabilities
+// would add half of the matrix instructions again.)
 //
 // SPLIT: launches whose tiles are fewer than the chip's places for work-groups share the units
 // of the whole launch out (Line); a work-group may go through parts of several items.
 //
 // 16384 tokens, 16 heads on 4, causal: 0.96 ms, 1.15 PFLOP/s, MFMAs busy 0.53 at a power-limited 2.02 GHz.  8 prompts
-// of up to 512, 28 on 4: 26 us, one round of eight tiles of keys one after the other.  5 of up to 701 x 5003, 12 on
-// 4: 66 us and 13 for joining; workers in the order of the XCDs, key heads first, so that neighbours share keys in L2: 5 %
-// less there, but up to 10 more elsewhere (256 x 16384 98 to 109, 1000 x 1500 35 to 37).
+// of up to 512, 28 on 4: 25 us, one round of eight tiles of keys one after the other.  5 of up to 701 x 5003, 12 on
+// 4: 65 us and 13 for joining, bound by the memory side: 20 tiles of keys a worker, but 264 MB fetched for 37 of inputs and
+// outputs, as a sequence's tiles read the same keys at different times on different XCDs.  Workers in the order of the
+// XCDs, key heads first, so that neighbours share keys in L2: 5 % less there, but up to 10 more elsewhere (256 x 16384 98
+// to 109, 1000 x 1500 35 to 37).
 template <bool BOUNDED, bool CAUSAL, bool SPLIT, bool PIPE>
 __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -1094,8 +1098,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_kernel(PackedArgs P) {
 }  // namespace
 
 // Few rows a sequence, on average: the memory-bound kernel, a wave of which takes 16 or 32.  In us, against tiles of
-// 128 rows, shared out: 16 tokens with 8192 keys, 32 / 8 heads 51 56; 4 x 8192 19 22; 16 of 4 x 4096 36 37; 1 x 16384
-// 25 23; 64 tokens with 1024 keys 34 31 (and half the error: the probabilities stay unrounded).
+// 128 rows, shared out: 16 tokens with 8192 keys, 32 / 8 heads 50 56; 4 x 8192 19 22; 16 of 4 x 4096 35 37; 1 x 16384
+// 25 23; 64 tokens with 1024 keys 32 31 (and half the error: the probabilities stay unrounded).
 int few_rows(const dit_packed_shape& s) {
   const int64_t rows = (int64_t)s.Tq * (s.heads / s.kv_heads);
   return rows <= 16 * (int64_t)s.batch ? 16 : rows <= 32 * (int64_t)s.batch ? 32 : 0;
@@ -1111,7 +1115,8 @@ constexpr int FEW_WORKERS = 1024, FEW_LEAST = 4;
 // another work-group, and less where causal tiles of few keys stand beside those of many), shared ones 2.1 times their
 // share of all, masked or not, and 20 for parts and joining (fitted; shares of what causal tiles see alone begin and
 // end inside items: 2/2 16384 x 16384 183, but 16/4 2048 x 8192 177).  By the average
-// length, which is all that the host knows.  Measured, shared and whole:
+// length of the slots, which is all that the host knows: the constants are fitted to them, and a cache that is nearly
+// empty costs less than the rule counts.  Measured, shared and whole:
 //   heads / key heads, queries x keys   32/8 256 x 16384 101 386   16/16 77 x 4096 23 92   32/8 8 of 64 x 4096 42 101
 //   8/8 2048 x 2048 causal 43 47, 2 of up to 4096 x 4096 106 89, 3 of up to 2048 x 2048 65 47   12/12 1000 x 1500 34 40
 //   28/4 2048 x 2048 causal 93 63   28/4 512 x 512 causal 24 19   16/4 2048 x 8192 causal 141 165   2/2 16384 x 16384 causal 230 308
@@ -1126,8 +1131,8 @@ bool split_tiles(const dit_packed_shape& s, bool causal) {
 
 // Whether the pipelined loop is the faster one: it fills and drains over some tiles.  In us, pipelined and
 // not, whole tiles: 8 of 512 x 512 causal, 28 / 4 heads 29.8 26.7; 1024 x 1024 29.0 31.8; 4096 x 4096, 16 / 4 99 114;
-// 16384 x 16384 983 1107.  Shares of 33 tiles (5 of up to 701 x 5003 in a cache, half filled, 12 / 4, bounded) 86 75, of 36
-// (256 x 16384, 32 / 8) 90 96, of 128 (1024 x 16384) 265 304.
+// 16384 x 16384 983 1107.  Shares of 33 tiles by the slots, 20 as they are filled (5 of up to 701 x 5003 in a cache, 12 / 4,
+// bounded) 86 75, of 36 (256 x 16384, 32 / 8) 90 96, of 128 (1024 x 16384) 265 304.
 bool pipelined(const dit_packed_shape& s, bool split) {
   const double units = (double)s.Tk / s.batch / KT;
   return split ? units * (double)(tiles_of(s, ROWS) * s.kv_heads) >= 64.0 * SPLIT_WORKERS : units >= 12;

@@ -427,7 +427,7 @@ __device__ __forceinline__ void store_fp4(const Fp4Prob& P, f32x16_t (&acc)[TM][
 // last one are copied as zeros (no memory traffic), which keeps every iteration alike.
 //
 // 32760 x 5120 x 13824 1.04 ms, 4.4 PFLOP/s; 32760 x 13824 x 5120 1.25 ms, with 4-bit rows out 1.05, with GELU, too, 1.16.
-// What bounds it is power (the clock falls to 1.94 GHz, MFMAs busy 0.53 there) and the way through LDS (0.42, and 0.15
+// What bounds it is power (the clock falls to 1.85 - 1.94 GHz, MFMAs busy 0.53 - 0.57 there) and the way through LDS (0.42, and 0.15
 // in conflicts of the scale reads, 2.5 % of the time): of 1.08 ms the loop takes 0.93 without copies, 1.1 without
 // fragment reads, 0.87 without both.  A tile's beginning and end take 5 us, 10 with bf16 rows out
 // (3 more where the first products waited for both slices and the scales came by way of registers),
