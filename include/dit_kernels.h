@@ -389,7 +389,8 @@ typedef struct dit_packed_shape {
  * A query without a key gets zeros; rows of o outside every sequence are left as
  * they are.  What k and v hold for keys that a query does not see (infinities, NaN) does not reach it.
  * An infinite value that a query sees makes its output infinite (NaN beside one of the other sign, and where
- * its probability is below f32's least number).
+ * its probability is below f32's least number).  Sums are f32 until they are divided: values above 2^120 over
+ * the number of keys may give infinities.
  * Sequences of a batch may be of any lengths, single queries against long caches among them.
  *   flags  0, DIT_ATTN_BOUNDED_LOGITS, DIT_ATTN_CAUSAL or both
  *   ws     device, dit_attention_packed_ws_bytes(s) (0: then NULL will do; the offsets are not read for it), 16-byte aligned
